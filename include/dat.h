@@ -234,6 +234,95 @@ dat_status dat_lamb_update(dat_model* m, const float* grads, int use_adam, float
                            float beta2, float zeta, float weight_decay, float c_l, float c_u, int t,
                            void* stream);
 
+/* ---- AdamW over a tensor table ----------------------------------------------------------------------
+ * One step for every tensor of a flat parameter vector (tensor t = elements offsets[t] .. offsets[t+1]-1), t = 1, 2, ...:
+ *   m <- b1 m + (1-b1) g;  v <- b2 v + (1-b2) (g g);
+ *   theta <- theta - lr * ( (m c1) / (sqrt(v c2) + eps) + wd_t theta ),   c1 = 1/(1-b1^t), c2 = 1/(1-b2^t),
+ * in fp32, one rounding per operation as bracketed (1-b, c1 and c2 are formed in fp64 and rounded once).
+ *   theta: device fp32 [d];  grads: device, fp32 or bf16 by `grad_dtype`, [d];  offsets_dev: device int64 [num_tensors+1];
+ *   decay: optional device fp32 [num_tensors], wd_t = decay[t] (tensors that do not decay have 0); NULL: wd_t = weight_decay.
+ *   theta_bf16: optional device bf16 [d], receives the updated parameters rounded to nearest-even (the compute copy).
+ * state_bits = 32: m, v device fp32 [d]; `scales` and `seed` are not used.
+ * state_bits = 8: m, v device uint8 [d]; scales device int16 [dat_adamw_slots(d, num_tensors)][2].  256 consecutive elements of a
+ *   tensor (the last ones of a tensor may be fewer) are a block; block j of tensor t has the slot offsets[t]/256 + t + j, whose
+ *   scales are { s_m, s_v }.  With T(x) = (bits of fp32 |x|) >> 20, which counts eighths of a binade, a moment x is stored as
+ *   m: c = T - s_m + 127 in 7 bits and the sign in the eighth, v: c = T - s_v + 255, s = T(largest of the block) + 1: 16 binades
+ *   for m, 32 for v.  c <= 0 is stored as 0 and means zero, except that a v > 0 is stored as at least 1: no denominator vanishes
+ *   beside a moment that does not.  Rounding is stochastic, T = min((bits + 16 r + 8) >> 20, 0x7f7), unbiased in m and in v (rounding to
+ *   nearest would freeze v, which changes by a thousandth a step where a code is worth an eighth): r is the low (m) or high (v)
+ *   half of word i mod 4 of the Philox4x32-10 block slot*64 + i/4, stream 2, key = seed, i = place in the block.  Pass another
+ *   seed with every step.  Zeroed codes and scales are zero moments.
+ *   A block whose m or v holds a NaN or an infinity gets s = -1: from then on the moment decodes to NaN in the whole block
+ *   (with 32 bits in that element alone), and so do the parameters it updates.
+ * All pointers need the alignment of their elements only.  t, lr and seed are launch arguments: a captured graph repeats them.
+ * Asynchronous on `stream`, no allocation.  DAT_ERR_ARG: null pointers, state_bits not 8 or 32, t < 1, b1 or b2 outside [0,1),
+ * lr, eps or weight_decay negative or NaN, more than 2^31-1 slots.  d = 0: nothing happens.
+ * dat_adamw_moments: the values that 8-bit moments stand for, device fp32 [d] each (a checkpoint, a change to 32 bits).
+ * dat_model_adamw_update: the same step on a model's master parameters; conv and linear weights decay, biases, scales and shifts
+ *   do not.  The moments live in the model (allocated on the first call, zero; `state_bits` is fixed from then on:
+ *   DAT_ERR_UNSUPPORTED otherwise); the bf16 compute copies of the weights are refreshed afterwards. */
+int64_t dat_adamw_slots(int64_t d, int num_tensors);
+dat_status dat_adamw_update(float* theta, const void* grads, dat_dtype grad_dtype, const int64_t* offsets_dev, int num_tensors,
+                            int64_t d, int state_bits, void* m, void* v, int16_t* scales, uint64_t seed, float lr, float beta1,
+                            float beta2, float eps, float weight_decay, const float* decay, int t, uint16_t* theta_bf16,
+                            void* stream);
+dat_status dat_adamw_moments(const uint8_t* m, const uint8_t* v, const int16_t* scales, const int64_t* offsets_dev,
+                             int num_tensors, int64_t d, float* m_out, float* v_out, void* stream);
+dat_status dat_model_adamw_update(dat_model* m, const float* grads, int state_bits, uint64_t seed, float lr, float beta1,
+                                  float beta2, float eps, float weight_decay, int t, void* stream);
+
+/* ---- log probabilities of given labels ---------------------------------------------------------------
+ * Rows of logits, device fp32 or bf16 [N][V], row n at logits + n*ld elements (ld >= V), any alignment of the rows:
+ *   lse[n] = log sum_i exp(x_i);  logp[n] = x_y - lse, y = labels[n];  entropy[n] = -sum_i p_i log p_i, p = exp(x - lse);
+ *   top_index[n][0..top-1] (int32), top_logp[n][0..top-1]: the `top` largest logits in descending order, equal ones by ascending
+ *   index, and their log probabilities.
+ * labels: device int32 [N].  logp (with labels), entropy, lse, top_logp and top_index (together, top >= 1): device fp32 [N] or
+ * [N][top]; each may be NULL.  0 <= top <= DAT_MAX_TOP, also above V.
+ *   A logit of -inf is a class that is not allowed: probability 0, never an alternative; places without one have index -1 and
+ *   log probability -inf.  A row with nothing else has lse = -inf, entropy 0, and logp -inf.
+ *   A row that holds a NaN or +inf has NaN for lse, logp, entropy and top_logp, and index -1.
+ *   A label outside [0, V) gives a NaN logp and, in the gradient, no one-hot term (as in every call that takes labels).
+ * dat_log_probs_backward: dlogits[n][i] = dlogp[n] ([i = y] - p_i) - dentropy[n] p_i (log p_i + entropy[n]), rounded once to
+ *   `dtype`; rows at dlogits + n*ldd.  labels, dlogp: device, together or both NULL; entropy, dentropy likewise.  lse: as the forward call
+ *   wrote it.  p_i = 0 gives no entropy term; a row with nothing allowed gets zeros, one whose lse is NaN gets NaN.  dlogits may
+ *   be the logits themselves (then ldd = ld); elements between the rows are not touched.
+ * workspace: device, 16-byte aligned, dat_log_probs_workspace(N, V, top) bytes (may be 0, then NULL is allowed); nothing in it
+ * outlives the call.  Asynchronous on `stream`, no allocation.  N = 0: nothing happens.  DAT_ERR_ARG: null or misaligned
+ * pointers, N or top negative, top > DAT_MAX_TOP, V < 1, ld < V, a workspace that is too small; DAT_ERR_SHAPE: V > 2^30, N > 2^31-1. */
+#define DAT_MAX_TOP 32
+size_t dat_log_probs_workspace(int64_t N, int64_t V, int top);
+dat_status dat_log_probs(const void* logits, dat_dtype dtype, int64_t N, int64_t V, int64_t ld, const int32_t* labels, int top,
+                         float* logp, float* entropy, float* lse, float* top_logp, int32_t* top_index, void* workspace,
+                         size_t workspace_bytes, void* stream);
+dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype, int64_t N, int64_t V, int64_t ld, const int32_t* labels,
+                                  const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                                  void* dlogits, int64_t ldd, void* stream);
+
+/* ---- group normalisation with an activation, channels last ------------------------------------------------
+ * x, y, dy, dx: device, fp32 or bf16 by `dtype`, [B,H,W,C]; groups of C/groups consecutive channels, each normalised over the
+ * H*W*C/groups values of one image (no sample enters another's result):
+ *   xhat = (x - mean) rstd,  rstd = 1/sqrt(var + eps) (biased variance),  z = xhat gamma + beta,  y = act(z);
+ *   act: none, ReLU max(z, 0), SiLU z/(1 + exp(-z)).  One fp32 rounding per operation as written; y is rounded once to `dtype`.
+ * gamma, beta: device fp32 [C], both NULL for 1 and 0.  mean, rstd: device fp32 [B][groups], written by the forward call (from
+ * deviations from the mean, not from a difference of squares) and read by the backward call.
+ *   dat_group_norm_backward:  dz = dy act'(z), ReLU'(z) = [z > 0] with z evaluated as in the forward call (no sign differs);
+ *   dbeta = sum dz, dgamma = sum dz xhat (device fp32 [C], both NULL to skip; written, not added to), sums in fp32 in a fixed order
+ *   (the same bits on every call);  dx = rstd (h - mean(h) - xhat mean(h xhat)), h = gamma dz, means over the group.  y is not needed.
+ * dx may be dy (same buffer), y may be x.  workspace: device, 16-byte aligned, dat_group_norm_workspace(pass, ...) bytes (pass 0 forward, 1
+ * backward; may be 0, then NULL is allowed); nothing in it outlives the call.  Asynchronous on `stream`, no allocation.
+ * B = 0: no output but dgamma = dbeta = 0.  DAT_ERR_ARG: null or misaligned pointers, sizes below 1 (B below 0), groups that
+ * do not divide C, unknown act or dtype, eps negative or NaN, a workspace that is too small; DAT_ERR_SHAPE: H*W*C, B*groups or
+ * B*C above 2^30. */
+typedef enum { DAT_ACT_NONE = 0, DAT_ACT_RELU = 1, DAT_ACT_SILU = 2 } dat_act;
+size_t dat_group_norm_workspace(int pass, dat_dtype dtype, int B, int H, int W, int C, int groups);
+dat_status dat_group_norm_forward(const void* x, const float* gamma, const float* beta, dat_dtype dtype, int B, int H, int W,
+                                  int C, int groups, float eps, dat_act act, void* y, float* mean, float* rstd,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+dat_status dat_group_norm_backward(const void* x, const void* dy, const float* gamma, const float* beta, const float* mean,
+                                   const float* rstd, dat_dtype dtype, int B, int H, int W, int C, int groups, dat_act act,
+                                   void* dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
 /* ---- convolution kernels on their own (bf16 storage, fp32 accumulate on MFMA) --------------
  * The three contractions behind dat_attack / dat_step, exposed for per-shape parity tests and
  * timing.  Tensors are device bf16 (uint16 bit patterns): x [B,H,W,Cin], w [Cout,k,k,Cin],

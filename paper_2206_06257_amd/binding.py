@@ -14,6 +14,8 @@ ARCH_PREACT_RESNET18, ARCH_WRN28_10 = 4, 5
 PHI_CE, PHI_TRADES_KL = 0, 1
 F32, BF16 = 0, 1
 INIT_ZERO, INIT_UNIFORM, INIT_GIVEN = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+MAX_TOP = 32
 
 EXPORTS = [
     "dat_model_create", "dat_model_destroy", "dat_model_num_params", "dat_model_tensor_table",
@@ -23,6 +25,8 @@ EXPORTS = [
     "dat_status_string", "dat_last_error", "dat_philox_uniform", "dat_profile_enable", "dat_profile_read", "dat_aggregate", "dat_lamb_update",
     "dat_attack_kl", "dat_step_reg", "dat_model_set_option", "dat_make_xadv",
     "dat_conv_backward_weight_static", "dat_conv_backward_weight_static_limit", "dat_set_kernel_option", "dat_conv_plan", "dat_model_grad_scales", "dat_quantize_scaled",
+    "dat_adamw_slots", "dat_adamw_update", "dat_adamw_moments", "dat_model_adamw_update", "dat_log_probs_workspace", "dat_log_probs",
+    "dat_log_probs_backward", "dat_group_norm_workspace", "dat_group_norm_forward", "dat_group_norm_backward",
     "dat_inspect_counts", "dat_inspect_op", "dat_inspect_tensor", "dat_inspect_read", "dat_inspect_bn",
 ]
 
@@ -81,6 +85,19 @@ for _n in ("dat_conv_forward", "dat_conv_backward_data", "dat_conv_backward_weig
 _lib.dat_philox_uniform.argtypes = [_u64, _i64, _u64, C.c_uint32, _vp, _vp]
 _lib.dat_aggregate.argtypes = [_vp, _vp, _i, _vp, _i, _i64, _i, _vp, _vp]
 _lib.dat_lamb_update.argtypes = [_vp, _vp, _i, _f, _f, _f, _f, _f, _f, _f, _i, _vp]
+_lib.dat_adamw_slots.restype = _i64
+_lib.dat_adamw_slots.argtypes = [_i64, _i]
+_lib.dat_adamw_update.argtypes = [_vp, _vp, _i, _vp, _i, _i64, _i, _vp, _vp, _vp, _u64, _f, _f, _f, _f, _f, _vp, _i, _vp, _vp]
+_lib.dat_adamw_moments.argtypes = [_vp, _vp, _vp, _vp, _i, _i64, _vp, _vp, _vp]
+_lib.dat_model_adamw_update.argtypes = [_vp, _vp, _i, _u64, _f, _f, _f, _f, _f, _i, _vp]
+_lib.dat_log_probs_workspace.restype = C.c_size_t
+_lib.dat_log_probs_workspace.argtypes = [_i64, _i64, _i]
+_lib.dat_log_probs.argtypes = [_vp, _i, _i64, _i64, _i64, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
+_lib.dat_log_probs_backward.argtypes = [_vp, _i, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp]
+_lib.dat_group_norm_workspace.restype = C.c_size_t
+_lib.dat_group_norm_workspace.argtypes = [_i] * 7
+_lib.dat_group_norm_forward.argtypes = [_vp, _vp, _vp] + [_i] * 6 + [_f, _i, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
+_lib.dat_group_norm_backward.argtypes = [_vp] * 6 + [_i] * 7 + [_vp, _vp, _vp, _vp, C.c_size_t, _vp]
 _lib.dat_attack_kl.argtypes = [_vp, _vp, _i, _f, _f, _i, _Init, _vp, _vp, _vp]
 _lib.dat_step_reg.argtypes = [_vp, _vp, _vp, _vp, _i, _f, _i, _vp, _vp, _vp]
 _lib.dat_profile_enable.argtypes = [_vp, _i]
@@ -225,6 +242,11 @@ class Model:
                     t=1, stream=None):
         _check(_lib.dat_lamb_update(self._h, _ptr(_dev(grads, torch.float32)), int(bool(use_adam)), eta, beta1, beta2, zeta,
                                     weight_decay, c_l, c_u, int(t), _stream(stream)), "dat_lamb_update")
+
+    def adamw_update(self, grads, lr, t, state_bits=32, seed=0, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, stream=None):
+        assert grads.numel() == self.d
+        _check(_lib.dat_model_adamw_update(self._h, _ptr(_dev(grads, torch.float32)), int(state_bits), int(seed) & 0xFFFFFFFFFFFFFFFF,
+                                           lr, beta1, beta2, eps, weight_decay, int(t), _stream(stream)), "dat_model_adamw_update")
 
     def set_option(self, opt, value):
         _check(_lib.dat_model_set_option(self._h, int(opt), int(value)), "dat_model_set_option")
@@ -386,6 +408,200 @@ def aggregate(q_list, scales_list, offsets_dev, d, bits, out=None, stream=None):
         out = torch.empty(d, dtype=torch.float32, device=q_list[0].device)
     _check(_lib.dat_aggregate(qp, sp, M, optr, T, d, bits, _ptr(out), _stream(stream)), "dat_aggregate")
     return out
+
+
+class _On:
+    """Runs a call on the tensors' device, on `stream` or on that device's current stream; what the call allocates belongs to it."""
+
+    def __init__(self, stream, *tensors):
+        device = tensors[0].device
+        for t in tensors:
+            if t is not None and (not t.is_cuda or t.device != device):
+                raise ValueError("all tensors of a call belong on one GPU: %s and %s" % (device, t.device))
+        if stream is not None and stream.device != device:
+            raise ValueError("the stream belongs to %s, the tensors are on %s" % (stream.device, device))
+        self._device, self._ctx = torch.cuda.device(device), None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self._device.__enter__()
+        if self._ctx is not None:
+            self._ctx.__enter__()
+        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *exc):
+        if self._ctx is not None:
+            self._ctx.__exit__(*exc)
+        self._device.__exit__(*exc)
+
+
+def _want(name, t, dtypes, shape=None, contiguous=True, optional=False):
+    """Checks a tensor argument of the calls below."""
+    if t is None and optional:
+        return
+    if t.dtype not in dtypes or (shape is not None and tuple(t.shape) != tuple(shape)) or (contiguous and not t.is_contiguous()):
+        raise ValueError("%s: %s %s%s, expected %s %s" % (name, t.dtype, tuple(t.shape), "" if t.is_contiguous() else " (not contiguous)",
+                                                          " or ".join(str(d) for d in dtypes), "" if shape is None else tuple(shape)))
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+def _code(t):
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def adamw_slots(d, num_tensors):
+    return int(_lib.dat_adamw_slots(d, num_tensors))
+
+
+def adamw_state(d, num_tensors, bits=32, device="cuda"):
+    """Zero moments of `d` parameters in `num_tensors` tensors: (m, v, scales), scales None with 32 bits."""
+    if bits == 32:
+        return torch.zeros(d, device=device), torch.zeros(d, device=device), None
+    if bits != 8:
+        raise ValueError("moments have 8 or 32 bits, not %r" % (bits,))
+    return (torch.zeros(d, dtype=torch.uint8, device=device), torch.zeros(d, dtype=torch.uint8, device=device),
+            torch.zeros(adamw_slots(d, num_tensors), 2, dtype=torch.int16, device=device))
+
+
+def _adamw_table(offsets_dev, d, num_tensors, m, v, scales):
+    """(pointer, tensors) of a table, and the checks of the moments."""
+    _want("m", m, (torch.float32, torch.uint8), (d,))
+    _want("v", v, (m.dtype,), (d,))
+    if isinstance(offsets_dev, tuple):
+        ptr, T = C.c_void_p(offsets_dev[0]), offsets_dev[1]
+    else:
+        _want("offsets_dev", offsets_dev, (torch.int64,))
+        ptr, T = _ptr(offsets_dev), offsets_dev.numel() - 1
+    if m.dtype == torch.uint8:
+        if scales is None:
+            raise ValueError("8-bit moments need their scales")
+        _want("scales", scales, (torch.int16,), (adamw_slots(d, T), 2))
+    return ptr, T
+
+
+def adamw_update(theta, grads, m, v, offsets_dev, lr, t, scales=None, seed=0, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0,
+                 decay=None, theta_bf16=None, stream=None):
+    """One AdamW step in place: theta fp32 [d], grads fp32 or bf16 [d], m and v fp32 or (with `scales`) uint8 [d] as adamw_state
+    makes them, offsets_dev an int64 CUDA tensor [T+1] or (pointer, T).  decay: fp32 [T], one weight decay for each tensor."""
+    d = theta.numel()
+    _want("theta", theta, (torch.float32,), (d,))
+    _want("grads", grads, _FLOATS, (d,))
+    _want("theta_bf16", theta_bf16, (torch.bfloat16,), (d,), optional=True)
+    ptr, T = _adamw_table(offsets_dev, d, None, m, v, scales)
+    _want("decay", decay, (torch.float32,), (T,), optional=True)
+    with _On(stream, theta, grads, m, v, scales, decay, theta_bf16, None if isinstance(offsets_dev, tuple) else offsets_dev) as st:
+        _check(_lib.dat_adamw_update(_ptr(theta), _ptr(grads), _code(grads), ptr, T, d, 8 if m.dtype == torch.uint8 else 32, _ptr(m), _ptr(v),
+                                     _ptr(scales), int(seed) & 0xFFFFFFFFFFFFFFFF, lr, beta1, beta2, eps, weight_decay, _ptr(decay),
+                                     int(t), _ptr(theta_bf16), st), "dat_adamw_update")
+
+
+def adamw_moments(m, v, scales, offsets_dev, stream=None):
+    """The fp32 values that 8-bit moments stand for."""
+    _want("m", m, (torch.uint8,))
+    d = m.numel()
+    ptr, T = _adamw_table(offsets_dev, d, None, m, v, scales)
+    with _On(stream, m, v, scales, None if isinstance(offsets_dev, tuple) else offsets_dev) as st:
+        m_out, v_out = torch.empty(d, device=m.device), torch.empty(d, device=m.device)
+        _check(_lib.dat_adamw_moments(_ptr(m), _ptr(v), _ptr(scales), ptr, T, d, _ptr(m_out), _ptr(v_out), st), "dat_adamw_moments")
+    return m_out, v_out
+
+
+def _rows(name, t, shape=None):
+    """Logits [N, V] whose rows are contiguous: the stride of the rows."""
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError("%s: expected %s, got %s" % (name, "[N, V]" if shape is None else tuple(shape), tuple(t.shape)))
+    _want(name, t, _FLOATS, contiguous=False)
+    N, V = t.shape
+    if (V > 1 and t.stride(1) != 1) or (N > 1 and t.stride(0) < V):
+        raise ValueError("%s: rows have to be contiguous and apart, strides are %s" % (name, tuple(t.stride())))
+    return max(t.stride(0), V) if N > 1 else V
+
+
+def log_probs(logits, labels=None, top=0, stream=None):
+    """Rows of logits [N, V] (fp32 or bf16, rows may be padded), labels int32 [N] or None -> (logp, entropy, lse, top_logp, top_index):
+    fp32 [N] (logp None without labels), fp32 and int32 [N, top] (None for top = 0); see dat_log_probs."""
+    ld = _rows("logits", logits)
+    N, V = logits.shape
+    _want("labels", labels, (torch.int32,), (N,), optional=True)
+    with _On(stream, logits, labels) as st:
+        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=logits.device)  # noqa: E731
+        logp, entropy, lse = None if labels is None else new(N), new(N), new(N)
+        top_logp, top_index = (new(N, top), new(N, top, dtype=torch.int32)) if top > 0 else (None, None)
+        size = int(_lib.dat_log_probs_workspace(N, V, top))
+        ws = new(size, dtype=torch.uint8) if size else None
+        _check(_lib.dat_log_probs(_ptr(logits), _code(logits), N, V, ld, _ptr(labels), top, _ptr(logp), _ptr(entropy), _ptr(lse),
+                                  _ptr(top_logp), _ptr(top_index), _ptr(ws), size, st), "dat_log_probs")
+    return logp, entropy, lse, top_logp, top_index
+
+
+def log_probs_backward(logits, labels, lse, entropy=None, dlogp=None, dentropy=None, dlogits=None, stream=None):
+    """Gradient by the logits for incoming gradients of logp and of the entropies (either may be None); dlogits may be the logits."""
+    ld = _rows("logits", logits)
+    N, V = logits.shape
+    f32 = (torch.float32,)
+    _want("lse", lse, f32, (N,))
+    _want("labels", labels, (torch.int32,), (N,), optional=dlogp is None)
+    for name, t in (("entropy", entropy), ("dentropy", dentropy)):
+        _want(name, t, f32, (N,), optional=dentropy is None)
+    _want("dlogp", dlogp, f32, (N,), optional=True)
+    with _On(stream, logits, lse, labels, entropy, dlogp, dentropy, dlogits) as st:
+        if dlogits is None:
+            dlogits = torch.empty(N, V, dtype=logits.dtype, device=logits.device)
+        ldd = _rows("dlogits", dlogits, (N, V))
+        _want("dlogits", dlogits, (logits.dtype,), contiguous=False)
+        _check(_lib.dat_log_probs_backward(_ptr(logits), _code(logits), N, V, ld, None if dlogp is None else _ptr(labels), _ptr(lse),
+                                           None if dentropy is None else _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), ldd, st),
+               "dat_log_probs_backward")
+    return dlogits
+
+
+def _gn_workspace(pass_, x, groups):
+    B, H, W, Cc = x.shape
+    size = int(_lib.dat_group_norm_workspace(pass_, _code(x), B, H, W, Cc, groups))
+    return (torch.empty(size, dtype=torch.uint8, device=x.device) if size else None), size
+
+
+def group_norm_forward(x, gamma, beta, groups, act=ACT_NONE, eps=1e-5, y=None, stream=None):
+    """x [B,H,W,C] fp32 or bf16, gamma and beta fp32 [C] or both None -> (y like x, mean, rstd fp32 [B, groups])."""
+    if x.dim() != 4:
+        raise ValueError("x: expected [B, H, W, C], got %s" % (tuple(x.shape),))
+    B, H, W, Cc = x.shape
+    _want("x", x, _FLOATS)
+    _want("gamma", gamma, (torch.float32,), (Cc,), optional=True)
+    _want("beta", beta, (torch.float32,), (Cc,), optional=True)
+    _want("y", y, (x.dtype,), x.shape, optional=True)
+    with _On(stream, x, gamma, beta, y) as st:
+        if y is None:
+            y = torch.empty_like(x)
+        mean, rstd = (torch.empty(B, max(groups, 0), device=x.device) for _ in range(2))
+        ws, size = _gn_workspace(0, x, groups)
+        _check(_lib.dat_group_norm_forward(_ptr(x), _ptr(gamma), _ptr(beta), _code(x), B, H, W, Cc, groups, eps, act, _ptr(y), _ptr(mean),
+                                           _ptr(rstd), _ptr(ws), size, st), "dat_group_norm_forward")
+    return y, mean, rstd
+
+
+def group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, act=ACT_NONE, dx=None, dgamma=None, dbeta=None, stream=None):
+    """Gradients of group_norm_forward from its mean and rstd -> (dx like x, dgamma, dbeta fp32 [C])."""
+    if x.dim() != 4:
+        raise ValueError("x: expected [B, H, W, C], got %s" % (tuple(x.shape),))
+    B, H, W, Cc = x.shape
+    f32 = (torch.float32,)
+    _want("x", x, _FLOATS)
+    for name, t in (("dy", dy), ("dx", dx)):
+        _want(name, t, (x.dtype,), x.shape, optional=name == "dx")
+    for name, t in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
+        _want(name, t, f32, (Cc,), optional=True)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _want(name, t, f32, (B, groups))
+    with _On(stream, x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta) as st:
+        dx = torch.empty_like(x) if dx is None else dx
+        dgamma = torch.empty(Cc, device=x.device) if dgamma is None else dgamma
+        dbeta = torch.empty(Cc, device=x.device) if dbeta is None else dbeta
+        ws, size = _gn_workspace(1, x, groups)
+        _check(_lib.dat_group_norm_backward(_ptr(x), _ptr(dy), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _code(x), B, H, W, Cc, groups,
+                                            act, _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), size, st), "dat_group_norm_backward")
+    return dx, dgamma, dbeta
 
 
 def philox_uniform(start, n, seed, stream_id, device="cuda"):

@@ -212,6 +212,15 @@ struct LambParams {
 dat_status launch_lamb(float* theta, const float* g, float* m, float* v, float* u, const int64_t* off, int T, int64_t d,
                        const LambParams& hp, double* norms, hipStream_t st);
 
+struct AdamwParams {
+  float lr, b1, b2, eps, wd;   // wd multiplies the tensor's decay where there is a table of them
+  float om1, om2, c1, c2;      // 1-b, 1/(1-b^t)
+};
+// Checks the ranges that dat.h gives and forms the derived values; false: an argument is out of range.
+bool adamw_params(float lr, float beta1, float beta2, float eps, float weight_decay, int t, AdamwParams* hp);
+dat_status launch_adamw(float* theta, const void* g, int g_dtype, const int64_t* off, int T, int64_t d, int bits, void* m, void* v,
+                        int16_t* scales, uint64_t seed, const AdamwParams& hp, const float* decay, bf16_t* copy, hipStream_t st);
+
 struct AggregateArgs {
   const uint8_t* q[DAT_MAX_WORKERS];
   const float* scales[DAT_MAX_WORKERS];

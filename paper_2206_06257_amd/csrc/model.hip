@@ -11,6 +11,8 @@
 #include <string.h>
 #include <algorithm>
 #include <math.h>
+#include <memory>
+#include <new>
 #include <vector>
 #include "kernels.h"
 
@@ -108,6 +110,9 @@ struct dat_model {
   struct PassBank { std::vector<void*> act; std::vector<float*> mean, rstd; std::vector<uint8_t*> mask, argmax; bool ready = false; } bank2;
   bool keep_both_passes = true;
   float* opt_m = nullptr; float* opt_v = nullptr; float* opt_u = nullptr; double* opt_norms = nullptr;   // LAMB state
+  void* adamw_m = nullptr; void* adamw_v = nullptr; int16_t* adamw_scales = nullptr;   // AdamW moments ...
+  float* adamw_decays = nullptr;     //   ... per tensor 1 (conv and linear weights) or 0
+  int adamw_bits = 0;                //   ... their width, fixed by the first update
   // optional per-launch timing (dat_profile_*): one event pair per launch group
   bool prof = false;
   struct ProfRec { int cls; hipEvent_t a, b; double work; int64_t nlaunch; };
@@ -1175,6 +1180,37 @@ extern "C" dat_status dat_lamb_update(dat_model* m, const float* grads, int use_
   hp.inv_bc2 = use_adam ? (float)(1.0 / (1.0 - pow((double)beta2, t))) : 1.0f;
   DAT_TRY(launch_lamb(m->master, grads, m->opt_m, m->opt_v, m->opt_u, m->offsets_dev, (int)m->ptab.size(), m->d, hp,
                       m->opt_norms, st));
+  DAT_TRY(refresh_compute(*m, st));
+  return DAT_OK;
+}
+
+extern "C" dat_status dat_model_adamw_update(dat_model* m, const float* grads, int state_bits, uint64_t seed, float lr, float beta1,
+                                             float beta2, float eps, float weight_decay, int t, void* stream) {
+  AdamwParams hp;
+  if (!m || !grads || !aligned(grads, 4) || (state_bits != 8 && state_bits != 32)) return DAT_ERR_ARG;
+  if (!adamw_params(lr, beta1, beta2, eps, weight_decay, t, &hp)) return DAT_ERR_ARG;
+  if (m->adamw_bits && m->adamw_bits != state_bits)
+    return fail_with(DAT_ERR_UNSUPPORTED, "the model's AdamW moments have the width of the first update");
+  hipStream_t st = (hipStream_t)stream;
+  const int T = (int)m->ptab.size();
+  if (!m->adamw_bits) {
+    const size_t bytes = (size_t)m->d * (state_bits / 8), slots = (size_t)dat_adamw_slots(m->d, T);
+    if (!m->adamw_decays) DAT_TRY(dev_alloc(*m, &m->adamw_decays, (size_t)T * 4));
+    std::unique_ptr<float[]> decays(new (std::nothrow) float[T]);
+    if (!decays) return DAT_ERR_NOMEM;
+    for (int i = 0; i < T; ++i) decays[i] = m->ptab[i].kind == 0 || m->ptab[i].kind == 4 ? 1.0f : 0.0f;
+    DAT_HIP(hipMemcpy(m->adamw_decays, decays.get(), (size_t)T * 4, hipMemcpyHostToDevice));
+    if (state_bits == 8 && !m->adamw_scales) DAT_TRY(dev_alloc(*m, &m->adamw_scales, slots * 4));
+    void *mm = nullptr, *vv = nullptr;
+    DAT_TRY(dev_alloc(*m, &mm, (bytes + 3) / 4 * 4));
+    DAT_TRY(dev_alloc(*m, &vv, (bytes + 3) / 4 * 4));
+    DAT_TRY(launch_fill_zero(mm, bytes, st));
+    DAT_TRY(launch_fill_zero(vv, bytes, st));
+    if (state_bits == 8) DAT_TRY(launch_fill_zero(m->adamw_scales, slots * 4, st));
+    m->adamw_m = mm; m->adamw_v = vv; m->adamw_bits = state_bits;
+  }
+  DAT_TRY(launch_adamw(m->master, grads, DAT_F32, m->offsets_dev, T, m->d, state_bits, m->adamw_m, m->adamw_v, m->adamw_scales, seed,
+                       hp, m->adamw_decays, nullptr, st));
   DAT_TRY(refresh_compute(*m, st));
   return DAT_OK;
 }

@@ -1,0 +1,659 @@
+"""Group norm, label log probabilities and AdamW on the GPU against plain forms in 64 bits, over lengths, types, strides, masks,
+streams and captured graphs.
+
+Tolerances count roundings: U = 2^-24 is half a step of fp32, half(t) that of the stored type relative to the value, and a sum
+of n terms kept by threads that add at most n/64 of them one after the other, then in a tree, is off by at most (n/64 + 16) U
+times the sum of the magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+from tests import plain_ops as po
+
+pytestmark = pytest.mark.gpu
+U = po.U
+
+
+@pytest.fixture(scope="module")
+def dat():
+    import paper_2206_06257_amd as dat
+    return dat
+
+
+def half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+def assert_near(got, want, tol, what):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    tol = np.broadcast_to(tol, want.shape)
+    bad = ~(np.abs(got - want) <= tol) & ~((got == want) | (np.isnan(got) & np.isnan(want)))
+    if bad.any():
+        i = tuple(np.argwhere(bad)[0])
+        raise AssertionError("%s: %d of %d off, first %s: %r, expected %r within %r" % (what, bad.sum(), bad.size, i, got[i], want[i], tol[i]))
+
+
+# ---- group norm -------------------------------------------------------------------------------------------------------
+# (B, H, W, C, groups): one value, one pixel, one image, odd sizes, one group, a group for each channel, wide, channels that are no
+# multiple of a vector, groups that straddle vectors, many images, long maps
+GN_SHAPES = [(1, 1, 1, 1, 1), (1, 1, 1, 64, 32), (2, 1, 3, 8, 8), (1, 8, 8, 512, 32), (3, 7, 5, 24, 4), (2, 9, 9, 35, 7), (5, 4, 4, 160, 32),
+             (2, 3, 3, 2048, 32), (2, 33, 31, 40, 5), (65, 4, 4, 16, 2), (3, 56, 56, 64, 32), (1, 128, 128, 32, 1), (2, 57, 61, 120, 120),
+             (1, 40, 40, 640, 32), (4, 2, 2, 6, 3), (2, 112, 112, 16, 4), (1, 30, 30, 1024, 2)]
+
+
+def gn_inputs(shape, dtype, seed, offset=0.5):
+    B, H, W, C, G = shape
+    x = (randn(seed, B, H, W, C) * torch.exp(0.5 * randn(seed + 1, C)) + offset * randn(seed + 2, C)).to(dtype)
+    return x, 1 + 0.2 * randn(seed + 3, C), 0.2 * randn(seed + 4, C), randn(seed + 5, B, H, W, C).to(dtype)
+
+
+def gn_check_forward(dat, x, gamma, beta, G, act, out, eps=1e-5):
+    y, mean, rstd = out
+    B, H, W, C = x.shape
+    n = H * W * C // G
+    xs = host(x)
+    g, b = (np.ones(C), np.zeros(C)) if gamma is None else (host(gamma), host(beta))
+    want, m, r, xhat = po.gn_forward(xs, g, b, G, act, eps)
+    K = n / 64 + 32
+    size = np.abs(xs).reshape(B, -1, G, C // G).max(axis=(1, 3))
+    assert_near(host(mean), m, K * U * size, "mean")
+    # var is off by K U var from its sum and by 4 U size |x - mean| from the rounded differences
+    dev = K * U + 4 * U * size * r * (1 + size * r * K * U)
+    assert_near(host(rstd), r, dev * r, "rstd")
+    spread = lambda s: np.repeat(s, C // G, axis=1)[:, None, None, :]  # noqa: E731
+    tol_z = np.abs(g) * (np.abs(xhat) * (spread(dev) + 4 * U) + spread(size * r) * (K + 2) * U) + 2 * U * (np.abs(xhat * g) + np.abs(b))
+    assert_near(host(y), want, 1.1 * tol_z + (half(y.dtype) + 16 * U) * np.abs(want) * 1.01, "y")
+
+
+def gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, act, out):
+    dx, dgamma, dbeta = out
+    B, H, W, C = x.shape
+    g, b = (np.ones(C), np.zeros(C)) if gamma is None else (host(gamma), host(beta))
+    want, wg, wb, size, sg, sb = po.gn_backward(host(x), host(dy), g, b, host(mean), host(rstd), G, act)
+    # SiLU' = s (1 + z (1-s)) loses up to (4 + |z|) U of 1 + |z| <= 1 + |xhat gamma| + |beta|; dz of at most 12 |dy| in size
+    z = np.abs(po.gn_z32(host(x), g, b, host(mean), host(rstd))).max() + 1 if act == 2 else 1.0
+    dyh = np.abs(host(dy)).max() * np.abs(g).max() * host(rstd).max() if act == 2 else 0.0
+    K = H * W * C // G / 64 + 32
+    assert_near(host(dx), want, (K * size + 16 * z * z * dyh) * U + (half(dx.dtype)) * np.abs(want) * 1.01, "dx")
+    K = B * H * W / 64 + B + 32
+    extra = 16 * z * z * np.abs(host(dy)).sum(axis=(0, 1, 2)) if act == 2 else 0.0
+    assert_near(host(dgamma), wg, (K * sg + extra * 12) * U, "dgamma")
+    assert_near(host(dbeta), wb, (K * sb + extra) * U, "dbeta")
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", GN_SHAPES)
+def test_group_norm(dat, shape, dtype, act):
+    B, H, W, C, G = shape
+    x, gamma, beta, dy = gn_inputs(shape, dtype, 100)
+    y, mean, rstd = dat.group_norm_forward(x, gamma, beta, G, act)
+    gn_check_forward(dat, x, gamma, beta, G, act, (y, mean, rstd))
+    out = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, G, act)
+    gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, act, out)
+    again = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, G, act)
+    assert all(torch.equal(a, b) for a, b in zip(out, again))      # sums in a fixed order
+
+
+@pytest.mark.parametrize("shape", [(2, 9, 9, 40, 5), (3, 56, 56, 64, 32), (2, 5, 5, 35, 7)])
+def test_group_norm_far_mean(dat, shape):
+    """Values whose mean is a thousand times their spread: a difference of squares would lose all digits."""
+    x, gamma, beta, dy = gn_inputs(shape, torch.float32, 7)
+    x = x * 0.1 + 100.0
+    out = dat.group_norm_forward(x, gamma, beta, shape[4], 0)
+    gn_check_forward(dat, x, gamma, beta, shape[4], 0, out)
+
+
+def test_group_norm_without_scale_and_in_place(dat):
+    shape = (3, 14, 14, 64, 16)
+    x, gamma, beta, dy = gn_inputs(shape, torch.bfloat16, 31)
+    gn_check_forward(dat, x, None, None, 16, 1, dat.group_norm_forward(x, None, None, 16, 1))
+    y, mean, rstd = dat.group_norm_forward(x, gamma, beta, 16, 2)
+    own = x.clone()
+    y2, m2, r2 = dat.group_norm_forward(own, gamma, beta, 16, 2, y=own)
+    assert y2 is own and torch.equal(own, y) and torch.equal(m2, mean) and torch.equal(r2, rstd)
+    dx, dgamma, dbeta = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, 16, 2)
+    own = dy.clone()
+    dx2, dg2, db2 = dat.group_norm_backward(x, own, gamma, beta, mean, rstd, 16, 2, dx=own)
+    assert dx2 is own and torch.equal(own, dx) and torch.equal(dg2, dgamma) and torch.equal(db2, dbeta)
+    out = dat.group_norm_backward(x, dy, None, None, mean, rstd, 16, 1)
+    gn_check_backward(dat, x, dy, None, None, mean, rstd, 16, 1, out)
+
+
+@pytest.mark.parametrize("shape", [(2, 9, 9, 40, 5), (2, 30, 30, 64, 16)])
+def test_group_norm_unaligned_buffers(dat, shape):
+    """Buffers that start at any element: same values, nothing written beside the outputs."""
+    B, H, W, C, G = shape
+    for dtype in (torch.float32, torch.bfloat16):
+        x, gamma, beta, dy = gn_inputs(shape, dtype, 41)
+        n = x.numel()
+
+        def shifted(t):
+            buf = torch.full((n + 16,), 7.0, dtype=dtype, device="cuda")
+            buf[1:n + 1] = t.reshape(-1)
+            return buf, buf[1:n + 1].view(shape[:4])
+
+        (_, xs), (_, dys), (by, ys), (bx, dxs) = shifted(x), shifted(dy), shifted(torch.zeros_like(x)), shifted(torch.zeros_like(x))
+        y, mean, rstd = dat.group_norm_forward(xs, gamma, beta, G, 1, y=ys)
+        gn_check_forward(dat, x, gamma, beta, G, 1, (y, mean, rstd))
+        out = dat.group_norm_backward(xs, dys, gamma, beta, mean, rstd, G, 1, dx=dxs)
+        gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, 1, out)
+        for buf in (by, bx):
+            assert float(buf[0]) == 7.0 and (buf[n + 1:] == 7.0).all()
+
+
+def test_group_norm_non_finite_stays_in_its_group(dat):
+    """A NaN or an infinity spoils the group of the image that it is in, and the channel sums of that group."""
+    shape = (3, 6, 6, 32, 4)
+    x, gamma, beta, dy = gn_inputs(shape, torch.float32, 51)
+    clean = dat.group_norm_forward(x, gamma, beta, 4, 1)
+    bad = x.clone()
+    bad[1, 2, 3, 9] = float("nan")
+    bad[2, 0, 0, 31] = float("inf")
+    y, mean, rstd = dat.group_norm_forward(bad, gamma, beta, 4, 1)
+    hit = torch.zeros(3, 4, dtype=torch.bool, device="cuda")
+    hit[1, 1] = hit[2, 3] = True
+    assert torch.isnan(mean[1, 1]) and not torch.isfinite(mean[2, 3]) and torch.isnan(rstd[hit]).all()
+    assert torch.equal(mean[~hit], clean[1][~hit]) and torch.equal(rstd[~hit], clean[2][~hit])
+    per = hit[:, None, None, :].expand(3, 6, 6, 4).repeat_interleave(8, dim=3)
+    assert torch.isnan(y[per]).all() and torch.equal(y[~per], clean[0][~per])
+    dx, dgamma, dbeta = dat.group_norm_backward(bad, dy, gamma, beta, mean, rstd, 4, 2)
+    assert torch.isnan(dx[per]).all() and torch.isfinite(dx[~per]).all()
+    channels = per.any(dim=0).any(dim=0).any(dim=0)
+    assert torch.isfinite(dgamma[~channels]).all() and torch.isnan(dgamma[channels]).all()
+
+
+def test_group_norm_no_images(dat):
+    x = torch.empty(0, 4, 4, 16, device="cuda")
+    y, mean, rstd = dat.group_norm_forward(x, None, None, 4)
+    assert y.shape == x.shape and mean.shape == (0, 4)
+    dx, dgamma, dbeta = dat.group_norm_backward(x, x, None, None, mean, rstd, 4)
+    assert float(dgamma.abs().max()) == 0.0 and float(dbeta.abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("act", [0, 2])
+def test_group_norm_gradient_against_differences(dat, act):
+    """<gradient, direction> against central differences of the 64-bit forward formula (step 1e-4: truncation below 1e-7 of the
+    magnitudes, rounding below 1e-11)."""
+    shape, G = (2, 5, 5, 12, 3), 3
+    x, gamma, beta, w = gn_inputs(shape, torch.float32, 61)
+    _, mean, rstd = dat.group_norm_forward(x, gamma, beta, G, act)
+    grads = [host(t) for t in dat.group_norm_backward(x, w, gamma, beta, mean, rstd, G, act)]
+    at = [host(t) for t in (x, gamma, beta)]
+    rng = np.random.default_rng(5)
+    for k in range(3):
+        u = rng.standard_normal(at[k].shape)
+        ends = []
+        for sign in (1, -1):
+            p = [a + sign * 1e-4 * u if i == k else a for i, a in enumerate(at)]
+            ends.append((po.gn_forward(p[0], p[1], p[2], G, act, 1e-5)[0] * host(w)).sum())
+        want = (ends[0] - ends[1]) / 2e-4
+        assert abs((grads[k] * u).sum() - want) <= 1e-5 * np.abs(grads[k] * u).sum() + 1e-5 * np.abs(host(w)).sum() * 1e-2
+
+
+# ---- log probabilities ---------------------------------------------------------------------------------------------
+def lp_check(x, labels, top, out):
+    logp, H, lse, tl, ti = out
+    xs, ys = host(x), labels.cpu().numpy()
+    w = po.log_probs(xs, ys, top)
+    V = xs.shape[1]
+    with np.errstate(invalid="ignore"):
+        biggest = np.where(np.isfinite(xs), xs, -np.inf).max(axis=1)
+        biggest = np.where(np.isfinite(biggest), np.abs(biggest), 0.0)
+        # e^(x-M) is off by (|x-M| + 4) U of itself, |x-M| e^(x-M) <= 0.37; s by (V/64 + 24) U; the log adds 2 U of its value
+        K = V / 64 + 24
+        tol = lambda v: U * (K + 4 * (np.log(V) + np.where(np.isfinite(v), np.abs(v), 0.0)))  # noqa: E731
+        assert_near(host(lse), w[2], tol(w[2]) + 2 * U * biggest, "lse")
+        assert_near(host(logp), w[0], tol(w[0]), "logp")
+        # w / s: the terms |x-M| e^(x-M) are added like s and have sum <= (log V + 1) s
+        assert_near(host(H), w[1], 3 * (K + 4) * (np.log(V) + 1) * U, "entropy")
+        if top:
+            assert np.array_equal(ti.cpu().numpy(), w[4]), "top_index"
+            assert_near(host(tl), w[3], tol(w[3]), "top_logp")
+
+
+def lp_rows(seed, N, V, dtype, ld=None, mask=None, scale=3.0):
+    ld = ld or V
+    x = randn(seed, N, ld) * scale
+    if mask is not None:
+        x[torch.rand(N, ld, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed + 1)) < 0.3] = mask
+    labels = torch.randint(0, V, (N,), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed + 2))
+    return x.to(dtype)[:, :V], labels
+
+
+LP_SHAPES = [(1, 1, 1), (1, 2, 1), (7, 10, 3), (64, 10, 10), (5, 17, 32), (256, 1000, 5), (3, 1023, 8), (9, 1025, 1), (4, 4097, 20), (1, 8192, 32),
+             (2, 32769, 7), (130, 2049, 5), (1, 131075, 20), (3, 262144, 32), (300, 64, 0), (1500, 33, 2)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,top", LP_SHAPES)
+def test_log_probs(dat, N, V, top, dtype):
+    for ld, mask in ((V, None), (V + 5, -float("inf")), ((V + 7) // 8 * 8, torch.finfo(dtype).min)):
+        x, labels = lp_rows(200 + V, N, V, dtype, ld, mask)
+        lp_check(x, labels, top, dat.log_probs(x, labels, top))
+
+
+@pytest.mark.parametrize("V", [10, 1000, 5000, 70001])
+@pytest.mark.parametrize("kind", ["equal", "ascending", "descending", "comb", "two", "zeros"])
+def test_log_probs_order_of_alternatives(dat, V, kind):
+    """Rows that are hard to select from: ties throughout, the largest last or first, all large values a fixed distance apart."""
+    i = torch.arange(V, device="cuda", dtype=torch.float32)
+    row = {"equal": torch.full((V,), 1.5, device="cuda"), "ascending": i / V, "descending": -i / V,
+           "comb": torch.where(i.long() % 1024 == 3, 5.0 + i / V, i / V - 9.0), "two": (i.long() % 2).float(),
+           "zeros": torch.where(i.long() % 3 == 0, -0.0, 0.0)}[kind]
+    x = torch.stack([row, row.flip(0)]).to(torch.bfloat16)
+    labels = torch.tensor([V - 1, 0], dtype=torch.int32, device="cuda")
+    for top in (1, 5, 32):
+        lp_check(x, labels, top, dat.log_probs(x, labels, top))
+        lp_check(x.float(), labels, top, dat.log_probs(x.float(), labels, top))
+
+
+@pytest.mark.parametrize("V", [3, 700, 9001, 70000])
+def test_log_probs_special_rows(dat, V):
+    inf, nan = float("inf"), float("nan")
+    x, labels = lp_rows(77, 10, V, torch.float32)
+    x[0] = -inf                                   # nothing allowed
+    x[1] = -inf
+    x[1, V // 2] = -3.0                           # one class allowed
+    x[2, V - 1] = nan
+    x[3, 0] = inf
+    x[4] = torch.finfo(torch.float32).min         # everything at the type's lowest value
+    x[5, : V - 1] = torch.finfo(torch.float32).min
+    x[6, labels[6]] = -inf                        # the given label is masked
+    x[7] = 3e38
+    x[8] = -1e-40                                 # values below the normal range
+    labels[1] = V // 2
+    labels[9] = V
+    lp_check(x, labels, min(V, 6), dat.log_probs(x, labels, min(V, 6)))
+    labels[9] = -1
+    out = dat.log_probs(x, labels, 2)
+    lp_check(x, labels, 2, out)
+    a, b = randn(5, 10), randn(6, 10)
+    dx = dat.log_probs_backward(x, labels, out[2], out[1], a, b)
+    want, size = po.log_probs_backward(host(x), labels.cpu().numpy(), host(out[2]), host(out[1]), host(a), host(b))
+    assert_near(host(dx), want, 16 * U * size + U * np.abs(want), "dlogits")
+    assert float(dx[0].abs().max()) == 0.0 and torch.isnan(dx[2]).all()
+
+
+def test_log_probs_without_labels_and_rows(dat):
+    x, labels = lp_rows(11, 6, 100, torch.float32)
+    logp, H, lse, tl, ti = dat.log_probs(x)
+    assert logp is None and tl is None and ti is None
+    full = dat.log_probs(x, labels, 4)
+    assert torch.equal(full[1], H) and torch.equal(full[2], lse)
+    empty = dat.log_probs(x[:0], labels[:0], 3)
+    assert [tuple(t.shape) for t in empty] == [(0,), (0,), (0,), (0, 3), (0, 3)]
+    assert dat.log_probs_backward(x[:0], labels[:0], lse[:0], None, lse[:0]).shape == (0, 100)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V", [(1, 1), (7, 10), (256, 1000), (3, 4099), (1, 131075), (65, 257)])
+def test_log_probs_backward(dat, N, V, dtype):
+    for ld, mask, use_a, use_b in ((V, None, True, True), (V + 3, -float("inf"), True, False), (V + 8, torch.finfo(dtype).min, False, True)):
+        x, labels = lp_rows(300 + V, N, V, dtype, ld, mask)
+        _, H, lse, _, _ = dat.log_probs(x, labels)
+        a, b = randn(1, N) if use_a else None, randn(2, N) if use_b else None
+        dx = dat.log_probs_backward(x, labels if use_a else None, lse, H if use_b else None, a, b)
+        zero = np.zeros(N)
+        want, size = po.log_probs_backward(host(x), labels.cpu().numpy() if use_a else np.full(N, -1), host(lse), host(H),
+                                           host(a) if use_a else zero, host(b) if use_b else zero)
+        tol = 16 * U * size + half(dtype) * np.abs(want) * 1.01 + (2.0 ** -133 if dtype == torch.bfloat16 else 2.0 ** -149)
+        assert_near(host(dx), want, tol, "dlogits")
+        buf = torch.full((N, ld), 7.0, dtype=dtype, device="cuda")      # rows apart: what lies between them stays
+        dat.log_probs_backward(x, labels, lse, H, a, b, dlogits=buf[:, :V])
+        assert torch.equal(buf[:, :V], dx) and (buf[:, V:] == 7.0).all()
+        own = x.clone(memory_format=torch.preserve_format) if ld == V else torch.empty(N, ld, dtype=dtype, device="cuda")[:, :V].copy_(x)
+        dat.log_probs_backward(own, labels, lse, H, a, b, dlogits=own)
+        assert torch.equal(own, dx)
+
+
+def test_log_probs_gradient_against_differences(dat):
+    x, labels = lp_rows(400, 3, 9, torch.float32, scale=1.5)
+    _, H, lse, _, _ = dat.log_probs(x, labels)
+    a, b = randn(1, 3), randn(2, 3)
+    dx = host(dat.log_probs_backward(x, labels, lse, H, a, b))
+    u = np.random.default_rng(3).standard_normal(dx.shape)
+    ends = []
+    for sign in (1, -1):
+        logp, ent, _, _, _ = po.log_probs(host(x) + sign * 1e-4 * u, labels.cpu().numpy(), 0)
+        ends.append((host(a) * logp + host(b) * ent).sum())
+    want = (ends[0] - ends[1]) / 2e-4
+    assert abs((dx * u).sum() - want) <= 1e-5 * np.abs(dx * u).sum() + 1e-6
+
+
+# ---- AdamW ---------------------------------------------------------------------------------------------------------
+TABLES = {"one": [1], "small": [3, 0, 1, 256, 257, 255, 0, 4, 513], "ragged": None, "long": [70001, 2, 1000, 33333], "many": [5] * 1500}
+
+
+def table(name):
+    n = TABLES[name] or [int(v) for v in np.exp(np.random.default_rng(3).uniform(0, 8, 60))]
+    return np.concatenate([[0], np.cumsum(n)]).astype(np.int64)
+
+
+def adamw_gradient(rng, offsets, step):
+    g = rng.standard_normal(offsets[-1]) * 10.0 ** rng.uniform(-4, 0, offsets[-1])
+    if step == 2 and len(offsets) > 3:
+        g[offsets[0]:offsets[2]] = 0.0
+    return g.astype(np.float32)
+
+
+@pytest.mark.parametrize("copy", [False, True])
+@pytest.mark.parametrize("grads", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("name", list(TABLES))
+def test_adamw(dat, name, bits, grads, copy):
+    """Five steps against the plain form stepping from its own state: the same bits of every code, moment and parameter (every
+    operation is rounded once on both sides)."""
+    off = table(name)
+    d, T = int(off[-1]), len(off) - 1
+    rng = np.random.default_rng(9)
+    theta = rng.standard_normal(d).astype(np.float32)
+    decay = (rng.random(T) < 0.5).astype(np.float32) * np.float32(0.05)
+    od, dd, th = torch.from_numpy(off).cuda(), torch.from_numpy(decay).cuda(), torch.from_numpy(theta).cuda()
+    m, v, scales = dat.adamw_state(d, T, bits)
+    half_copy = torch.zeros(d, dtype=torch.bfloat16, device="cuda") if copy else None
+    wd = np.repeat(decay, np.diff(off))
+    pm, pv = np.zeros(d, np.float32), np.zeros(d, np.float32)
+    cm, cv = np.zeros(d, np.uint8), np.zeros(d, np.uint8)
+    slots = dat.adamw_slots(d, T)
+    sm, sv = np.zeros(slots, np.int16), np.zeros(slots, np.int16)
+    slot, place = po.adamw_places(off)
+    for t in range(1, 6):
+        g = adamw_gradient(rng, off, t)
+        if grads == torch.bfloat16:
+            g = po.bf16_round(g)
+        seed = (t << 40) + 12345
+        dat.adamw_update(th, torch.from_numpy(g).cuda().to(grads), m, v, od, 0.01, t, scales=scales, seed=seed, beta2=0.99, decay=dd, theta_bf16=half_copy)
+        theta, pm, pv = po.adamw_step(theta, g, pm, pv, wd, 0.01, 0.9, 0.99, 1e-8, t)
+        if bits == 8:
+            word = po.philox(np.arange(slots * 64, dtype=np.uint64), seed, 2).reshape(-1)[slot * 256 + place]
+            cm, sm = po.adamw_encode(pm, word & 0xFFFF, off, slots, 127, sm)
+            cv, sv = po.adamw_encode(pv, word >> 16, off, slots, 255, sv)
+            pm, pv = po.adamw_decode(cm, sm, off, 127), po.adamw_decode(cv, sv, off, 255)
+            assert np.array_equal(m.cpu().numpy(), cm) and np.array_equal(v.cpu().numpy(), cv), t
+            assert np.array_equal(scales.cpu().numpy(), np.stack([sm, sv], 1)), t
+            got = dat.adamw_moments(m, v, scales, od)
+        else:
+            got = m, v
+        assert np.array_equal(got[0].cpu().numpy(), pm) and np.array_equal(got[1].cpu().numpy(), pv), t
+        assert np.array_equal(th.cpu().numpy(), theta), t
+        if copy:
+            assert np.array_equal(half_copy.float().cpu().numpy(), po.bf16_round(theta))
+
+
+def test_adamw_one_decay_for_all_and_unaligned_buffers(dat):
+    """Buffers that start at any element; what lies beside them stays."""
+    off = table("ragged")
+    d, T = int(off[-1]), len(off) - 1
+    rng = np.random.default_rng(4)
+    theta, g = rng.standard_normal(d).astype(np.float32), adamw_gradient(rng, off, 1)
+    for bits in (8, 32):
+        want = {}
+        for shift in (0, 1, 3):
+            def at(t):
+                buf = torch.full((d + 8,), 7, dtype=t.dtype, device="cuda")
+                buf[shift:shift + d] = t
+                return buf, buf[shift:shift + d]
+            m0, v0, scales = dat.adamw_state(d, T, bits)
+            bufs, (th, gr, m, v, cp) = zip(*[at(t) for t in (torch.from_numpy(theta).cuda(), torch.from_numpy(g).cuda(), m0, v0,
+                                                               torch.zeros(d, dtype=torch.bfloat16, device="cuda"))])
+            dat.adamw_update(th, gr, m, v, torch.from_numpy(off).cuda(), 0.02, 1, scales=scales, seed=3, weight_decay=0.1, theta_bf16=cp)
+            got = [t.cpu() for t in (th, m, v, cp)]
+            want = want or got
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            for buf in bufs:
+                assert (buf[:shift] == 7).all() and (buf[shift + d:] == 7).all()
+        ref, _, _ = po.adamw_step(theta, g, np.float32(0) * g, np.float32(0) * g, np.float32(0.1), 0.02, 0.9, 0.999, 1e-8, 1)
+        assert np.array_equal(want[0].numpy(), ref)
+
+
+def test_adamw_extreme_gradients(dat):
+    """Values below the normal range and near the largest; a NaN or an infinity stays in its block (8 bits) or element (32 bits)."""
+    off = np.array([0, 300, 1024, 1100], np.int64)
+    d, T = 1100, 3
+    g = np.random.default_rng(1).standard_normal(d).astype(np.float32)
+    g[0:40] *= np.float32(1e-38)
+    g[40:80] *= np.float32(1e-22)
+    g[256:300] *= np.float32(1e-40)
+    g[300:310] = np.float32(1e19)
+    g[600], g[1050] = np.nan, np.inf
+    slot, place = po.adamw_places(off)
+    slots = dat.adamw_slots(d, T)
+    for bits in (8, 32):
+        m, v, scales = dat.adamw_state(d, T, bits)
+        th = torch.ones(d, device="cuda")
+        for t in (1, 2):
+            dat.adamw_update(th, torch.from_numpy(g).cuda(), m, v, torch.from_numpy(off).cuda(), 0.01, t, scales=scales, seed=t)
+        bad = np.zeros(d, bool)
+        bad[[600, 1050]] = True
+        if bits == 8:
+            blocks = np.unique(slot[bad])
+            assert (scales.cpu().numpy()[blocks] == -1).all()
+            bad = np.isin(slot, blocks)
+            m, v = dat.adamw_moments(m, v, scales, torch.from_numpy(off).cuda())
+            assert np.array_equal(np.isnan(m.cpu().numpy()), bad) and np.array_equal(np.isnan(v.cpu().numpy()), bad)
+        assert np.array_equal(np.isnan(th.cpu().numpy()), bad)
+
+
+def test_adamw_rounding_is_unbiased(dat):
+    """The stored moments' mean over many elements of one value is that value: a step of the code is at most 1/8 of it, so the mean
+    of n independent roundings has a standard deviation of at most 1/16 / sqrt(n); six of them are allowed."""
+    n = 1 << 18
+    off = torch.tensor([0, n], device="cuda")
+    for value in (0.3, 1.7e-3):
+        m, v, scales = dat.adamw_state(n, 1, 8)
+        g = torch.full((n,), value, device="cuda")
+        g[::256] = 1.0                      # every block has a larger value
+        dat.adamw_update(torch.zeros(n, device="cuda"), g, m, v, off, 0.0, 1, scales=scales, seed=11)
+        fm, fv = dat.adamw_moments(m, v, scales, off)
+        keep = torch.ones(n, dtype=torch.bool, device="cuda")
+        keep[::256] = False
+        bound = 6 / 16 / (n - n // 256) ** 0.5
+        for f, x in ((fm, 0.1 * value), (fv, 1e-3 * value * value)):
+            mean = float(f[keep].double().mean()) / x
+            assert abs(mean - 1) <= bound + 2e-6, (value, mean)
+            assert len(torch.unique(f[keep])) == 2
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_model_adamw_update(dat, bits):
+    """A model's step is the call on its flat vector, with decay for conv and linear weights."""
+    import synth_inputs as syn
+    model = dat.Model(dat.ARCH_TESTNET, dat.BF16, 2, 16, 16, 5)
+    off = model.offsets
+    theta = syn.perturbed_params(8, off, model.fan_in, model.kind)
+    model.set_params(theta)
+    decay = torch.tensor([0.1 if k in (0, 4) else 0.0 for k in model.kind], device="cuda")
+    th, od = torch.from_numpy(theta).cuda(), torch.from_numpy(off).cuda()
+    m, v, scales = dat.adamw_state(model.d, model.num_tensors, bits)
+    for t in (1, 2, 3):
+        g = randn(t, model.d) * 0.01
+        model.adamw_update(g, 0.01, t, state_bits=bits, seed=t, weight_decay=0.1)
+        dat.adamw_update(th, g, m, v, od, 0.01, t, scales=scales, seed=t, decay=decay)
+        assert np.array_equal(model.get_params(), th.cpu().numpy()), t
+    with pytest.raises(dat.DatError) as e:
+        model.adamw_update(g, 0.01, 4, state_bits=40 - bits)
+    assert e.value.status == 6
+    # the compute copies follow: the same logits as a model that is given these parameters
+    other = dat.Model(dat.ARCH_TESTNET, dat.BF16, 2, 16, 16, 5)
+    other.set_params(model.get_params())
+    x, y = torch.rand(2, 16, 16, 3, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert torch.equal(model.input_grad(x, y)[1], other.input_grad(x, y)[1])
+    model.close()
+    other.close()
+
+
+# ---- streams, graphs, together -------------------------------------------------------------------------------------
+class Net:
+    """conv 3x3 -> group norm + ReLU -> conv 3x3 stride 2 -> group norm + SiLU -> mean over pixels -> linear -> log probabilities ->
+    gradients -> AdamW, all from the library's calls (torch for the pooling and the linear layer).  deep=False: the second convolution
+    is a pointwise product by torch (dat_conv_backward_data waits for the device: it cannot be captured)."""
+
+    def __init__(self, dat, bits, seed=0, classes=11, deep=True):
+        self.dat, self.bits, self.classes, self.deep = dat, bits, classes, deep
+        sizes = [16 * 9 * 8, 16, 16, 32 * 9 * 16, 32, 32, classes * 32]
+        self.off = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int64)
+        d = int(self.off[-1])
+        self.theta = 0.1 * randn(seed, d)
+        for i in (1, 4):
+            self.theta[self.off[i]:self.off[i + 1]] = 1.0
+        self.copy = self.theta.to(torch.bfloat16)
+        self.grad = torch.zeros(d, device="cuda")
+        self.m, self.v, self.scales = dat.adamw_state(d, len(sizes), bits)
+        self.offsets = torch.from_numpy(self.off).cuda()
+        self.decay = torch.tensor([0.01, 0, 0, 0.01, 0, 0, 0.01], device="cuda")
+
+    def part(self, flat, i, *shape):
+        return flat[self.off[i]:self.off[i + 1]].view(*shape)
+
+    def step(self, x, y, t):
+        dat, p = self.dat, self.part
+        w1, w2 = p(self.copy, 0, 16, 3, 3, 8), p(self.copy, 3, 32, 3, 3, 16)
+        g1, b1, g2, b2, wl = p(self.theta, 1, 16), p(self.theta, 2, 16), p(self.theta, 4, 32), p(self.theta, 5, 32), p(self.theta, 6, self.classes, 32)
+        a1 = dat.conv_forward(x, w1, 1, 1)
+        y1, m1, r1 = dat.group_norm_forward(a1, g1, b1, 4, dat.ACT_RELU)
+        if self.deep:
+            a2 = dat.conv_forward(y1, w2, 2, 1)
+        else:
+            wp, rows = w2[:, 1, 1, :].float().contiguous(), y1.float().view(-1, 16)
+            a2 = (rows @ wp.t()).to(torch.bfloat16).view(*y1.shape[:3], 32)
+        y2, m2, r2 = dat.group_norm_forward(a2, g2, b2, 8, dat.ACT_SILU)
+        f = y2.float().mean(dim=(1, 2))
+        logits = f @ wl.t()
+        logp, H, lse, _, top = dat.log_probs(logits, y, 3)
+        B = x.shape[0]
+        dz = dat.log_probs_backward(logits, y, lse, H, torch.full_like(logp, -1.0 / B), torch.full_like(logp, -0.1 / B))
+        p(self.grad, 6, self.classes, 32).copy_(dz.t() @ f)
+        n = y2.shape[1] * y2.shape[2]
+        dy2 = ((dz @ wl) / n)[:, None, None, :].expand_as(y2).to(torch.bfloat16).contiguous()
+        da2, _, _ = dat.group_norm_backward(a2, dy2, g2, b2, m2, r2, 8, dat.ACT_SILU, dgamma=p(self.grad, 4, 32), dbeta=p(self.grad, 5, 32))
+        if self.deep:
+            dat.conv_backward_weight(y1, da2, 3, 2, 1, dw=p(self.grad, 3, 32, 3, 3, 16), static=True)
+            dy1 = dat.conv_backward_data(da2, w2, (x.shape[1], x.shape[2]), 2, 1)
+        else:
+            d2 = da2.float().view(-1, 32)
+            p(self.grad, 3, 32, 3, 3, 16)[:, 1, 1, :] = d2.t() @ rows
+            dy1 = (d2 @ wp).to(torch.bfloat16).view_as(y1)
+        da1, _, _ = dat.group_norm_backward(a1, dy1, g1, b1, m1, r1, 4, dat.ACT_RELU, dgamma=p(self.grad, 1, 16), dbeta=p(self.grad, 2, 16))
+        dat.conv_backward_weight(x, da1, 3, 1, 1, dw=p(self.grad, 0, 16, 3, 3, 8), static=True)
+        dat.adamw_update(self.theta, self.grad, self.m, self.v, self.offsets, 1e-2, t, scales=self.scales, seed=t, decay=self.decay, theta_bf16=self.copy)
+        return logits, logp, top
+
+    def loss64(self, theta, x, y):
+        """The same objective in float64 torch (CPU), from unrounded parameters."""
+        p = self.part
+        F = torch.nn.functional
+        z = F.conv2d(x.permute(0, 3, 1, 2), p(theta, 0, 16, 3, 3, 8).permute(0, 3, 1, 2), padding=1)
+        z = F.relu(F.group_norm(z, 4, p(theta, 1, 16), p(theta, 2, 16)))
+        z = F.conv2d(z, p(theta, 3, 32, 3, 3, 16).permute(0, 3, 1, 2), stride=2, padding=1)
+        z = F.silu(F.group_norm(z, 8, p(theta, 4, 32), p(theta, 5, 32)))
+        q = F.log_softmax(z.mean(dim=(2, 3)) @ p(theta, 6, self.classes, 32).t(), dim=1)
+        H = -(q.exp() * q).sum(1)
+        return (-q[torch.arange(len(y)), y.long()] - 0.1 * H).mean()
+
+
+def net_batch(seed, B=6):
+    return randn(seed, B, 9, 9, 8).to(torch.bfloat16), torch.randint(0, 11, (B,), dtype=torch.int32, device="cuda",
+                                                                     generator=torch.Generator(device="cuda").manual_seed(seed))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_network_of_these_calls(dat, bits):
+    """The gradients of a whole step, tensor by tensor, against autograd in 64 bits.  Weights, activations and activation gradients are
+    bf16: a chain of six roundings of 2^-8 forward and backward each, and ReLU masks that they move (under 1 % of the values)
+    leave a relative error of at most 12 * 2^-8 = 0.047, doubled for the masks, in the 2-norm."""
+    net = Net(dat, bits)
+    for t in (1, 2, 3):
+        x, y = net_batch(t)
+        before = net.copy.float() * 1.0
+        for i in (1, 2, 4, 5, 6):
+            net.part(before, i, -1).copy_(net.part(net.theta, i, -1))
+        net.step(x, y, t)
+        th = before.double().cpu().requires_grad_(True)
+        (want,) = torch.autograd.grad(net.loss64(th, x.double().cpu(), y.cpu()), th)
+        for i in range(7):
+            a, b = host(net.part(net.grad, i, -1)), net.part(want, i, -1).numpy()
+            assert np.linalg.norm(a - b) <= 0.1 * np.linalg.norm(b), (t, i, np.linalg.norm(a - b) / np.linalg.norm(b))
+    assert torch.equal(net.copy, net.theta.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_captured_step_replays(dat, bits):
+    """The whole step captured: every replay, with other work and other inputs between, gives what eager steps give."""
+    eager, graphed = Net(dat, bits, deep=False), Net(dat, bits, deep=False)
+    x, y = net_batch(1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graphed.step(x, y, 1)                      # the libraries' own first calls
+    torch.cuda.current_stream().wait_stream(side)
+    eager.step(x, y, 1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = graphed.step(x, y, 2)                # t and the seed are part of the captured launches
+    for i in range(4):
+        nx, ny = net_batch(10 + i)
+        x.copy_(nx)
+        y.copy_(ny)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = eager.step(nx, ny, 2)
+        for a, b in zip(out, want):
+            assert torch.equal(a, b), i
+        assert torch.equal(graphed.theta, eager.theta) and torch.equal(graphed.m, eager.m) and torch.equal(graphed.v, eager.v), i
+        dat.group_norm_forward(randn(i, 2, 20, 20, 64), None, None, 8)         # eager work between the replays
+        torch.cuda.synchronize()
+
+
+def test_two_captured_graphs_and_another_stream(dat):
+    """Two graphs of calls that use workspaces, replayed at once on two streams, and eager calls on a third: nothing is shared."""
+    cases = []
+    for k in range(2):
+        x, gamma, beta, dy = gn_inputs((4, 40, 40, 64, 16), torch.bfloat16, 70 + 10 * k)
+        z, labels = lp_rows(80 + k, 2, 100003, torch.bfloat16)
+
+        def work(x=x, gamma=gamma, beta=beta, dy=dy, z=z, labels=labels):
+            y, mean, rstd = dat.group_norm_forward(x, gamma, beta, 16, 1)
+            return (y, mean, rstd) + dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, 16, 1) + dat.log_probs(z, labels, 9)
+
+        want = work()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = work()
+        cases.append((work, want, graph, out))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(3):
+        for _, _, _, out in cases:
+            for t in out:
+                t.zero_()
+        torch.cuda.synchronize()
+        for (_, _, graph, _), s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        with torch.cuda.stream(streams[2]):
+            eager = cases[0][0]()
+        torch.cuda.synchronize()
+        for _, want, _, out in cases:
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert all(torch.equal(a, b) for a, b in zip(eager, cases[0][1]))
+
+
+def test_stream_argument(dat):
+    s = torch.cuda.Stream()
+    x, gamma, beta, dy = gn_inputs((8, 32, 32, 64, 16), torch.bfloat16, 90)
+    z, labels = lp_rows(91, 5, 3001, torch.float32)
+    want = dat.group_norm_forward(x, gamma, beta, 16, 1), dat.log_probs(z, labels, 4)
+    torch.cuda.synchronize()
+    got = dat.group_norm_forward(x, gamma, beta, 16, 1, stream=s), dat.log_probs(z, labels, 4, stream=s)
+    s.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
