@@ -8,8 +8,9 @@
 // Two ways, both bound by HBM:
 //   resident  one workgroup holds a slice of whole groups of one image in registers: every tensor is moved once.
 //   split     an image's slice is too large for that: partial sums over ranges of pixels, a small kernel that joins them, and a
-//             second pass over the tensors.  Images go in batches whose tensors fit into the last-level cache, where the second
-//             pass finds them.
+//             second pass over the tensors, from the last image to the first: the last-level cache still holds what the first
+//             pass read last.
+#include <type_traits>
 #include "kernels.h"
 
 namespace dat {
@@ -22,46 +23,108 @@ struct GnArgs {
   int nv;            // vectors of a pixel's channels
   int sv, slices;    // vectors of a slice, slices of a pixel
   int chunk, chunks; // split: pixels of a range, ranges of an image
-  int b0;            // split: first image of the batch
   float eps;
 };
 
-template <typename T, int VE> struct Vec;
-template <> struct Vec<float, 4> { typedef float4 type; };
-template <> struct Vec<bf16_t, 8> { typedef uint4 type; };
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <typename T, int VE> struct Vec;          // VE channels as they lie in memory
+template <> struct Vec<float, 4> { typedef u32x4 type; };
+template <> struct Vec<bf16_t, 8> { typedef u32x4 type; };
 template <> struct Vec<float, 1> { typedef float type; };
 template <> struct Vec<bf16_t, 1> { typedef bf16_t type; };
 
-__device__ __forceinline__ void unpack(const float4& v, float (&f)[4]) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
-__device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+template <typename T, int VE> __device__ __forceinline__ void unpack(const typename Vec<T, VE>::type& v, float (&f)[VE]) {
+  if constexpr (VE == 1 && sizeof(T) == 4) f[0] = v;
+  else if constexpr (VE == 1) f[0] = bf2f(v);
+  else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    for (int j = 0; j < VE; ++j) f[j] = __uint_as_float(v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < VE; j += 2) { f[j] = __uint_as_float(v[j / 2] << 16); f[j + 1] = __uint_as_float(v[j / 2] & 0xffff0000u); }
+  }
 }
-__device__ __forceinline__ void unpack(const float& v, float (&f)[1]) { f[0] = v; }
-__device__ __forceinline__ void unpack(const bf16_t& v, float (&f)[1]) { f[0] = bf2f(v); }
-__device__ __forceinline__ void pack(const float (&f)[4], float4* v) { *v = make_float4(f[0], f[1], f[2], f[3]); }
-__device__ __forceinline__ void pack(const float (&f)[8], uint4* v) {
-  *v = make_uint4(f2bf_pack(f[0], f[1]), f2bf_pack(f[2], f[3]), f2bf_pack(f[4], f[5]), f2bf_pack(f[6], f[7]));
+template <typename T, int VE> __device__ __forceinline__ typename Vec<T, VE>::type pack(const float (&f)[VE]) {
+  typename Vec<T, VE>::type v;
+  if constexpr (VE == 1 && sizeof(T) == 4) v = f[0];
+  else if constexpr (VE == 1) v = f2bf(f[0]);
+  else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) v[j] = __float_as_uint(f[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < VE; j += 2) v[j / 2] = f2bf_pack(f[j], f[j + 1]);
+  }
+  return v;
 }
-__device__ __forceinline__ void pack(const float (&f)[1], float* v) { *v = f[0]; }
-__device__ __forceinline__ void pack(const float (&f)[1], bf16_t* v) { *v = f2bf(f[0]); }
+// Channels h .. h+3 of a 16-byte vector.
+template <typename T> __device__ __forceinline__ void unpack4(const u32x4& v, int h, float (&f)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(T) == 4) f[j] = __uint_as_float(v[j]);
+    else f[j] = __uint_as_float(j % 2 ? v[(h + j) / 2] & 0xffff0000u : v[(h + j) / 2] << 16);
+  }
+}
+template <typename T> __device__ __forceinline__ void pack4(const float (&f)[4], int h, u32x4& v) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(T) == 4) v[j] = __float_as_uint(f[j]);
+    else if (j % 2) v[(h + j) / 2] = f2bf_pack(f[j - 1], f[j]);
+  }
+}
+// Held vectors are unpacked anew in every pass: without this the compiler unpacks them where they are loaded, or keeps the
+// unpacked values of one pass for the next, twice the registers, and spills.
+__device__ __forceinline__ void forget(u32x4& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void forget(float& v) { asm volatile("" : "+v"(v)); }
 
-__device__ __forceinline__ float gn_xhat(float x, float mean, float rstd) { return __fmul_rn(__fsub_rn(x, mean), rstd); }
-__device__ __forceinline__ float gn_z(float xhat, float gamma, float beta) { return __fadd_rn(__fmul_rn(xhat, gamma), beta); }
-// 1 / (1 + e^-z).  The results that leave in bf16 take the hardware's exponential and reciprocal, a few units of 2^-23 off.
+// acc + a.lo b.lo + a.hi b.hi of two pairs of bf16
+__device__ __forceinline__ float dot_pairs(uint32_t a, uint32_t b, float acc) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, a), __builtin_bit_cast(bf16x2_t, b), acc, false);
+}
+
+// Buffer descriptors: a lane beyond the range reads zeros and writes nothing, so no load or store stands behind a branch, where
+// it would be waited for together with everything else in flight.  All of the offset is in the vector register: with a scalar
+// register for the part that all lanes share, the compiler takes the registers of a store's data as free at once, and on gfx950
+// what it computed into them next came out in memory (single lanes, now and then).  The wait states after a store keep its data
+// where it is until it has been read; the empty statements of forget() would be counted as some.
+typedef __amdgpu_buffer_rsrc_t BufRsrc;
+constexpr uint32_t kOob = 0xfffffff0u;
+__device__ __forceinline__ void buffer_load(BufRsrc r, uint32_t off, u32x4& v) { v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0); }
+__device__ __forceinline__ void buffer_store(BufRsrc r, uint32_t off, const u32x4& v) { __builtin_amdgcn_raw_buffer_store_b128(v, r, (int)off, 0, 0); }
+__device__ __forceinline__ void after_store() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 3");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// z = xhat gamma + beta of the ReLU's derivative: one rounding per operation, as dat.h says.
+__device__ __forceinline__ float gn_z(float xm, float rstd, float gamma, float beta) {
+  return __fadd_rn(__fmul_rn(__fmul_rn(xm, rstd), gamma), beta);
+}
+// 1 / (1 + e^-z) from the hardware's exponential and reciprocal (1 unit of 2^-23 each).  fp32 outputs: the rounding error of the
+// exponent z log2(e) goes back in, or it would grow with |z|.
 template <typename T> __device__ __forceinline__ float sigmoid(float z) {
-  if (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-  return 1.0f / (1.0f + expf(-z));
+  constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f, kLn2 = 0.69314718055994530942f;
+  if (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z));
+  const float y = -__builtin_amdgcn_fmed3f(z, -126.0f, 126.0f), t = y * kLog2e;
+  const float low = fmaf(y, kLog2eLow, fmaf(y, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
+  return __builtin_amdgcn_rcpf(1.0f + fmaf(e * kLn2, low, e));
 }
 template <typename T, int ACT> __device__ __forceinline__ float act_of(float z) {
-  if (ACT == DAT_ACT_RELU) return z <= 0.0f ? 0.0f : z;      // NaN stays
+  if (ACT == DAT_ACT_RELU) return __builtin_elementwise_maximum(z, 0.0f);      // NaN stays
   if (ACT == DAT_ACT_SILU) return z * sigmoid<T>(z);
   return z;
 }
-template <typename T, int ACT> __device__ __forceinline__ float act_grad(float z, float dy) {
-  if (ACT == DAT_ACT_RELU) return z > 0.0f ? dy : 0.0f;
-  if (ACT == DAT_ACT_SILU) { const float s = sigmoid<T>(z); return dy * (s * (1.0f + z * (1.0f - s))); }
+template <typename T> __device__ __forceinline__ float silu_dz(float z, float dy) {
+  const float s = sigmoid<T>(z);
+  return dy * fmaf(z * s, 1.0f - s, s);
+}
+// dz of one channel.  xm = x - mean, scale = rstd gamma.
+template <typename T, int ACT>
+__device__ __forceinline__ float gn_dz(float xm, float dy, float rstd, float gamma, float scale, float beta) {
+  if (ACT == DAT_ACT_RELU) return gn_z(xm, rstd, gamma, beta) > 0.0f ? dy : 0.0f;
+  if (ACT == DAT_ACT_SILU) return silu_dz<T>(fmaf(xm, scale, beta), dy);
   return dy;
 }
 __device__ __forceinline__ float rstd_of(float sum, float n, float eps) { return __fdiv_rn(1.0f, sqrtf(__fdiv_rn(sum, n) + eps)); }
@@ -75,209 +138,340 @@ template <int VE> struct Affine {
   }
 };
 
+// Groups of a thread's vector of VE channels, GV of them: 1 (the vector lies in one), VE/Cg where Cg divides VE, else VE (one
+// for each channel).  of(j): which of the GV entries channel j uses; first(c, Cg, g): the group of each entry.
+template <int VE, int GV> struct Groups {
+  static constexpr int of(int j) { return j * GV / VE; }
+  static __device__ __forceinline__ void find(int c, int Cg, int (&g)[GV]) {
+    if (GV < VE || GV == 1) {
+      const int g0 = GV == 1 ? c / Cg : c / (VE / GV);
+#pragma unroll
+      for (int k = 0; k < GV; ++k) g[k] = g0 + k;
+      return;
+    }
+    int g0 = c / Cg, r = c - g0 * Cg;
+#pragma unroll
+    for (int k = 0; k < GV; ++k) { g[k] = g0; if (++r == Cg) { r = 0; ++g0; } }
+  }
+  // columns of one group where a vector has GV columns
+  static __device__ __forceinline__ int columns(int Cg) { return GV == 1 ? Cg / VE : GV < VE ? 1 : Cg; }
+};
+
 // ---- resident ----------------------------------------------------------------------------------------------------------
+// Tile: slice of an image.  Neighbouring slices share cache lines: they go to workgroups of one XCD (workgroups are dealt to the
+// eight XCDs in turn).
+constexpr int kXcds = 8;
+__device__ __forceinline__ int tiles_per_xcd(int tiles) { return (tiles + kXcds - 1) / kXcds; }
+
 // Thread tid = ty*sv + tx holds vector tx of the slice at pixels ty, ty + rows, ...: at most VPT of them.
-template <typename T, int NT, int VPT> struct Tile {
-  static constexpr int VE = 16 / sizeof(T);
+template <typename T, int VE, int NT> struct Tile {
   typedef typename Vec<T, VE>::type V;
-  int sv, rows, tx, ty, count, c;            // width of this slice, threads along the pixels, own pixels, first channel
-  int64_t at, step;                          // first vector, distance to the next one (vectors)
-  __device__ __forceinline__ Tile(const GnArgs& a, int b, int slice) {
+  bool valid;
+  int b, sv, rows, tx, ty, c_slice, c;     // image, width, threads along the pixels, first channels of the slice and the thread
+  int full;                                // rounds in which every thread has a pixel
+  int64_t base;                            // bytes: first pixel of the slice
+  uint32_t size, step;                     // bytes: from there to the image's end (0: no tile); distance of a thread's pixels
+  uint32_t off, off_last;                  // bytes: the thread's first pixel, for the full rounds and for the one after them
+  __device__ __forceinline__ Tile(const GnArgs& a, int index, int tiles) {
+    const int per = tiles_per_xcd(tiles), i = index / kXcds, tile = (index - i * kXcds) * per + i;
+    valid = i < per && tile < tiles;
+    b = valid ? tile / a.slices : 0;
+    const int slice = valid ? tile - b * a.slices : 0;
     sv = min(a.sv, a.nv - slice * a.sv);
     rows = NT / sv;
     ty = threadIdx.x / sv; tx = threadIdx.x - ty * sv;
-    count = ty < rows && ty < a.P ? (a.P - ty + rows - 1) / rows : 0;
-    const int v = slice * a.sv + tx;
+    full = a.P / rows;
+    const int v = slice * a.sv + tx, left = a.P - full * rows;
+    c_slice = slice * a.sv * VE;
     c = v * VE;
-    at = ((int64_t)b * a.P + min(ty, a.P - 1)) * a.nv + v;
-    step = (int64_t)rows * a.nv;
+    constexpr uint32_t kBytes = sizeof(V);
+    base = ((int64_t)b * a.P * a.nv + slice * a.sv) * kBytes;
+    size = valid ? ((uint32_t)a.P * (uint32_t)a.nv - (uint32_t)(slice * a.sv)) * kBytes : 0u;
+    step = (uint32_t)rows * (uint32_t)a.nv * kBytes;
+    const uint32_t own = ((uint32_t)ty * (uint32_t)a.nv + (uint32_t)tx) * kBytes;
+    off = ty < rows ? own : kOob;
+    off_last = ty < left ? own : kOob;
   }
-  // Pixels past the end: the last own one again (the first, for a thread without any), not used.
-  __device__ __forceinline__ void load(const void* p, V (&v)[VPT]) const {
-    const V* src = reinterpret_cast<const V*>(p) + at;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) v[i] = src[min(i, max(count - 1, 0)) * step];
+  __device__ __forceinline__ BufRsrc buffer(const void* p) const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(reinterpret_cast<const char*>(p)) + base, 0, (int)size, 0x00020000);
   }
+  // (one select a round instead of a register for each of them from the loads to the stores)
+  __device__ __forceinline__ void forget_rounds() { asm volatile("" : "+v"(off), "+v"(off_last)); }
+  __device__ __forceinline__ bool own(int i) const { return (i < full ? off : i == full ? off_last : kOob) != kOob; }
+  __device__ __forceinline__ uint32_t round(int i) const {     // (kOob stays beyond every range: the sum saturates)
+    return __builtin_elementwise_add_sat(i < full ? off : i == full ? off_last : kOob, (uint32_t)i * step);
+  }
+  __device__ __forceinline__ void load(BufRsrc r, int i, V& v) const { buffer_load(r, round(i), v); }
+  __device__ __forceinline__ void store(BufRsrc r, int i, const V& v) const { buffer_store(r, round(i), v); after_store(); }
 };
 
-// Joins what the threads of a slice hold for SUB columns each, columns of a group being ncol neighbours: the groups' sums in
-// s_out.  Lanes of a group take rows (or columns, where there are more of these) in turn.
-template <int NT, int SUB>
-__device__ __forceinline__ void group_sums(const float (&v)[SUB], int sv, int rows, int ncol, int ng, float* s_red, float* s_out) {
-  __syncthreads();                 // s_red and s_out of the round before have been read
+// Threads hold M sets of N columns each, thread ty*sv + tx those of vector tx; brings the sums over ty to s_red[set][row][sv*N],
+// NT*N floats a set, with as few rows as the return value says.  Lanes of a wavefront that share a vector are joined in registers.
+template <int NT, int M, int N>
+__device__ __forceinline__ int lay_columns(float (&v)[M][N], int sv, int rows, float* s_red) {
+  __syncthreads();                 // what was in s_red has been read
+  int at = threadIdx.x;
+  bool lay = true;
+  if (sv < 64 && (sv & (sv - 1)) == 0) {
+    for (int d = 32; d >= sv; d >>= 1) {
 #pragma unroll
-  for (int j = 0; j < SUB; ++j) s_red[threadIdx.x * SUB + j] = v[j];
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[m][j] += __shfl_xor(v[m][j], d);
+    }
+    const int lane = threadIdx.x & 63;
+    lay = lane < sv;
+    at = (threadIdx.x >> 6) * sv + lane;
+    rows = NT / 64;
+  }
+  if (lay) {
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int j = 0; j < N; ++j) s_red[(m * NT + at) * N + j] = v[m][j];
+  }
   __syncthreads();
+  return rows;
+}
+// Sums of ng groups of ncol neighbouring columns over the rows of width w, of M sets `set` floats apart; done(g, sums) by one
+// thread of each.
+template <int NT, int M, typename F>
+__device__ __forceinline__ void sum_columns(const float* s_red, int set, int w, int rows, int ncol, int ng, F done) {
   int lanes = 64;
   while (lanes > 1 && lanes * ng > NT) lanes >>= 1;
-  const int k = threadIdx.x & (lanes - 1), w = sv * SUB;
+  while (lanes > 1 && lanes >= 2 * rows * ncol) lanes >>= 1;
+  const int k = threadIdx.x & (lanes - 1);
   for (int g0 = 0; g0 < ng; g0 += NT / lanes) {
     const int g = g0 + threadIdx.x / lanes;
-    float sum = 0.0f;
-    if (g < ng) {
-      const float* col = s_red + g * ncol;
-      if (ncol >= lanes) { for (int c = k; c < ncol; c += lanes) for (int r = 0; r < rows; ++r) sum += col[r * w + c]; }
-      else { for (int r = k; r < rows; r += lanes) for (int c = 0; c < ncol; ++c) sum += col[r * w + c]; }
+    float sum[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      sum[m] = 0.0f;
+      if (g < ng) {
+        const float* col = s_red + m * set + g * ncol;
+        if (ncol >= lanes) { for (int c = k; c < ncol; c += lanes) for (int r = 0; r < rows; ++r) sum[m] += col[r * w + c]; }
+        else { for (int r = k; r < rows; r += lanes) for (int c = 0; c < ncol; ++c) sum[m] += col[r * w + c]; }
+      }
+      for (int d = lanes >> 1; d >= 1; d >>= 1) sum[m] += __shfl_xor(sum[m], d);
     }
-    for (int d = lanes >> 1; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-    if (g < ng && k == 0) s_out[g] = sum;
+    if (g < ng && k == 0) done(g, sum);
   }
-  __syncthreads();
 }
 
-constexpr int kMaxSliceGroups = 512;
+constexpr int kMaxSliceGroups = 512, kMaxSlice = 256;     // of a slice: groups, vectors
 
-// SUB = 1: a vector lies inside one group; SUB = VE: columns are single channels.
-template <typename T, int ACT, bool WHOLE, int NT, int VPT>
+// bf16 with two channels or more to a group: sums and sums of squares in one pass by dot products of pairs, exact products added
+// in fp32, and var = E x^2 - mean^2 where mean^2 <= 4 var, which costs at most a factor five of the sums' rounding errors; a slice
+// with a group whose mean is farther out takes the deviations from the mean, as all others do (fp32 has half the arithmetic for
+// its bytes).
+template <typename T, int ACT, int GV, int NT, int VPT>
 __global__ __launch_bounds__(NT) void gn_forward_resident_kernel(GnArgs a) {
-  typedef Tile<T, NT, VPT> Tl;
-  constexpr int VE = Tl::VE, SUB = WHOLE ? 1 : VE;
-  __shared__ float s_red[NT * SUB], s_mean[kMaxSliceGroups], s_rstd[kMaxSliceGroups];
-  const int b = blockIdx.x / a.slices, slice = blockIdx.x - b * a.slices;
-  const Tl t(a, b, slice);
+  constexpr int VE = 16 / sizeof(T);
+  constexpr bool kPairs = sizeof(T) == 2 && GV < VE;
+  typedef Tile<T, VE, NT> Tl;
+  typedef Groups<VE, GV> Gr;
+  __shared__ float s_red[NT * GV * (kPairs ? 2 : 1)], s_mean[kMaxSliceGroups], s_rstd[kMaxSliceGroups];
+  Tl t(a, blockIdx.x, a.B * a.slices);
+  if (!t.valid) return;            // (the number of tiles is rounded up to the XCDs)
   typename Tl::V v[VPT];
-  t.load(a.x, v);
-  const int ng = t.sv * VE / a.Cg, g_first = slice * a.sv * VE / a.Cg, ncol = WHOLE ? a.Cg / VE : a.Cg;
+  {
+    const BufRsrc x = t.buffer(a.x);
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) t.load(x, i, v[i]);
+  }
   const float n = (float)a.P * (float)a.Cg;
-  float acc[SUB], f[VE];
+  const int ncol = Gr::columns(a.Cg);
+  const int ng = t.sv * VE / a.Cg, g_first = t.c_slice / a.Cg, w = t.sv * GV;
+  float* out_mean = a.mean + (int64_t)t.b * a.G + g_first;
+  float* out_rstd = a.rstd + (int64_t)t.b * a.G + g_first;
+  int g[GV];
+  Gr::find(t.c - t.c_slice, a.Cg, g);
+  float mean[GV], f[VE];
+  bool far = false;
+  if constexpr (kPairs) {
+    float acc[2][GV];
 #pragma unroll
-  for (int j = 0; j < SUB; ++j) acc[j] = 0.0f;
+    for (int k = 0; k < GV; ++k) acc[0][k] = acc[1][k] = 0.0f;
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
-    if (i < t.count) {
-      unpack(v[i], f);
-      if (WHOLE) {
-        float s = 0.0f;
+    for (int i = 0; i < VPT; ++i) {            // (past the end: zeros)
+      forget(v[i]);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) s += f[j];
-        acc[0] += s;
-      } else {
-#pragma unroll
-        for (int j = 0; j < SUB; ++j) acc[j] += f[j];
+      for (int j = 0; j < VE; j += 2) {
+        const int k = Gr::of(j);
+        acc[0][k] = dot_pairs(v[i][j / 2], 0x3f803f80u, acc[0][k]);
+        acc[1][k] = dot_pairs(v[i][j / 2], v[i][j / 2], acc[1][k]);
       }
     }
-  group_sums<NT, SUB>(acc, t.sv, t.rows, ncol, ng, s_red, s_mean);
-  float mean[SUB], rstd[SUB];
-  const int c0 = t.tx * VE;
+    const int rows = lay_columns<NT, 2, GV>(acc, t.sv, t.rows, s_red);
+    sum_columns<NT, 2>(s_red, NT * GV, w, rows, ncol, ng, [&](int k, const float (&sum)[2]) {
+      const float mu = __fdiv_rn(sum[0], n), var = fmaf(-mu, mu, __fdiv_rn(sum[1], n)), r = __fdiv_rn(1.0f, sqrtf(fmaxf(var, 0.0f) + a.eps));
+      if (mu * mu > 4.0f * var) far = true;
+      // (a NaN or an infinity in the group: var is NaN, and so is rstd)
+      s_mean[k] = mu; s_rstd[k] = var == var ? r : var;
+      out_mean[k] = mu; out_rstd[k] = var == var ? r : var;
+    });
+    far = __syncthreads_or(far);
+  } else {
+    float acc[1][GV];
 #pragma unroll
-  for (int j = 0; j < SUB; ++j) { mean[j] = t.count ? __fdiv_rn(s_mean[(c0 + j) / a.Cg], n) : 0.0f; acc[j] = 0.0f; }
+    for (int k = 0; k < GV; ++k) acc[0][k] = 0.0f;
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
-    if (i < t.count) {
-      unpack(v[i], f);
-      float s = 0.0f;
+    for (int i = 0; i < VPT; ++i) {            // (past the end: zeros)
+      forget(v[i]);
+      unpack<T, VE>(v[i], f);
+      float s[GV];
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float d = f[j] - mean[WHOLE ? 0 : j];
-        if (WHOLE) s = fmaf(d, d, s); else acc[j] = fmaf(d, d, acc[j]);
-      }
-      if (WHOLE) acc[0] += s;
+      for (int k = 0; k < GV; ++k) s[k] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < VE; ++j) s[Gr::of(j)] += f[j];
+#pragma unroll
+      for (int k = 0; k < GV; ++k) acc[0][k] += s[k];
     }
-  group_sums<NT, SUB>(acc, t.sv, t.rows, ncol, ng, s_red, s_rstd);
-  for (int g = threadIdx.x; g < ng; g += NT) {
-    a.mean[(int64_t)b * a.G + g_first + g] = __fdiv_rn(s_mean[g], n);
-    a.rstd[(int64_t)b * a.G + g_first + g] = rstd_of(s_rstd[g], n, a.eps);
+    const int rows = lay_columns<NT, 1, GV>(acc, t.sv, t.rows, s_red);
+    sum_columns<NT, 1>(s_red, 0, w, rows, ncol, ng, [&](int k, const float (&sum)[1]) { s_mean[k] = __fdiv_rn(sum[0], n); });
+    __syncthreads();
   }
-  if (t.count == 0) return;
 #pragma unroll
-  for (int j = 0; j < SUB; ++j) rstd[j] = rstd_of(s_rstd[(c0 + j) / a.Cg], n, a.eps);
-  const Affine<VE> w(a, t.c);
-  typename Tl::V* y = reinterpret_cast<typename Tl::V*>(a.out) + t.at;
+  for (int k = 0; k < GV; ++k) mean[k] = s_mean[g[k]];
+  if (!kPairs || far) {
+    float acc[1][GV];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
-    if (i < t.count) {
-      unpack(v[i], f);
+    for (int k = 0; k < GV; ++k) acc[0][k] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < VE; ++j) f[j] = act_of<T, ACT>(gn_z(gn_xhat(f[j], mean[WHOLE ? 0 : j], rstd[WHOLE ? 0 : j]), w.gamma[j], w.beta[j]));
-      pack(f, y + i * t.step);
+    for (int i = 0; i < VPT; ++i) {
+      forget(v[i]);
+      unpack<T, VE>(v[i], f);
+      float s[GV];
+#pragma unroll
+      for (int k = 0; k < GV; ++k) s[k] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < VE; ++j) { const float d = f[j] - mean[Gr::of(j)]; s[Gr::of(j)] = fmaf(d, d, s[Gr::of(j)]); }
+      const float own = t.own(i) ? 1.0f : 0.0f;
+#pragma unroll
+      for (int k = 0; k < GV; ++k) acc[0][k] = fmaf(s[k], own, acc[0][k]);
     }
+    const int rows = lay_columns<NT, 1, GV>(acc, t.sv, t.rows, s_red);
+    sum_columns<NT, 1>(s_red, 0, w, rows, ncol, ng, [&](int k, const float (&sum)[1]) {
+      const float r = rstd_of(sum[0], n, a.eps);
+      s_rstd[k] = r;
+      out_mean[k] = s_mean[k]; out_rstd[k] = r;
+    });
+    __syncthreads();
+  }
+  // z = (x - mean) (rstd gamma) + beta
+  Affine<VE> af(a, t.c);
+#pragma unroll
+  for (int j = 0; j < VE; ++j) af.gamma[j] *= s_rstd[g[Gr::of(j)]];
+  const BufRsrc y = t.buffer(a.out);
+  t.forget_rounds();
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    forget(v[i]);
+    unpack<T, VE>(v[i], f);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f[j] = act_of<T, ACT>(fmaf(f[j] - mean[Gr::of(j)], af.gamma[j], af.beta[j]));
+    t.store(y, i, pack<T, VE>(f));
+  }
 }
 
-// s1[c] = sum dz, s2[c] = sum dz xhat of the slice's channels, joined over the pixels; written to part as well.
-template <int NT, int VE>
-__device__ __forceinline__ void channel_sums(const float (&v)[VE], int sv, int rows, float* s_red, float* s_out, float* part) {
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < VE; ++j) s_red[threadIdx.x * VE + j] = v[j];
-  __syncthreads();
-  const int w = sv * VE;
-  int lanes = 64;
-  while (lanes > 1 && lanes * w > NT) lanes >>= 1;
-  const int k = threadIdx.x & (lanes - 1);
-  for (int c0 = 0; c0 < w; c0 += NT / lanes) {
-    const int c = c0 + threadIdx.x / lanes;
-    float sum = 0.0f;
-    if (c < w) for (int r = k; r < rows; r += lanes) sum += s_red[r * w + c];
-    for (int d = lanes >> 1; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-    if (c < w && k == 0) { s_out[c] = sum; part[c] = sum; }
-  }
-}
-
-// part[0][b][c] = sum dz, part[1][b][c] = sum dz xhat.
-template <typename T, int ACT, int NT, int VPT>
+// part[0][b][c] = sum dz, part[1][b][c] = sum dz xhat.  A vector's channels go four at a time: unpacked values of eight (bf16) do not
+// fit beside the held vectors and the channels' constants.  (Vectors of four bf16 channels fit, but twice the loads cost more:
+// 256 x 28 x 28 x 512 174 us against 148.)
+template <typename T, int ACT, int GV, int NT, int VPT>
 __global__ __launch_bounds__(NT) void gn_backward_resident_kernel(GnArgs a) {
-  typedef Tile<T, NT, VPT> Tl;
-  constexpr int VE = Tl::VE;
-  __shared__ float s_red[NT * VE];
-  __shared__ float s_c[2][NT * VE];
-  const int b = blockIdx.x / a.slices, slice = blockIdx.x - b * a.slices;
-  const Tl t(a, b, slice);
+  constexpr int VE = 16 / sizeof(T);
+  typedef Tile<T, VE, NT> Tl;
+  typedef Groups<VE, GV> Gr;
+  __shared__ float s_red[2 * NT * VE], s_c[2][kMaxSlice * VE], s_g[2][kMaxSliceGroups];
+  Tl t(a, blockIdx.x, a.B * a.slices);
+  if (!t.valid) return;
   typename Tl::V vx[VPT], vd[VPT];
-  t.load(a.x, vx);
-  t.load(a.dy, vd);
-  float mean[VE], rstd[VE], s1[VE], s2[VE], f[VE], d[VE];
-  const Affine<VE> w(a, t.c);
+  {
+    const BufRsrc x = t.buffer(a.x), dy = t.buffer(a.dy);
 #pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const int64_t g = (int64_t)b * a.G + (t.c + j) / a.Cg;
-    mean[j] = a.mean_in[g]; rstd[j] = a.rstd_in[g];
-    s1[j] = s2[j] = 0.0f;
+    for (int i = 0; i < VPT; ++i) { t.load(x, i, vx[i]); t.load(dy, i, vd[i]); }
   }
-#pragma unroll
-  for (int i = 0; i < VPT; ++i)
-    if (i < t.count) {
-      unpack(vx[i], f);
-      unpack(vd[i], d);
-#pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float xhat = gn_xhat(f[j], mean[j], rstd[j]);
-        const float dz = act_grad<T, ACT>(gn_z(xhat, w.gamma[j], w.beta[j]), d[j]);
-        s1[j] += dz; s2[j] = fmaf(dz, xhat, s2[j]);
-      }
-    }
-  float* part = a.part + (int64_t)b * a.C + slice * a.sv * VE;
-  channel_sums<NT, VE>(s1, t.sv, t.rows, s_red, s_c[0], part);
-  channel_sums<NT, VE>(s2, t.sv, t.rows, s_red, s_c[1], part + (int64_t)a.B * a.C);
-  __syncthreads();
-  if (t.count == 0) return;
   const float n = (float)a.P * (float)a.Cg;
-  const int c_slice = slice * a.sv * VE;
-  float c1[VE], c2[VE];
+  const int w = t.sv * VE, ng = w / a.Cg, g_first = t.c_slice / a.Cg;
+  int g[GV];
+  Gr::find(t.c, a.Cg, g);
+  float mean[GV], rstd[GV], s[2][VE];
+  const Affine<VE> af(a, t.c);
 #pragma unroll
-  for (int j = 0; j < VE; ++j) {
-    const int first = (t.c + j) / a.Cg * a.Cg;
-    if (j > 0 && (t.c + j) % a.Cg) { c1[j] = c1[j - 1]; c2[j] = c2[j - 1]; continue; }
-    float u1 = 0.0f, u2 = 0.0f;
-    for (int c = first; c < first + a.Cg; ++c) {
-      const float gamma = a.gamma ? a.gamma[c] : 1.0f;
-      u1 = fmaf(gamma, s_c[0][c - c_slice], u1); u2 = fmaf(gamma, s_c[1][c - c_slice], u2);
-    }
-    c1[j] = u1 / n; c2[j] = u2 / n;
-  }
-  typename Tl::V* dx = reinterpret_cast<typename Tl::V*>(a.out) + t.at;
+  for (int k = 0; k < GV; ++k) { mean[k] = a.mean_in[(int64_t)t.b * a.G + g[k]]; rstd[k] = a.rstd_in[(int64_t)t.b * a.G + g[k]]; }
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
-    if (i < t.count) {
-      unpack(vx[i], f);
-      unpack(vd[i], d);
+  for (int j = 0; j < VE; ++j) s[0][j] = s[1][j] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float xhat = gn_xhat(f[j], mean[j], rstd[j]);
-        const float dz = act_grad<T, ACT>(gn_z(xhat, w.gamma[j], w.beta[j]), d[j]);
-        f[j] = rstd[j] * ((dz * w.gamma[j] - c1[j]) - xhat * c2[j]);
+  for (int i = 0; i < VPT; ++i) {          // (past the end: dy = 0)
+    forget(vx[i]);
+    forget(vd[i]);
+#pragma unroll
+    for (int h = 0; h < VE; h += 4) {
+      float f[4], d[4];
+      unpack4<T>(vx[i], h, f);
+      if constexpr (ACT == DAT_ACT_RELU) {     // dy becomes dz where it is held: the second pass needs no z
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool on = gn_z(f[j] - mean[Gr::of(h + j)], rstd[Gr::of(h + j)], af.gamma[h + j], af.beta[h + j]) > 0.0f;
+          const uint32_t whole = 0xffffffffu, half = j % 2 ? 0x0000ffffu : 0xffff0000u;   // what stays if it is off
+          vd[i][sizeof(T) == 4 ? h + j : (h + j) / 2] &= on ? whole : sizeof(T) == 4 ? 0u : half;
+        }
       }
-      pack(f, dx + i * t.step);
+      unpack4<T>(vd[i], h, d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = Gr::of(h + j);
+        const float xm = f[j] - mean[k];
+        if constexpr (ACT == DAT_ACT_SILU) d[j] = silu_dz<T>(fmaf(xm, rstd[k] * af.gamma[h + j], af.beta[h + j]), d[j]);
+        s[0][h + j] += d[j]; s[1][h + j] = fmaf(d[j], xm, s[1][h + j]);
+      }
+      __builtin_amdgcn_sched_barrier(0);       // (the scheduler would unpack them all first, and spill)
     }
+    if (ACT == DAT_ACT_RELU) forget(vd[i]);    // (masked here, not where it is read)
+  }
+#pragma unroll
+  for (int j = 0; j < VE; ++j) { s[1][j] *= rstd[Gr::of(j)]; forget(s[1][j]); }   // (here, not sunk below the first barrier)
+  float* part = a.part + (int64_t)t.b * a.C + t.c_slice;
+  const int rows = lay_columns<NT, 2, VE>(s, t.sv, t.rows, s_red);
+  sum_columns<NT, 2>(s_red, NT * VE, w, rows, 1, w, [&](int c, const float (&sum)[2]) {
+    const float gamma = a.gamma ? a.gamma[t.c_slice + c] : 1.0f;
+    part[c] = sum[0]; part[(int64_t)a.B * a.C + c] = sum[1];
+    s_c[0][c] = gamma * sum[0]; s_c[1][c] = gamma * sum[1];
+  });
+  __syncthreads();
+  sum_columns<NT, 2>(s_c[0], kMaxSlice * VE, 0, 1, a.Cg, ng, [&](int k, const float (&sum)[2]) {
+    s_g[0][k] = __fdiv_rn(sum[0], n); s_g[1][k] = __fdiv_rn(sum[1], n);
+  });
+  __syncthreads();
+  // dx = rstd (gamma dz - c1 - xhat c2) = (rstd gamma) dz + ((x - mean) (-rstd^2 c2) - rstd c1)
+  float q1[GV], q2[GV];
+#pragma unroll
+  for (int k = 0; k < GV; ++k) { q1[k] = -rstd[k] * s_g[0][g[k] - g_first]; q2[k] = -(rstd[k] * rstd[k]) * s_g[1][g[k] - g_first]; }
+  float scale[VE];
+#pragma unroll
+  for (int j = 0; j < VE; ++j) scale[j] = rstd[Gr::of(j)] * af.gamma[j];
+  const BufRsrc dx = t.buffer(a.out);
+  t.forget_rounds();
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    forget(vx[i]);
+    forget(vd[i]);
+#pragma unroll
+    for (int h = 0; h < VE; h += 4) {
+      float f[4], d[4];
+      unpack4<T>(vx[i], h, f);
+      unpack4<T>(vd[i], h, d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = Gr::of(h + j);
+        const float xm = f[j] - mean[k];
+        if constexpr (ACT == DAT_ACT_SILU) d[j] = silu_dz<T>(fmaf(xm, scale[h + j], af.beta[h + j]), d[j]);
+        f[j] = fmaf(scale[h + j], d[j], fmaf(xm, q2[k], q1[k]));
+      }
+      pack4<T>(f, h, vx[i]);
+    }
+    t.store(dx, i, vx[i]);
+  }
 }
 
 // ---- split -------------------------------------------------------------------------------------------------------------
@@ -285,7 +479,7 @@ __global__ __launch_bounds__(NT) void gn_backward_resident_kernel(GnArgs a) {
 constexpr int kT = 256;
 constexpr int kHeld = 8;          // pixels a thread of the forward statistics holds: chunk = kHeld * rows
 
-template <typename T, int VE> struct Range {
+template <typename T, int VE, bool BACK> struct Range {   // BACK: images from the last to the first
   typedef typename Vec<T, VE>::type V;
   int sv, rows, tx, ty, c, p0, p1;           // p0: own first pixel; p1: end of the range
   int64_t base;                              // vectors of the image's first pixel, own channels
@@ -295,7 +489,7 @@ template <typename T, int VE> struct Range {
     b = blockIdx.x / per;
     const int rest = blockIdx.x - b * per, slice = rest / a.chunks;
     chunk = rest - slice * a.chunks;
-    b += a.b0;
+    if (BACK) b = a.B - 1 - b;
     sv = min(a.sv, a.nv - slice * a.sv);
     rows = kT / sv;
     ty = threadIdx.x / sv; tx = threadIdx.x - ty * sv;
@@ -307,19 +501,19 @@ template <typename T, int VE> struct Range {
   }
 };
 
-// Sums of VE values over the threads of a vector; result in the threads with ty = 0.
-template <int VE> __device__ __forceinline__ void range_sums(float (&v)[VE], int sv, int rows, int tx, int ty, float* s_red) {
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < VE; ++j) s_red[j * kT + threadIdx.x] = v[j];
-  __syncthreads();
+// Sums of VE values over the threads of a vector; result in the threads with ty = 0.  Lanes of a wavefront that share a vector
+// are joined in registers first.
+template <int M, int VE> __device__ __forceinline__ void range_sums(float (&v)[M][VE], int sv, int rows, int tx, int ty, float* s_red) {
+  const int left = lay_columns<kT, M, VE>(v, sv, rows, s_red);
   if (ty == 0) {
 #pragma unroll
-    for (int j = 0; j < VE; ++j) {
-      float s = 0.0f;
-      for (int r = 0; r < rows; ++r) s += s_red[j * kT + r * sv + tx];
-      v[j] = s;
-    }
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        float s = 0.0f;
+        for (int r = 0; r < left; ++r) s += s_red[(m * kT + r * sv + tx) * VE + j];
+        v[m][j] = s;
+      }
   }
 }
 
@@ -327,43 +521,43 @@ template <int VE> __device__ __forceinline__ void range_sums(float (&v)[VE], int
 template <typename T, int VE>
 __global__ __launch_bounds__(kT) void gn_stats_kernel(GnArgs a) {
   __shared__ float s_red[VE * kT], s_mean[VE * kT];
-  const Range<T, VE> r(a);
-  const typename Range<T, VE>::V* x = reinterpret_cast<const typename Range<T, VE>::V*>(a.x) + r.base;
-  typename Range<T, VE>::V v[kHeld];
+  const Range<T, VE, false> r(a);
+  const typename Range<T, VE, false>::V* x = reinterpret_cast<const typename Range<T, VE, false>::V*>(a.x) + r.base;
+  typename Range<T, VE, false>::V v[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) v[i] = x[(int64_t)min(r.p0 + i * r.rows, a.P - 1) * a.nv];
-  float acc[VE], f[VE];
+  float acc[1][VE], f[VE];
 #pragma unroll
-  for (int j = 0; j < VE; ++j) acc[j] = 0.0f;
+  for (int j = 0; j < VE; ++j) acc[0][j] = 0.0f;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
     if (r.p0 + i * r.rows < r.p1) {
-      unpack(v[i], f);
+      unpack<T, VE>(v[i], f);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) acc[j] += f[j];
+      for (int j = 0; j < VE; ++j) acc[0][j] += f[j];
     }
-  range_sums<VE>(acc, r.sv, r.rows, r.tx, r.ty, s_red);
+  range_sums<1, VE>(acc, r.sv, r.rows, r.tx, r.ty, s_red);
   const float n = (float)(r.p1 - r.chunk * a.chunk);
   if (r.ty == 0) {
 #pragma unroll
-    for (int j = 0; j < VE; ++j) { acc[j] = __fdiv_rn(acc[j], n); s_mean[j * kT + r.tx] = acc[j]; }
+    for (int j = 0; j < VE; ++j) { acc[0][j] = __fdiv_rn(acc[0][j], n); s_mean[j * kT + r.tx] = acc[0][j]; }
   }
   __syncthreads();
   float mean[VE];
 #pragma unroll
-  for (int j = 0; j < VE; ++j) { mean[j] = s_mean[j * kT + r.tx]; acc[j] = 0.0f; }
+  for (int j = 0; j < VE; ++j) { mean[j] = s_mean[j * kT + r.tx]; acc[0][j] = 0.0f; }
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
     if (r.p0 + i * r.rows < r.p1) {
-      unpack(v[i], f);
+      unpack<T, VE>(v[i], f);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) { const float d = f[j] - mean[j]; acc[j] = fmaf(d, d, acc[j]); }
+      for (int j = 0; j < VE; ++j) { const float d = f[j] - mean[j]; acc[0][j] = fmaf(d, d, acc[0][j]); }
     }
-  range_sums<VE>(acc, r.sv, r.rows, r.tx, r.ty, s_red);
+  range_sums<1, VE>(acc, r.sv, r.rows, r.tx, r.ty, s_red);
   if (r.ty == 0) {
-    float* part = a.part + ((int64_t)(r.b - a.b0) * a.chunks + r.chunk) * 2 * a.C + r.c;
+    float* part = a.part + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + r.c;
 #pragma unroll
-    for (int j = 0; j < VE; ++j) { part[j] = mean[j]; part[a.C + j] = acc[j]; }
+    for (int j = 0; j < VE; ++j) { part[j] = mean[j]; part[a.C + j] = acc[0][j]; }
   }
 }
 
@@ -391,125 +585,135 @@ __global__ __launch_bounds__(64) void gn_join_stats_kernel(GnArgs a) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d);
   if (threadIdx.x == 0) {
-    a.mean[(int64_t)(a.b0 + b) * a.G + g] = mean;
-    a.rstd[(int64_t)(a.b0 + b) * a.G + g] = rstd_of(s, n, a.eps);
+    a.mean[(int64_t)b * a.G + g] = mean;
+    a.rstd[(int64_t)b * a.G + g] = rstd_of(s, n, a.eps);
   }
 }
 
 template <typename T, int VE, int ACT>
 __global__ __launch_bounds__(kT) void gn_apply_kernel(GnArgs a) {
-  const Range<T, VE> r(a);
+  const Range<T, VE, true> r(a);
   if (r.p0 >= r.p1) return;
-  typedef typename Range<T, VE>::V V;
+  typedef typename Range<T, VE, true>::V V;
   const V* x = reinterpret_cast<const V*>(a.x) + r.base;
   V* y = reinterpret_cast<V*>(a.out) + r.base;
-  const Affine<VE> w(a, r.c);
-  float mean[VE], rstd[VE], f[VE];
+  Affine<VE> w(a, r.c);
+  float mean[VE], f[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
     const int64_t g = (int64_t)r.b * a.G + (r.c + j) / a.Cg;
-    mean[j] = a.mean[g]; rstd[j] = a.rstd[g];
+    mean[j] = a.mean[g]; w.gamma[j] *= a.rstd[g];
   }
 #pragma unroll 4
   for (int p = r.p0; p < r.p1; p += r.rows) {
-    unpack(x[(int64_t)p * a.nv], f);
+    unpack<T, VE>(x[(int64_t)p * a.nv], f);
 #pragma unroll
-    for (int j = 0; j < VE; ++j) f[j] = act_of<T, ACT>(gn_z(gn_xhat(f[j], mean[j], rstd[j]), w.gamma[j], w.beta[j]));
-    pack(f, y + (int64_t)p * a.nv);
+    for (int j = 0; j < VE; ++j) f[j] = act_of<T, ACT>(fmaf(f[j] - mean[j], w.gamma[j], w.beta[j]));
+    y[(int64_t)p * a.nv] = pack<T, VE>(f);
   }
 }
 
-// Sums of dz and dz xhat of every channel within the range: part[(b, chunk)][0..1][c].
+// Sums of dz and dz xhat of every channel within the range: ranges[(image of the batch, chunk)][0..1][c].
 template <typename T, int VE, int ACT>
-__global__ __launch_bounds__(kT) void gn_grad_sums_kernel(GnArgs a) {
-  __shared__ float s_red[VE * kT];
-  const Range<T, VE> r(a);
-  typedef typename Range<T, VE>::V V;
+__global__ __launch_bounds__(kT) void gn_grad_sums_kernel(GnArgs a, float* ranges) {
+  __shared__ float s_red[2 * VE * kT];
+  const Range<T, VE, false> r(a);
+  typedef typename Range<T, VE, false>::V V;
   const V* x = reinterpret_cast<const V*>(a.x) + r.base;
   const V* dy = reinterpret_cast<const V*>(a.dy) + r.base;
   const Affine<VE> w(a, r.c);
-  float mean[VE], rstd[VE], s1[VE], s2[VE], f[VE], d[VE];
+  float mean[VE], rstd[VE], s[2][VE], f[VE], d[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
     const int64_t g = (int64_t)r.b * a.G + (r.c + j) / a.Cg;
     mean[j] = a.mean_in[g]; rstd[j] = a.rstd_in[g];
-    s1[j] = s2[j] = 0.0f;
+    s[0][j] = s[1][j] = 0.0f;
   }
 #pragma unroll 4
   for (int p = r.p0; p < r.p1; p += r.rows) {
-    unpack(x[(int64_t)p * a.nv], f);
-    unpack(dy[(int64_t)p * a.nv], d);
+    unpack<T, VE>(x[(int64_t)p * a.nv], f);
+    unpack<T, VE>(dy[(int64_t)p * a.nv], d);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      const float xhat = gn_xhat(f[j], mean[j], rstd[j]);
-      const float dz = act_grad<T, ACT>(gn_z(xhat, w.gamma[j], w.beta[j]), d[j]);
-      s1[j] += dz; s2[j] = fmaf(dz, xhat, s2[j]);
+      const float xm = f[j] - mean[j], dz = gn_dz<T, ACT>(xm, d[j], rstd[j], w.gamma[j], rstd[j] * w.gamma[j], w.beta[j]);
+      s[0][j] += dz; s[1][j] = fmaf(dz, xm, s[1][j]);
     }
   }
-  range_sums<VE>(s1, r.sv, r.rows, r.tx, r.ty, s_red);
-  range_sums<VE>(s2, r.sv, r.rows, r.tx, r.ty, s_red);
-  if (r.ty == 0) {
-    float* part = a.part + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + r.c;
 #pragma unroll
-    for (int j = 0; j < VE; ++j) { part[j] = s1[j]; part[a.C + j] = s2[j]; }
+  for (int j = 0; j < VE; ++j) s[1][j] *= rstd[j];
+  range_sums<2, VE>(s, r.sv, r.rows, r.tx, r.ty, s_red);
+  if (r.ty == 0) {
+    float* out = ranges + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + r.c;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) { out[j] = s[0][j]; out[a.C + j] = s[1][j]; }
   }
 }
 
-// One wavefront per image and group: the two means of the group, to join[(b, g)][0..1].
-__global__ __launch_bounds__(64) void gn_join_grad_kernel(GnArgs a, float* join) {
-  const int b = a.b0 + blockIdx.x / a.G, g = blockIdx.x % a.G, entries = a.chunks * a.Cg;
-  const float* part = a.part + (int64_t)b * a.chunks * 2 * a.C + g * a.Cg;
+// One workgroup per image and group: sums over the ranges, for every channel to part[0][b][c] and [1][b][c] (as the resident
+// kernel leaves them) and for the group, as means, to join[(b, g)][0..1].  A wavefront takes channels, its lanes the ranges.
+__global__ __launch_bounds__(kT) void gn_join_grad_kernel(GnArgs a, const float* ranges, float* join) {
+  __shared__ float s[2][kT / 64];
+  const int b = blockIdx.x / a.G, g = blockIdx.x % a.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float* q = ranges + (int64_t)b * a.chunks * 2 * a.C + g * a.Cg;
   float c1 = 0.0f, c2 = 0.0f;
-  for (int e = threadIdx.x; e < entries; e += 64) {
-    const int k = e / a.Cg, c = e - k * a.Cg;
-    const float gamma = a.gamma ? a.gamma[g * a.Cg + c] : 1.0f;
-    const float* q = part + (int64_t)k * 2 * a.C + c;
-    c1 = fmaf(gamma, q[0], c1); c2 = fmaf(gamma, q[a.C], c2);
-  }
+  for (int c = wave; c < a.Cg; c += kT / 64) {
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int k = lane; k < a.chunks; k += 64) { s1 += q[(int64_t)k * 2 * a.C + c]; s2 += q[(int64_t)k * 2 * a.C + a.C + c]; }
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) { c1 += __shfl_xor(c1, d); c2 += __shfl_xor(c2, d); }
-  const float n = (float)a.P * (float)a.Cg;
-  if (threadIdx.x == 0) { join[((int64_t)b * a.G + g) * 2] = c1 / n; join[((int64_t)b * a.G + g) * 2 + 1] = c2 / n; }
+    for (int d = 32; d >= 1; d >>= 1) { s1 += __shfl_xor(s1, d); s2 += __shfl_xor(s2, d); }
+    if (lane == 0) {
+      float* part = a.part + (int64_t)b * a.C + g * a.Cg + c;
+      part[0] = s1; part[(int64_t)a.B * a.C] = s2;
+    }
+    const float gamma = a.gamma ? a.gamma[g * a.Cg + c] : 1.0f;
+    c1 = fmaf(gamma, s1, c1); c2 = fmaf(gamma, s2, c2);
+  }
+  if (lane == 0) { s[0][wave] = c1; s[1][wave] = c2; }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const float* v = s[threadIdx.x];
+    join[((int64_t)b * a.G + g) * 2 + threadIdx.x] = ((v[0] + v[1]) + (v[2] + v[3])) / ((float)a.P * (float)a.Cg);
+  }
 }
 
 template <typename T, int VE, int ACT>
 __global__ __launch_bounds__(kT) void gn_grad_apply_kernel(GnArgs a, const float* join) {
-  const Range<T, VE> r(a);
+  const Range<T, VE, true> r(a);
   if (r.p0 >= r.p1) return;
-  typedef typename Range<T, VE>::V V;
+  typedef typename Range<T, VE, true>::V V;
   const V* x = reinterpret_cast<const V*>(a.x) + r.base;
   const V* dy = reinterpret_cast<const V*>(a.dy) + r.base;
   V* dx = reinterpret_cast<V*>(a.out) + r.base;
   const Affine<VE> w(a, r.c);
-  float mean[VE], rstd[VE], c1[VE], c2[VE], f[VE], d[VE];
+  float mean[VE], rstd[VE], q1[VE], q2[VE], f[VE], d[VE];
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
     const int64_t g = (int64_t)r.b * a.G + (r.c + j) / a.Cg;
-    mean[j] = a.mean_in[g]; rstd[j] = a.rstd_in[g]; c1[j] = join[2 * g]; c2[j] = join[2 * g + 1];
+    mean[j] = a.mean_in[g]; rstd[j] = a.rstd_in[g];
+    q1[j] = -rstd[j] * join[2 * g]; q2[j] = -(rstd[j] * rstd[j]) * join[2 * g + 1];
   }
 #pragma unroll 4
   for (int p = r.p0; p < r.p1; p += r.rows) {
-    unpack(x[(int64_t)p * a.nv], f);
-    unpack(dy[(int64_t)p * a.nv], d);
+    unpack<T, VE>(x[(int64_t)p * a.nv], f);
+    unpack<T, VE>(dy[(int64_t)p * a.nv], d);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      const float xhat = gn_xhat(f[j], mean[j], rstd[j]);
-      const float dz = act_grad<T, ACT>(gn_z(xhat, w.gamma[j], w.beta[j]), d[j]);
-      f[j] = rstd[j] * ((dz * w.gamma[j] - c1[j]) - xhat * c2[j]);
+      const float xm = f[j] - mean[j], dz = gn_dz<T, ACT>(xm, d[j], rstd[j], w.gamma[j], rstd[j] * w.gamma[j], w.beta[j]);
+      f[j] = fmaf(rstd[j] * w.gamma[j], dz, fmaf(xm, q2[j], q1[j]));
     }
-    pack(f, dx + (int64_t)p * a.nv);
+    dx[(int64_t)p * a.nv] = pack<T, VE>(f);
   }
 }
 
-// dbeta[c] = sum of part[k][c], dgamma[c] = sum of part[k][second + c] over k < n, `stride` floats apart.
+// dbeta[c] and dgamma[c]: the sums over the images of part[0][b][c] and part[1][b][c].
 constexpr int kParamRows = 16;
-__global__ __launch_bounds__(64 * kParamRows) void gn_param_kernel(const float* part, int n, int64_t stride, int64_t second, int C,
-                                                                   float* dgamma, float* dbeta) {
+__global__ __launch_bounds__(64 * kParamRows) void gn_param_kernel(const float* part, int B, int C, float* dgamma, float* dbeta) {
   __shared__ float s[2][kParamRows][64];
   const int lane = threadIdx.x & 63, row = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float s1 = 0.0f, s2 = 0.0f;
   if (c < C)
-    for (int k = row; k < n; k += kParamRows) { s1 += part[k * stride + c]; s2 += part[k * stride + second + c]; }
+#pragma unroll 8
+    for (int b = row; b < B; b += kParamRows) { s1 += part[(int64_t)b * C + c]; s2 += part[(int64_t)(B + b) * C + c]; }
   s[0][row][lane] = s1; s[1][row][lane] = s2;
   __syncthreads();
   if (row == 0 && c < C) {
@@ -527,10 +731,7 @@ struct Plan {
   int nv, sv, slices;
   int nt, vpt;         // resident: threads, vectors each; nt = 0: split
   int chunk, chunks;   // split
-  int batch;           // split: images at a time
 };
-
-constexpr int64_t kCacheBytes = 128ll << 20;   // of the 256 MiB last-level cache, for the tensors of a batch
 
 Plan plan_of(bool backward, dat_dtype dtype, bool vectors, int B, int P, int C, int G) {
   Plan p{};
@@ -539,18 +740,22 @@ Plan plan_of(bool backward, dat_dtype dtype, bool vectors, int B, int P, int C, 
   p.nv = C / p.ve;
   if (p.ve > 1) {
     const int unit = Cg / gcd(Cg, whole);              // vectors of the smallest slice of whole groups
-    static const int sizes[][2] = {{256, 2}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
-    const int most = backward ? 4 : 5;
-    // rows of 128 bytes if they fit, else 64; narrower where there would be few workgroups
-    for (int want = 8; want >= 4 && !p.nt; want >>= 1) {
-      int sv = unit * ((want + unit - 1) / unit);
-      while (sv > unit && (int64_t)B * ((p.nv + sv - 1) / sv) < 512) sv = sv / 2 / unit * unit >= unit ? sv / 2 / unit * unit : unit;
-      if (sv > p.nv) sv = p.nv;
-      if (sv * whole / Cg > kMaxSliceGroups) break;
-      for (int i = 0; i < most; ++i) {
-        const int nt = sizes[i][0], vpt = sizes[i][1];
-        if (sv <= nt && (P + nt / sv - 1) / (nt / sv) <= vpt) { p.sv = sv; p.nt = nt; p.vpt = vpt; break; }
-      }
+    // Tiles of up to 16 vectors a thread (backward: 8 of x and 8 of dy), in the smallest workgroup that takes rows of 64 bytes:
+    // several of them on a compute unit, each at its own stage.  Wider rows where the image is small; narrower ones where there
+    // would be fewer tiles than compute units want.
+    static const int fwd[][2] = {{256, 2}, {256, 8}, {256, 16}, {512, 16}, {1024, 16}}, bwd[][2] = {{256, 2}, {256, 8}, {512, 8}, {1024, 8}};
+    const int (*sizes)[2] = backward ? bwd : fwd;
+    const int count = backward ? 4 : 5, nv = p.nv;
+    auto fits = [&](int sv, int i) { return sv <= sizes[i][0] && (P + sizes[i][0] / sv - 1) / (sizes[i][0] / sv) <= sizes[i][1]; };
+    int sv = unit, i = 0;
+    while (sv * 16 < 64 && 2 * sv <= nv) sv *= 2;
+    const int least = sv;
+    while (2 * sv <= nv && fits(2 * sv, backward ? 1 : 2) && (int64_t)B * (nv / (2 * sv)) >= 1024) sv *= 2;
+    if (sv == least) while (sv > unit && (int64_t)B * ((nv + sv - 1) / sv) < 512) sv /= 2;
+    if (sv < unit) sv = unit;
+    while (i < count && !fits(sv, i)) ++i;
+    if (i < count && sv <= kMaxSlice && sv * whole / Cg <= kMaxSliceGroups && (int64_t)P * C * width < kOob) {
+      p.sv = sv; p.nt = sizes[i][0]; p.vpt = sizes[i][1];
     }
     if (p.nt) { p.slices = (p.nv + p.sv - 1) / p.sv; return p; }
   }
@@ -559,9 +764,6 @@ Plan plan_of(bool backward, dat_dtype dtype, bool vectors, int B, int P, int C, 
   p.slices = (p.nv + p.sv - 1) / p.sv;
   p.chunk = kHeld * (kT / p.sv);
   p.chunks = (P + p.chunk - 1) / p.chunk;
-  const int64_t image = (int64_t)P * C * width * (backward ? 2 : 1);
-  p.batch = (int)(kCacheBytes / image < 1 ? 1 : kCacheBytes / image > B ? B : kCacheBytes / image);
-  if (p.batch < 1) p.batch = 1;
   return p;
 }
 
@@ -573,8 +775,8 @@ dat_status check(dat_dtype dtype, int B, int H, int W, int C, int groups) {
 }
 
 size_t workspace_of(const Plan& p, bool backward, int B, int C, int G) {
-  if (backward) return p.nt ? (size_t)B * C * 8 : ((size_t)B * p.chunks * C + (size_t)B * G) * 8;
-  return p.nt ? 0 : (size_t)p.batch * p.chunks * C * 8;
+  if (backward) return p.nt ? (size_t)B * C * 8 : ((size_t)B * C + (size_t)B * G + (size_t)B * p.chunks * C) * 8;
+  return p.nt ? 0 : (size_t)B * p.chunks * C * 8;
 }
 
 #define DAT_GN_ACT(act, ...)                                                              \
@@ -584,28 +786,43 @@ size_t workspace_of(const Plan& p, bool backward, int B, int C, int G) {
     else { constexpr int ACT = DAT_ACT_NONE; __VA_ARGS__; }                               \
   } while (0)
 
-template <typename T, bool WHOLE> void launch_forward_resident(const Plan& p, const GnArgs& a, dat_act act, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.slices));
-#define DAT_GN_SIZE(NT, VPT) if (p.nt == NT && p.vpt == VPT) DAT_GN_ACT(act, hipLaunchKernelGGL((gn_forward_resident_kernel<T, ACT, WHOLE, NT, VPT>), grid, dim3(NT), 0, st, a))
-  DAT_GN_SIZE(256, 2); DAT_GN_SIZE(256, 8); DAT_GN_SIZE(512, 8); DAT_GN_SIZE(1024, 8); DAT_GN_SIZE(1024, 16);
+inline unsigned tiles_of(const GnArgs& a) { return (unsigned)(((int64_t)a.B * a.slices + kXcds - 1) / kXcds * kXcds); }
+
+template <typename T, int GV> void launch_forward_resident(const Plan& p, const GnArgs& a, dat_act act, hipStream_t st) {
+  const dim3 grid(tiles_of(a));
+#define DAT_GN_SIZE(NT, VPT) if (p.nt == NT && p.vpt == VPT) DAT_GN_ACT(act, hipLaunchKernelGGL((gn_forward_resident_kernel<T, ACT, GV, NT, VPT>), grid, dim3(NT), 0, st, a))
+  DAT_GN_SIZE(256, 2); DAT_GN_SIZE(256, 8); DAT_GN_SIZE(256, 16); DAT_GN_SIZE(512, 16); DAT_GN_SIZE(1024, 16);
 #undef DAT_GN_SIZE
 }
-template <typename T> void launch_backward_resident(const Plan& p, const GnArgs& a, dat_act act, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.slices));
-#define DAT_GN_SIZE(NT, VPT) if (p.nt == NT && p.vpt == VPT) DAT_GN_ACT(act, hipLaunchKernelGGL((gn_backward_resident_kernel<T, ACT, NT, VPT>), grid, dim3(NT), 0, st, a))
+template <typename T, int GV> void launch_backward_resident(const Plan& p, const GnArgs& a, dat_act act, hipStream_t st) {
+  const dim3 grid(tiles_of(a));
+#define DAT_GN_SIZE(NT, VPT) if (p.nt == NT && p.vpt == VPT) DAT_GN_ACT(act, hipLaunchKernelGGL((gn_backward_resident_kernel<T, ACT, GV, NT, VPT>), grid, dim3(NT), 0, st, a))
   DAT_GN_SIZE(256, 2); DAT_GN_SIZE(256, 8); DAT_GN_SIZE(512, 8); DAT_GN_SIZE(1024, 8);
 #undef DAT_GN_SIZE
 }
-template <typename T, int VE> void launch_forward_split(const GnArgs& a, int images, dat_act act, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)images * a.chunks * a.slices));
+template <int VE, typename F> void with_groups(int Cg, F f) {
+  const int gv = Cg % VE == 0 ? 1 : Cg > 1 && VE % Cg == 0 ? VE / Cg : VE;
+  if (gv == 1) f(std::integral_constant<int, 1>());
+  else if (gv == 2) f(std::integral_constant<int, 2>());
+  else if (gv == 4) f(std::integral_constant<int, 4>());
+  else if constexpr (VE == 8) f(std::integral_constant<int, 8>());
+}
+template <typename T> void launch_resident(bool backward, const Plan& p, const GnArgs& a, dat_act act, hipStream_t st) {
+  with_groups<16 / sizeof(T)>(a.Cg, [&](auto gv) {
+    if (backward) launch_backward_resident<T, decltype(gv)::value>(p, a, act, st);
+    else launch_forward_resident<T, decltype(gv)::value>(p, a, act, st);
+  });
+}
+template <typename T, int VE> void launch_forward_split(const GnArgs& a, dat_act act, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)a.B * a.chunks * a.slices));
   hipLaunchKernelGGL((gn_stats_kernel<T, VE>), grid, dim3(kT), 0, st, a);
-  hipLaunchKernelGGL(gn_join_stats_kernel, dim3((unsigned)((int64_t)images * a.G)), dim3(64), 0, st, a);
+  hipLaunchKernelGGL(gn_join_stats_kernel, dim3((unsigned)((int64_t)a.B * a.G)), dim3(64), 0, st, a);
   DAT_GN_ACT(act, hipLaunchKernelGGL((gn_apply_kernel<T, VE, ACT>), grid, dim3(kT), 0, st, a));
 }
-template <typename T, int VE> void launch_backward_split(const GnArgs& a, int images, dat_act act, float* join, hipStream_t st) {
-  const dim3 grid((unsigned)((int64_t)images * a.chunks * a.slices));
-  DAT_GN_ACT(act, hipLaunchKernelGGL((gn_grad_sums_kernel<T, VE, ACT>), grid, dim3(kT), 0, st, a));
-  hipLaunchKernelGGL(gn_join_grad_kernel, dim3((unsigned)((int64_t)images * a.G)), dim3(64), 0, st, a, join);
+template <typename T, int VE> void launch_backward_split(const GnArgs& a, dat_act act, float* join, float* ranges, hipStream_t st) {
+  const dim3 grid((unsigned)((int64_t)a.B * a.chunks * a.slices));
+  DAT_GN_ACT(act, hipLaunchKernelGGL((gn_grad_sums_kernel<T, VE, ACT>), grid, dim3(kT), 0, st, a, ranges));
+  hipLaunchKernelGGL(gn_join_grad_kernel, dim3((unsigned)((int64_t)a.B * a.G)), dim3(kT), 0, st, a, (const float*)ranges, join);
   DAT_GN_ACT(act, hipLaunchKernelGGL((gn_grad_apply_kernel<T, VE, ACT>), grid, dim3(kT), 0, st, a, (const float*)join));
 }
 
@@ -637,22 +854,17 @@ extern "C" dat_status dat_group_norm_forward(const void* x, const float* gamma, 
   if (B == 0) return DAT_OK;
   const Plan p = plan_of(false, dtype, aligned(x, 16) && aligned(y, 16), B, H * W, C, groups);
   GnArgs a{x, nullptr, gamma, beta, nullptr, nullptr, y, mean, rstd, (float*)workspace, B, H * W, C, groups, C / groups,
-           p.nv, p.sv, p.slices, p.chunk, p.chunks, 0, eps};
-  if ((int64_t)(p.nt ? B : p.batch) * p.slices * (p.nt ? 1 : p.chunks) > INT32_MAX) return DAT_ERR_SHAPE;
+           p.nv, p.sv, p.slices, p.chunk, p.chunks, eps};
+  if ((int64_t)B * p.slices * (p.nt ? 1 : p.chunks) > INT32_MAX) return DAT_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   if (p.nt) {
-    const bool whole = a.Cg % p.ve == 0;
-    if (dtype == DAT_BF16) { if (whole) launch_forward_resident<bf16_t, true>(p, a, act, st); else launch_forward_resident<bf16_t, false>(p, a, act, st); }
-    else { if (whole) launch_forward_resident<float, true>(p, a, act, st); else launch_forward_resident<float, false>(p, a, act, st); }
+    if (dtype == DAT_BF16) launch_resident<bf16_t>(false, p, a, act, st); else launch_resident<float>(false, p, a, act, st);
     DAT_LAUNCH_CHECK();
     return DAT_OK;
   }
-  for (a.b0 = 0; a.b0 < B; a.b0 += p.batch) {
-    const int images = B - a.b0 < p.batch ? B - a.b0 : p.batch;
-    if (dtype == DAT_BF16) { if (p.ve > 1) launch_forward_split<bf16_t, 8>(a, images, act, st); else launch_forward_split<bf16_t, 1>(a, images, act, st); }
-    else { if (p.ve > 1) launch_forward_split<float, 4>(a, images, act, st); else launch_forward_split<float, 1>(a, images, act, st); }
-    DAT_LAUNCH_CHECK();
-  }
+  if (dtype == DAT_BF16) { if (p.ve > 1) launch_forward_split<bf16_t, 8>(a, act, st); else launch_forward_split<bf16_t, 1>(a, act, st); }
+  else { if (p.ve > 1) launch_forward_split<float, 4>(a, act, st); else launch_forward_split<float, 1>(a, act, st); }
+  DAT_LAUNCH_CHECK();
   return DAT_OK;
 }
 
@@ -670,24 +882,19 @@ extern "C" dat_status dat_group_norm_backward(const void* x, const void* dy, con
   hipStream_t st = (hipStream_t)stream;
   const Plan p = plan_of(true, dtype, aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16), B, H * W, C, groups);
   GnArgs a{x, dy, gamma, beta, mean, rstd, dx, nullptr, nullptr, (float*)workspace, B, H * W, C, groups, C / groups,
-           p.nv, p.sv, p.slices, p.chunk, p.chunks, 0, 0.0f};
-  if ((int64_t)(p.nt ? B : p.batch) * p.slices * (p.nt ? 1 : p.chunks) > INT32_MAX) return DAT_ERR_SHAPE;
+           p.nv, p.sv, p.slices, p.chunk, p.chunks, 0.0f};
+  if ((int64_t)B * p.slices * (p.nt ? 1 : p.chunks) > INT32_MAX) return DAT_ERR_SHAPE;
   if (p.nt && B > 0) {
-    if (dtype == DAT_BF16) launch_backward_resident<bf16_t>(p, a, act, st); else launch_backward_resident<float>(p, a, act, st);
+    if (dtype == DAT_BF16) launch_resident<bf16_t>(true, p, a, act, st); else launch_resident<float>(true, p, a, act, st);
     DAT_LAUNCH_CHECK();
   } else if (B > 0) {
-    float* join = a.part + (int64_t)B * p.chunks * 2 * C;
-    for (a.b0 = 0; a.b0 < B; a.b0 += p.batch) {
-      const int images = B - a.b0 < p.batch ? B - a.b0 : p.batch;
-      if (dtype == DAT_BF16) { if (p.ve > 1) launch_backward_split<bf16_t, 8>(a, images, act, join, st); else launch_backward_split<bf16_t, 1>(a, images, act, join, st); }
-      else { if (p.ve > 1) launch_backward_split<float, 4>(a, images, act, join, st); else launch_backward_split<float, 1>(a, images, act, join, st); }
-      DAT_LAUNCH_CHECK();
-    }
+    float *join = a.part + (int64_t)B * C * 2, *ranges = join + (int64_t)B * groups * 2;
+    if (dtype == DAT_BF16) { if (p.ve > 1) launch_backward_split<bf16_t, 8>(a, act, join, ranges, st); else launch_backward_split<bf16_t, 1>(a, act, join, ranges, st); }
+    else { if (p.ve > 1) launch_backward_split<float, 4>(a, act, join, ranges, st); else launch_backward_split<float, 1>(a, act, join, ranges, st); }
+    DAT_LAUNCH_CHECK();
   }
   if (dgamma) {
-    const int n = p.nt ? B : B * p.chunks;
-    hipLaunchKernelGGL(gn_param_kernel, dim3((C + 63) / 64), dim3(64 * kParamRows), 0, st, (const float*)workspace, B == 0 ? 0 : n,
-                       (int64_t)(p.nt ? C : 2 * C), p.nt ? (int64_t)B * C : (int64_t)C, C, dgamma, dbeta);
+    hipLaunchKernelGGL(gn_param_kernel, dim3((C + 63) / 64), dim3(64 * kParamRows), 0, st, (const float*)workspace, B, C, dgamma, dbeta);
     DAT_LAUNCH_CHECK();
   }
   return DAT_OK;
