@@ -1,14 +1,21 @@
 // Log probabilities of given labels over rows of logits, with entropies and the largest alternatives, and the gradient.
 //
-// One pass with a running maximum M and the sums s = sum e^(x-M), w = sum (x-M) e^(x-M):  lse = M + log s,
-// logp_y = (x_y - M) - log s,  H = log s - w / s.  Alternatives are ordered by one 64-bit key, the logit (as an ordered integer)
-// above the complement of the index, so that equal logits go by ascending index and no two keys are equal.
+// With M = max x, s = sum 2^t and w = sum t 2^t, t = (x - M) log2 e:  lse = M + ln s,  logp_y = (x_y - M) - ln s,
+// H = ln s - ln 2 w / s.  The logits are read once: a workgroup holds its row, or a part of it, in registers; what comes of the
+// parts of a row is joined by a second, small kernel.  Bound by HBM (one read), beside it ten instructions a logit, four of them
+// the exponential's.
+//
+// Alternatives are ordered by one 64-bit key, the logit (as an ordered integer) above the complement of the index, so that equal
+// logits go by ascending index and no two keys are equal.  The k-th largest of 64 groups' maxima is no larger than the k-th
+// largest logit: what is not below it, a few more than k, goes to a list in LDS and is ranked there.  A list that would not fit
+// (many equal logits) is replaced by k searches for the next key.
 #include "kernels.h"
 
 namespace dat {
 namespace {
 
-constexpr float kInf = __builtin_inff();
+constexpr float kInf = __builtin_inff(), kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kTiny = -150.0f;             // 2^-150 is 0 in fp32: stands for all smaller exponents
 
 template <typename T> __device__ __forceinline__ float load1(const T* p);
 template <> __device__ __forceinline__ float load1<float>(const float* p) { return *p; }
@@ -16,31 +23,19 @@ template <> __device__ __forceinline__ float load1<bf16_t>(const bf16_t* p) { re
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f2bf(v); }
 
-// Running softmax statistics.  bad: a NaN or +inf was met.  m = -inf: nothing allowed so far (s = w = 0).
-struct Stats { float m, s, w; uint32_t bad; };
-
-__device__ __forceinline__ Stats merge(const Stats& a, const Stats& b) {
-  const float m = fmaxf(a.m, b.m);
-  // (x - m_new) e^(x-m_new) = ((x - m_old) + d) e^(x-m_old) e^d, d = m_old - m_new; an empty side adds nothing
-  const float da = a.m == m ? 0.0f : a.m - m, db = b.m == m ? 0.0f : b.m - m;
-  const float ea = expf(da), eb = expf(db);
-  const float wa = a.s > 0.0f && ea > 0.0f ? ea * fmaf(da, a.s, a.w) : 0.0f;
-  const float wb = b.s > 0.0f && eb > 0.0f ? eb * fmaf(db, b.s, b.w) : 0.0f;
-  return Stats{m, fmaf(a.s, ea, b.s * eb), wa + wb, a.bad | b.bad};
+__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // a NaN stays
+__device__ __forceinline__ float minus_inf_to_zero(float m) { return m == -kInf ? 0.0f : m; }
+// Adds one logit to the sums for the maximum m (finite).
+__device__ __forceinline__ void add(float x, float m, float& s, float& w) {
+  const float t = fmaxf((x - m) * kLog2e, kTiny), e = __builtin_amdgcn_exp2f(t);
+  s += e;
+  w = fmaf(t, e, w);
 }
-__device__ __forceinline__ void add(Stats& st, float x) {
-  if (!(x < kInf)) { st.bad = 1; return; }
-  if (x == -kInf) return;
-  if (x > st.m) {
-    const float d = st.m - x, e = expf(d);      // d = -inf at the first value: e = 0
-    st.w = e > 0.0f ? e * fmaf(d, st.s, st.w) : 0.0f;
-    st.s = fmaf(st.s, e, 1.0f);
-    st.m = x;
-  } else {
-    const float d = x - st.m, e = expf(d);
-    st.s += e;
-    if (e > 0.0f) st.w = fmaf(d, e, st.w);
-  }
+// The sums of maximum m as sums of maximum M >= m (m = -inf: nothing there).
+__device__ __forceinline__ void rescale(float m, float M, float& s, float& w) {
+  const float d = m == M ? 0.0f : fmaxf((m - M) * kLog2e, kTiny), e = __builtin_amdgcn_exp2f(d);
+  w = e * fmaf(d, s, w);
+  s *= e;
 }
 
 // Ordered key of a logit: larger logit first, then the lower index.  0 is below every allowed logit's key.
@@ -55,74 +50,300 @@ __device__ __forceinline__ float key_value(uint64_t k) {
 }
 __device__ __forceinline__ int32_t key_index(uint64_t k) { return (int32_t)(0xffffffffu - (uint32_t)k); }
 
+struct Part { float m, s, w, pad; };         // of one part of a row
 struct LogProbsArgs {
   const void* x; int64_t N, V, ld; const int32_t* labels; int top;
   float *logp, *entropy, *lse, *top_logp; int32_t* top_index;
+  int parts, part_vectors;                   // parts of a row, 16-byte vectors of a part
+  Part* part; uint64_t* keys;                // [N][parts], [N][parts][top]
 };
 
-template <int WAVES> __device__ Stats block_stats(Stats st, Stats* s_st) {
+template <int L> __device__ __forceinline__ float lanes_max(float v) {
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1)
-    st = merge(st, Stats{__shfl_xor(st.m, d), __shfl_xor(st.s, d), __shfl_xor(st.w, d), (uint32_t)__shfl_xor((int)st.bad, d)});
-  if ((threadIdx.x & 63) == 0) s_st[threadIdx.x >> 6] = st;
-  __syncthreads();
-  st = s_st[0];
-#pragma unroll
-  for (int i = 1; i < WAVES; ++i) st = merge(st, s_st[i]);
-  return st;
+  for (int d = L / 2; d >= 1; d >>= 1) v = maximum(v, __shfl_xor(v, d));
+  return v;
 }
-__device__ __forceinline__ uint64_t wave_max_key(uint64_t k) {
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)k, d); k = o > k ? o : k; }
+  for (int d = L / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+template <int L> __device__ __forceinline__ uint64_t lanes_max(uint64_t k) {
+#pragma unroll
+  for (int d = L / 2; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)k, d); k = o > k ? o : k; }
   return k;
 }
 
-// The row's results, by one thread.
-template <typename T> __device__ void write_stats(const LogProbsArgs& a, int64_t n, const Stats& st) {
-  const bool empty = st.m == -kInf;
-  const float ls = empty ? -kInf : logf(st.s), nan = __builtin_nanf("");
-  if (a.lse) a.lse[n] = st.bad ? nan : empty ? -kInf : st.m + ls;
-  if (a.entropy) a.entropy[n] = st.bad ? nan : empty ? 0.0f : fmaxf(ls - st.w / st.s, 0.0f);
+// The row's results from its maximum and sums, by one thread.  M: NaN or +inf for a row that holds such, -inf for an empty one.
+template <typename T> __device__ void write_stats(const LogProbsArgs& a, int64_t n, float M, float s, float w) {
+  const bool bad = !(M < kInf), empty = M == -kInf;
+  const float ls = logf(s), nan = __builtin_nanf("");
+  if (a.lse) a.lse[n] = bad ? nan : empty ? -kInf : M + ls;
+  if (a.entropy) a.entropy[n] = bad ? nan : empty ? 0.0f : fmaxf(ls - kLn2 * w / s, 0.0f);
   if (a.logp) {
     const int y = a.labels[n];
-    const bool ok = (unsigned)y < (unsigned)a.V && !st.bad;
-    a.logp[n] = !ok ? nan : empty ? -kInf : (load1((const T*)a.x + n * a.ld + y) - st.m) - ls;
+    const bool ok = (unsigned)y < (unsigned)a.V && !bad;
+    a.logp[n] = !ok ? nan : empty ? -kInf : (load1((const T*)a.x + n * a.ld + y) - M) - ls;
   }
 }
-__device__ void write_top(const LogProbsArgs& a, int64_t n, int r, uint64_t key, const Stats& st) {
-  const bool none = key == 0;
-  a.top_index[n * a.top + r] = none || st.bad ? -1 : key_index(key);
-  a.top_logp[n * a.top + r] = st.bad ? __builtin_nanf("") : none ? -kInf : (key_value(key) - st.m) - logf(st.s);
+__device__ __forceinline__ void write_top(const LogProbsArgs& a, int64_t n, int r, uint64_t key, float M, float s) {
+  const bool bad = !(M < kInf), none = key == 0;
+  a.top_index[n * a.top + r] = none || bad ? -1 : key_index(key);
+  a.top_logp[n * a.top + r] = bad ? __builtin_nanf("") : none ? -kInf : (key_value(key) - M) - logf(s);
 }
 
-constexpr int kRowT = 256;
-template <typename T>
-__global__ __launch_bounds__(kRowT) void log_probs_row_kernel(LogProbsArgs a) {
-  __shared__ Stats s_st[kRowT / 64];
-  __shared__ uint64_t s_key[kRowT / 64];
-  const int64_t n = blockIdx.x;
-  const T* x = (const T*)a.x + n * a.ld;
-  Stats st{-kInf, 0.0f, 0.0f, 0};
-  for (int64_t i = threadIdx.x; i < a.V; i += kRowT) add(st, load1(x + i));
-  st = block_stats<kRowT / 64>(st, s_st);
-  if (threadIdx.x == 0) write_stats<T>(a, n, st);
-  uint64_t below = ~0ull;
-  for (int r = 0; r < a.top; ++r) {
-    uint64_t best = 0;
-    for (int64_t i = threadIdx.x; i < a.V; i += kRowT) {
-      const uint64_t k = key_of(load1(x + i), (uint32_t)i);
-      best = k < below && k > best ? k : best;
-    }
-    best = wave_max_key(best);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_key[threadIdx.x >> 6] = best;
-    __syncthreads();
-    best = s_key[0];
+// ---- short rows: L lanes a row, E logits a lane ---------------------------------------------------------------------------
+constexpr int kShortT = 256;
+template <typename T, int L, int E>
+__global__ __launch_bounds__(kShortT) void log_probs_short_kernel(LogProbsArgs a) {
+  const int64_t n = (int64_t)blockIdx.x * (kShortT / L) + threadIdx.x / L;
+  const int lane = threadIdx.x & (L - 1), V = (int)a.V;
+  const bool row = n < a.N;                      // (lanes of a row that is not there take part in the exchanges of their wavefront)
+  const T* x = (const T*)a.x + (row ? n : 0) * a.ld;
+  float v[E], m = -kInf, s = 0.0f, w = 0.0f;
 #pragma unroll
-    for (int i = 1; i < kRowT / 64; ++i) best = s_key[i] > best ? s_key[i] : best;
-    if (threadIdx.x == 0) write_top(a, n, r, best, st);
-    below = best;
+  for (int e = 0; e < E; ++e) { const int i = lane + L * e; v[e] = i < V ? load1(x + i) : -kInf; }
+#pragma unroll
+  for (int e = 0; e < E; ++e) m = maximum(m, v[e]);
+  const float M = lanes_max<L>(m), base = minus_inf_to_zero(M);
+#pragma unroll
+  for (int e = 0; e < E; ++e) add(v[e], base, s, w);
+  s = lanes_sum<L>(s); w = lanes_sum<L>(w);
+  if (row && lane == 0) write_stats<T>(a, n, M, s, w);
+  if (a.top == 0) return;
+  uint64_t best = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) { const uint64_t k = key_of(v[e], lane + L * e); best = k > best ? k : best; }
+  for (int r = 0; r < a.top; ++r) {
+    const uint64_t next = lanes_max<L>(best);
+    if (row && lane == 0) write_top(a, n, r, next, M, s);
+    if (best == next && next) {                  // its owner looks for its own next one
+      best = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) { const uint64_t k = key_of(v[e], lane + L * e); best = k < next && k > best ? k : best; }
+    }
   }
+}
+
+// ---- long rows -----------------------------------------------------------------------------------------------------------
+constexpr int kList = 512;                       // candidates that the list in LDS holds
+template <int NT> struct Selection {             // shared memory of one workgroup
+  float s_v[NT / 64], s_s[NT / 64], s_w[NT / 64];
+  uint64_t s_group[64], s_list[kList], s_wave[NT / 64];
+  int s_count;
+};
+
+// The k-th largest of the groups' maxima, k >= 1, in every thread; NT/64 neighbouring threads are a group.
+template <int NT> __device__ __forceinline__ uint64_t lower_bound_of_top(uint64_t best, int k, Selection<NT>& sh) {
+  constexpr int G = NT / 64;
+#pragma unroll
+  for (int d = G / 2; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)best, d); best = o > best ? o : best; }
+  if (threadIdx.x % G == 0) sh.s_group[threadIdx.x / G] = best;
+  if (threadIdx.x == 0) sh.s_count = 0;
+  __syncthreads();
+  const uint64_t own = sh.s_group[threadIdx.x & 63];
+  int rank = 0;
+  for (int g = 0; g < 64; ++g) {
+    const uint64_t o = sh.s_group[g];
+    rank += o > own || (o == own && g < (int)(threadIdx.x & 63));
+  }
+  const uint64_t mask = __ballot(rank == k - 1);
+  return (uint64_t)__shfl((unsigned long long)own, __ffsll((unsigned long long)mask) - 1);
+}
+template <int NT> __device__ __forceinline__ void append(uint64_t key, Selection<NT>& sh) {
+  const int at = atomicAdd(&sh.s_count, 1);      // (the order of the list does not matter)
+  if (at < kList) sh.s_list[at] = key;
+}
+// done(r, key) for the k largest keys in order, by one thread each.  The list holds every key from the k-th largest up; where it
+// did not fit, next_below(key) finds a thread's largest key below one, k times.
+template <int NT, typename N, typename D>
+__device__ __forceinline__ void select_top(int k, Selection<NT>& sh, N next_below, D done) {
+  __syncthreads();
+  const int count = sh.s_count;
+  if (count <= kList) {
+    for (int i = threadIdx.x; i < count; i += NT) {
+      const uint64_t own = sh.s_list[i];
+      int rank = 0;
+      for (int j = 0; j < count; ++j) rank += sh.s_list[j] > own;
+      if (rank < k) done(rank, own);
+    }
+    for (int r = count + threadIdx.x; r < k; r += NT) done(r, 0);
+    return;
+  }
+  uint64_t below = ~0ull;
+  for (int r = 0; r < k; ++r) {
+    const uint64_t best = lanes_max<64>((uint64_t)next_below(below));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.s_wave[threadIdx.x >> 6] = best;
+    __syncthreads();
+    below = sh.s_wave[0];
+    for (int i = 1; i < NT / 64; ++i) below = sh.s_wave[i] > below ? sh.s_wave[i] : below;
+    if (threadIdx.x == 0) done(r, below);
+  }
+}
+
+// A workgroup's maximum and sums from those of its threads.
+template <int NT> __device__ __forceinline__ void block_stats(float m, float& M, float& s, float& w, Selection<NT>& sh) {
+  M = lanes_max<64>(m);
+  if ((threadIdx.x & 63) == 0) sh.s_v[threadIdx.x >> 6] = M;
+  __syncthreads();
+  M = sh.s_v[0];
+#pragma unroll
+  for (int i = 1; i < NT / 64; ++i) M = maximum(M, sh.s_v[i]);
+  rescale(m, M, s, w);
+  s = lanes_sum<64>(s); w = lanes_sum<64>(w);
+  if ((threadIdx.x & 63) == 0) { sh.s_s[threadIdx.x >> 6] = s; sh.s_w[threadIdx.x >> 6] = w; }
+  __syncthreads();
+  s = sh.s_s[0]; w = sh.s_w[0];
+#pragma unroll
+  for (int i = 1; i < NT / 64; ++i) { s += sh.s_s[i]; w += sh.s_w[i]; }
+}
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <typename T> __device__ __forceinline__ float element(const u32x4& v, int j) {
+  if (sizeof(T) == 4) return __uint_as_float(v[j]);
+  return __uint_as_float(j % 2 ? v[j / 2] & 0xffff0000u : v[j / 2] << 16);
+}
+
+// (Held vectors are unpacked anew in every pass: the compiler would keep the unpacked values, and spill.)
+__device__ __forceinline__ void forget(u32x4& v) { asm volatile("" : "+v"(v)); }
+
+// Rows start at any element: vectors are those of the 16-byte blocks that the row touches, what lies beside the row in the first
+// and the last counts as -inf.  (Such a block holds an element of the row, so all of it can be read.)
+template <typename T, int NT, int VPT, bool WHOLE>
+__global__ __launch_bounds__(NT) void log_probs_long_kernel(LogProbsArgs a) {
+  constexpr int VE = 16 / sizeof(T);
+  __shared__ Selection<NT> sh;
+  const int64_t n = WHOLE ? blockIdx.x : blockIdx.x / (unsigned)a.parts;
+  const int p = WHOLE ? 0 : (int)(blockIdx.x - n * a.parts), V = (int)a.V;
+  const uintptr_t row = reinterpret_cast<uintptr_t>((const T*)a.x + n * a.ld);
+  const int head = (int)(row & 15) / (int)sizeof(T), vectors = (head + V + VE - 1) / VE;
+  const int first = p * a.part_vectors, own = WHOLE ? vectors : max(0, min(a.part_vectors, vectors - first));
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((row & ~(uintptr_t)15) + (uintptr_t)first * 16), 0,
+                                                                     own * 16, 0x00020000);
+  u32x4 v[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(threadIdx.x + i * NT) * 16, 0, 0);
+  const int e0 = (first + (int)threadIdx.x) * VE - head;        // index of the thread's first element in the row
+  float m = -kInf, s = 0.0f, w = 0.0f;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int at = e0 + i * NT * VE;
+    const bool mine = (int)threadIdx.x + i * NT < own;
+    if (!mine || at < 0 || at > V - VE) {
+#pragma unroll
+      for (int j = 0; j < VE; ++j)
+        if (!mine || at + j < 0 || at + j >= V) {
+          if (sizeof(T) == 4) v[i][j] = 0xff800000u;
+          else v[i][j / 2] = j % 2 ? (v[i][j / 2] & 0xffffu) | 0xff800000u : (v[i][j / 2] & 0xffff0000u) | 0xff80u;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < VE; ++j) m = maximum(m, element<T>(v[i], j));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  const float base = minus_inf_to_zero(m);
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    forget(v[i]);
+    float si = 0.0f, wi = 0.0f;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) add(element<T>(v[i], j), base, si, wi);
+    s += si; w += wi;
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  float M;
+  block_stats<NT>(m, M, s, w, sh);
+  if (threadIdx.x == 0) {
+    if (WHOLE) write_stats<T>(a, n, M, s, w);
+    else a.part[n * a.parts + p] = Part{M, s, w, 0.0f};
+  }
+  if (a.top == 0) return;
+  // values only: elements equal to the bound go to the list as well
+  const uint64_t bound = lower_bound_of_top<NT>(key_of(m, 0xffffffffu), a.top, sh);
+  const float least = bound ? key_value(bound) : -kInf;
+  const T* x = reinterpret_cast<const T*>(row);
+  const int lo = max(0, first * VE - head), hi = min(V, (first + own) * VE - head);      // the part's elements
+  if (m >= least && m > -kInf) {
+    uint32_t hits = 0;                           // vectors that reach the bound: one or two, read again element by element
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      forget(v[i]);
+      float top = element<T>(v[i], 0);
+#pragma unroll
+      for (int j = 1; j < VE; ++j) top = fmaxf(top, element<T>(v[i], j));
+      hits |= top >= least ? 1u << i : 0u;
+    }
+    for (; hits; hits &= hits - 1) {
+      const int at = e0 + (__ffs(hits) - 1) * NT * VE;
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        const float f = at + j >= lo && at + j < hi ? load1(x + at + j) : -kInf;
+        if (f >= least && f > -kInf) append<NT>(key_of(f, at + j), sh);
+      }
+    }
+  }
+  select_top<NT>(a.top, sh,
+    [&](uint64_t below) {
+      uint64_t best = 0;
+      for (int i = lo + (int)threadIdx.x; i < hi; i += NT) { const uint64_t k = key_of(load1(x + i), i); best = k < below && k > best ? k : best; }
+      return best;
+    },
+    [&](int k, uint64_t key) {
+      if (WHOLE) write_top(a, n, k, key, M, s);
+      else a.keys[(n * a.parts + p) * a.top + k] = key;
+    });
+}
+
+// Joins the parts of a row.
+constexpr int kJoinT = 256;
+template <typename T>
+__global__ __launch_bounds__(kJoinT) void log_probs_join_kernel(LogProbsArgs a) {
+  __shared__ Selection<kJoinT> sh;
+  const int64_t n = blockIdx.x;
+  const Part* part = a.part + n * a.parts;
+  float m = -kInf, M, s = 0.0f, w = 0.0f;
+  for (int p = threadIdx.x; p < a.parts; p += kJoinT) m = maximum(m, part[p].m);
+  for (int p = threadIdx.x; p < a.parts; p += kJoinT) {
+    float ps = part[p].s, pw = part[p].w;
+    rescale(part[p].m, m, ps, pw);
+    s += ps; w += pw;
+  }
+  block_stats<kJoinT>(m, M, s, w, sh);
+  if (threadIdx.x == 0) write_stats<T>(a, n, M, s, w);
+  if (a.top == 0) return;
+  const uint64_t* keys = a.keys + n * a.parts * a.top;
+  const int count = a.parts * a.top;
+  uint64_t best = 0;
+  for (int i = threadIdx.x; i < count; i += kJoinT) best = keys[i] > best ? keys[i] : best;
+  const uint64_t bound = lower_bound_of_top<kJoinT>(best, a.top, sh);
+  for (int i = threadIdx.x; i < count; i += kJoinT) if (keys[i] && keys[i] >= bound) append<kJoinT>(keys[i], sh);
+  select_top<kJoinT>(a.top, sh,
+    [&](uint64_t below) {
+      uint64_t k = 0;
+      for (int i = threadIdx.x; i < count; i += kJoinT) k = keys[i] < below && keys[i] > k ? keys[i] : k;
+      return k;
+    },
+    [&](int k, uint64_t key) { write_top(a, n, k, key, M, s); });
+}
+
+// Which kernel: short rows; one workgroup a row; or parts, where a row is longer than 1024 threads hold or where there would be
+// few workgroups of many logits.
+struct LogProbsPlan { int lanes, nt, vpt, parts, part_vectors; };
+LogProbsPlan log_probs_plan(int width, int64_t N, int64_t V) {
+  if (V <= 64) return {16, 0, 0, 1, 0};
+  if (V <= 1024) return {64, 0, 0, 1, 0};
+  static const int sizes[][2] = {{256, 1}, {256, 4}, {256, 16}, {512, 16}, {1024, 16}};
+  const int64_t vectors = V * width / 16 + 2;            // at most, with the row's start anywhere
+  int64_t parts = (vectors + 1024 * 16 - 1) / (1024 * 16);
+  if (N * parts < 128 && vectors > 4096) {
+    const int64_t want = (256 + N - 1) / N, most = vectors / 512;
+    if (parts < want) parts = want < most ? want : most;
+  }
+  const int64_t each = (vectors + parts - 1) / parts;
+  int i = 0;
+  while (sizes[i][0] * sizes[i][1] < each) ++i;
+  return {0, sizes[i][0], sizes[i][1], (int)parts, (int)each};
 }
 
 struct LogProbsGradArgs {
@@ -141,20 +362,55 @@ __device__ __forceinline__ RowGrad row_grad(const LogProbsGradArgs& g, int64_t n
   if (r.lse == -kInf) { r.a = r.b = r.H = 0.0f; r.lse = kInf; r.y = -1; }     // nothing allowed: p = 0 everywhere
   return r;
 }
-__device__ __forceinline__ float grad1(float x, int64_t i, const RowGrad& r) {
-  const float q = x - r.lse, p = expf(q);
+__device__ __forceinline__ float grad1(float x, int i, const RowGrad& r) {
+  const float q = x - r.lse, p = __builtin_amdgcn_exp2f(maximum(q * kLog2e, kTiny));   // (NaN where lse is)
   const float d = r.a * ((i == r.y ? 1.0f : 0.0f) - p);
   return p == 0.0f ? d : fmaf(-r.b * p, q + r.H, d);
 }
 
-constexpr int kGradT = 256;
+// Streaming, bound by HBM (one read, one write).  A thread takes vectors of 16 bytes from the row's start, at any alignment: global
+// memory takes them whole.
+constexpr int kGradT = 256, kGradV = 4;      // vectors a thread
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Vector { T x[16 / sizeof(T)]; };
 template <typename T>
-__global__ __launch_bounds__(kGradT) void log_probs_grad_kernel(LogProbsGradArgs g) {
-  const int64_t n = blockIdx.x;
+__global__ __launch_bounds__(kGradT) void log_probs_grad_kernel(LogProbsGradArgs g, unsigned blocks) {
+  constexpr int VE = 16 / sizeof(T);
+  const int64_t n = blockIdx.x / blocks;
+  const int V = (int)g.V, first = (int)(blockIdx.x - n * blocks) * (kGradT * kGradV * VE) + (int)threadIdx.x * VE;
   const RowGrad r = row_grad(g, n);
   const T* x = (const T*)g.x + n * g.ld;
   T* dx = (T*)g.dx + n * g.ldd;
-  for (int64_t i = threadIdx.x; i < g.V; i += kGradT) store1(dx + i, grad1(load1(x + i), i, r));
+  Vector<T> v[kGradV];
+#pragma unroll
+  for (int k = 0; k < kGradV; ++k) {
+    const int i = first + k * kGradT * VE;
+    if (i + VE <= V) v[k] = *reinterpret_cast<const Vector<T>*>(x + i);
+  }
+#pragma unroll
+  for (int k = 0; k < kGradV; ++k) {
+    const int i = first + k * kGradT * VE;
+    if (i + VE <= V) {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) store1(&v[k].x[j], grad1(load1(&v[k].x[j]), i + j, r));
+      *reinterpret_cast<Vector<T>*>(dx + i) = v[k];
+    } else {
+      for (int j = i; j < V; ++j) store1(dx + j, grad1(load1(x + j), j, r));
+    }
+  }
+}
+
+template <typename T> void launch_log_probs(const LogProbsPlan& p, const LogProbsArgs& a, hipStream_t st) {
+  const unsigned rows = (unsigned)a.N;
+  if (p.lanes == 16) { hipLaunchKernelGGL((log_probs_short_kernel<T, 16, 4>), dim3((rows + 15) / 16), dim3(kShortT), 0, st, a); return; }
+  if (p.lanes == 64) { hipLaunchKernelGGL((log_probs_short_kernel<T, 64, 16>), dim3((rows + 3) / 4), dim3(kShortT), 0, st, a); return; }
+#define DAT_LP_SIZE(NT, VPT)                                                                                                        \
+  if (p.nt == NT && p.vpt == VPT) {                                                                                                 \
+    if (p.parts == 1) hipLaunchKernelGGL((log_probs_long_kernel<T, NT, VPT, true>), dim3(rows), dim3(NT), 0, st, a);                \
+    else hipLaunchKernelGGL((log_probs_long_kernel<T, NT, VPT, false>), dim3(rows * (unsigned)p.parts), dim3(NT), 0, st, a);        \
+  }
+  DAT_LP_SIZE(256, 1) DAT_LP_SIZE(256, 4) DAT_LP_SIZE(256, 16) DAT_LP_SIZE(512, 16) DAT_LP_SIZE(1024, 16)
+#undef DAT_LP_SIZE
+  if (p.parts > 1) hipLaunchKernelGGL(log_probs_join_kernel<T>, dim3(rows), dim3(kJoinT), 0, st, a);
 }
 
 }  // namespace
@@ -162,7 +418,18 @@ __global__ __launch_bounds__(kGradT) void log_probs_grad_kernel(LogProbsGradArgs
 
 using namespace dat;
 
-extern "C" size_t dat_log_probs_workspace(int64_t, int64_t, int) { return 0; }
+namespace {
+size_t workspace_of(const LogProbsPlan& p, int64_t N, int top) {
+  return p.parts > 1 ? (size_t)N * p.parts * (sizeof(Part) + sizeof(uint64_t) * (size_t)top) : 0;
+}
+}  // namespace
+
+// (The larger of the types' needs.)
+extern "C" size_t dat_log_probs_workspace(int64_t N, int64_t V, int top) {
+  if (N < 1 || V < 1 || V > (1ll << 30) || N > INT32_MAX || top < 0 || top > DAT_MAX_TOP) return 0;
+  const size_t a = workspace_of(log_probs_plan(2, N, V), N, top), b = workspace_of(log_probs_plan(4, N, V), N, top);
+  return a > b ? a : b;
+}
 
 namespace {
 dat_status check_rows(const void* x, dat_dtype dtype, int64_t N, int64_t V, int64_t ld) {
@@ -184,10 +451,12 @@ extern "C" dat_status dat_log_probs(const void* logits, dat_dtype dtype, int64_t
   if (!aligned(labels, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(lse, 4) || !aligned(top_logp, 4) || !aligned(top_index, 4)) return DAT_ERR_ARG;
   const size_t need = dat_log_probs_workspace(N, V, top);
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return DAT_ERR_ARG;
-  LogProbsArgs a{logits, N, V, ld, labels, top, logp, entropy, lse, top_logp, top_index};
+  const LogProbsPlan p = log_probs_plan(dtype == DAT_BF16 ? 2 : 4, N, V);
+  LogProbsArgs a{logits, N, V, ld, labels, top, logp, entropy, lse, top_logp, top_index, p.parts, p.part_vectors, (Part*)workspace, nullptr};
+  if (p.parts > 1) a.keys = reinterpret_cast<uint64_t*>(a.part + N * p.parts);
+  if (N * p.parts > INT32_MAX) return DAT_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == DAT_BF16) hipLaunchKernelGGL(log_probs_row_kernel<bf16_t>, dim3((unsigned)N), dim3(kRowT), 0, st, a);
-  else hipLaunchKernelGGL(log_probs_row_kernel<float>, dim3((unsigned)N), dim3(kRowT), 0, st, a);
+  if (dtype == DAT_BF16) launch_log_probs<bf16_t>(p, a, st); else launch_log_probs<float>(p, a, st);
   DAT_LAUNCH_CHECK();
   return DAT_OK;
 }
@@ -203,8 +472,10 @@ extern "C" dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype
   if (!aligned(labels, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4)) return DAT_ERR_ARG;
   LogProbsGradArgs g{logits, N, V, ld, ldd, labels, lse, entropy, dlogp, dentropy, dlogits};
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == DAT_BF16) hipLaunchKernelGGL(log_probs_grad_kernel<bf16_t>, dim3((unsigned)N), dim3(kGradT), 0, st, g);
-  else hipLaunchKernelGGL(log_probs_grad_kernel<float>, dim3((unsigned)N), dim3(kGradT), 0, st, g);
+  const int64_t per = kGradT * kGradV * 16 / (dtype == DAT_BF16 ? 2 : 4), blocks = (V + per - 1) / per;
+  if (N * blocks > INT32_MAX) return DAT_ERR_SHAPE;
+  if (dtype == DAT_BF16) hipLaunchKernelGGL(log_probs_grad_kernel<bf16_t>, dim3((unsigned)(N * blocks)), dim3(kGradT), 0, st, g, (unsigned)blocks);
+  else hipLaunchKernelGGL(log_probs_grad_kernel<float>, dim3((unsigned)(N * blocks)), dim3(kGradT), 0, st, g, (unsigned)blocks);
   DAT_LAUNCH_CHECK();
   return DAT_OK;
 }
