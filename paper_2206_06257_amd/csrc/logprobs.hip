@@ -58,19 +58,30 @@ struct LogProbsArgs {
   Part* part; uint64_t* keys;                // [N][parts], [N][parts][top]
 };
 
-template <int L> __device__ __forceinline__ float lanes_max(float v) {
-#pragma unroll
-  for (int d = L / 2; d >= 1; d >>= 1) v = maximum(v, __shfl_xor(v, d));
+// Reductions over L = 16 or 64 neighbouring lanes by DPP (a vector instruction a step, no LDS); every lane has the result.
+template <int CTRL, int ROWS> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, ROWS, 0xf, false); }
+template <int L, typename F> __device__ __forceinline__ int lanes_reduce(int v, F f) {
+  v = f(v, dpp<0xb1, 0xf>(v));                   // the other of two, of two pairs, of half a row, of a row of 16
+  v = f(v, dpp<0x4e, 0xf>(v));
+  v = f(v, dpp<0x141, 0xf>(v));
+  v = f(v, dpp<0x140, 0xf>(v));
+  if (L == 64) {
+    const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47),
+              d = __builtin_amdgcn_readlane(v, 63);
+    v = f(f(a, b), f(c, d));
+  }
   return v;
+}
+template <int L> __device__ __forceinline__ float lanes_max(float v) {
+  return __int_as_float(lanes_reduce<L>(__float_as_int(v), [](int a, int b) { return __float_as_int(maximum(__int_as_float(a), __int_as_float(b))); }));
 }
 template <int L> __device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int d = L / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+  return __int_as_float(lanes_reduce<L>(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
 }
-template <int L> __device__ __forceinline__ uint64_t lanes_max(uint64_t k) {
+template <int L> __device__ __forceinline__ int lanes_min(int v) { return lanes_reduce<L>(v, [](int a, int b) { return min(a, b); }); }
+__device__ __forceinline__ uint64_t wave_max(uint64_t k) {
 #pragma unroll
-  for (int d = L / 2; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)k, d); k = o > k ? o : k; }
+  for (int d = 32; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)k, d); k = o > k ? o : k; }
   return k;
 }
 
@@ -93,7 +104,7 @@ __device__ __forceinline__ void write_top(const LogProbsArgs& a, int64_t n, int 
 }
 
 // ---- short rows: L lanes a row, E logits a lane ---------------------------------------------------------------------------
-constexpr int kShortT = 256;
+constexpr int kShortT = 64;
 template <typename T, int L, int E>
 __global__ __launch_bounds__(kShortT) void log_probs_short_kernel(LogProbsArgs a) {
   const int64_t n = (int64_t)blockIdx.x * (kShortT / L) + threadIdx.x / L;
@@ -111,17 +122,21 @@ __global__ __launch_bounds__(kShortT) void log_probs_short_kernel(LogProbsArgs a
   s = lanes_sum<L>(s); w = lanes_sum<L>(w);
   if (row && lane == 0) write_stats<T>(a, n, M, s, w);
   if (a.top == 0) return;
-  uint64_t best = 0;
+  // a lane offers its largest logit that is not taken; among equal ones the lowest index goes first
+  uint32_t taken = 0;
+  float best;
+  int at;
+  auto offer = [&]() {
+    best = -kInf; at = 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e) { const uint64_t k = key_of(v[e], lane + L * e); best = k > best ? k : best; }
+    for (int e = 0; e < E; ++e) if (v[e] > best && !(taken >> e & 1)) { best = v[e]; at = e; }
+  };
+  offer();
   for (int r = 0; r < a.top; ++r) {
-    const uint64_t next = lanes_max<L>(best);
-    if (row && lane == 0) write_top(a, n, r, next, M, s);
-    if (best == next && next) {                  // its owner looks for its own next one
-      best = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) { const uint64_t k = key_of(v[e], lane + L * e); best = k < next && k > best ? k : best; }
-    }
+    const float top = lanes_max<L>(best);
+    const int own = lane + L * at, index = lanes_min<L>(best == top ? own : 0x7fffffff);
+    if (row && lane == 0) write_top(a, n, r, top > -kInf ? key_of(top, index) : 0, M, s);
+    if (best == top && own == index) { taken |= 1u << at; offer(); }
   }
 }
 
@@ -129,26 +144,31 @@ __global__ __launch_bounds__(kShortT) void log_probs_short_kernel(LogProbsArgs a
 constexpr int kList = 512;                       // candidates that the list in LDS holds
 template <int NT> struct Selection {             // shared memory of one workgroup
   float s_v[NT / 64], s_s[NT / 64], s_w[NT / 64];
-  uint64_t s_group[64], s_list[kList], s_wave[NT / 64];
+  float s_group[64], s_bound;
+  uint64_t s_list[kList], s_wave[NT / 64];
   int s_count;
 };
 
-// The k-th largest of the groups' maxima, k >= 1, in every thread; NT/64 neighbouring threads are a group.
-template <int NT> __device__ __forceinline__ uint64_t lower_bound_of_top(uint64_t best, int k, Selection<NT>& sh) {
+// The k-th largest of the maxima of 64 groups of threads (or less), k >= 1, in every thread; -inf where fewer hold anything.
+template <int NT> __device__ __forceinline__ float lower_bound_of_top(float best, int k, Selection<NT>& sh) {
   constexpr int G = NT / 64;
-#pragma unroll
-  for (int d = G / 2; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)best, d); best = o > best ? o : best; }
+  if (G >= 2) best = fmaxf(best, __int_as_float(dpp<0xb1, 0xf>(__float_as_int(best))));
+  if (G >= 4) best = fmaxf(best, __int_as_float(dpp<0x4e, 0xf>(__float_as_int(best))));
+  if (G >= 8) best = fmaxf(best, __int_as_float(dpp<0x141, 0xf>(__float_as_int(best))));
+  if (G >= 16) best = fmaxf(best, __int_as_float(dpp<0x140, 0xf>(__float_as_int(best))));
   if (threadIdx.x % G == 0) sh.s_group[threadIdx.x / G] = best;
   if (threadIdx.x == 0) sh.s_count = 0;
   __syncthreads();
-  const uint64_t own = sh.s_group[threadIdx.x & 63];
-  int rank = 0;
-  for (int g = 0; g < 64; ++g) {
-    const uint64_t o = sh.s_group[g];
-    rank += o > own || (o == own && g < (int)(threadIdx.x & 63));
+  if (threadIdx.x < 64) {                        // (by one wavefront: the others' turn on the vector units is another workgroup's)
+    const float own = sh.s_group[threadIdx.x];
+    int above = 0;
+#pragma unroll
+    for (int g = 0; g < 64; ++g) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(own), g)) > own;
+    const float bound = -lanes_max<64>(above < k ? -own : -kInf);
+    if (threadIdx.x == 0) sh.s_bound = bound;
   }
-  const uint64_t mask = __ballot(rank == k - 1);
-  return (uint64_t)__shfl((unsigned long long)own, __ffsll((unsigned long long)mask) - 1);
+  __syncthreads();
+  return sh.s_bound;
 }
 template <int NT> __device__ __forceinline__ void append(uint64_t key, Selection<NT>& sh) {
   const int at = atomicAdd(&sh.s_count, 1);      // (the order of the list does not matter)
@@ -172,7 +192,7 @@ __device__ __forceinline__ void select_top(int k, Selection<NT>& sh, N next_belo
   }
   uint64_t below = ~0ull;
   for (int r = 0; r < k; ++r) {
-    const uint64_t best = lanes_max<64>((uint64_t)next_below(below));
+    const uint64_t best = wave_max(next_below(below));
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh.s_wave[threadIdx.x >> 6] = best;
     __syncthreads();
@@ -229,14 +249,16 @@ __global__ __launch_bounds__(NT) void log_probs_long_kernel(LogProbsArgs a) {
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int at = e0 + i * NT * VE;
-    const bool mine = (int)threadIdx.x + i * NT < own;
-    if (!mine || at < 0 || at > V - VE) {
+    // elements from..to of the vector belong to the row and the part
+    int from = max(-at, 0), to = (int)threadIdx.x + i * NT < own ? min(V - at, VE) : 0;
+    asm volatile("" : "+v"(from), "+v"(to));     // (the compiler would follow the conditions from vector to vector)
+    if (from > 0 || to < VE) {
 #pragma unroll
-      for (int j = 0; j < VE; ++j)
-        if (!mine || at + j < 0 || at + j >= V) {
-          if (sizeof(T) == 4) v[i][j] = 0xff800000u;
-          else v[i][j / 2] = j % 2 ? (v[i][j / 2] & 0xffffu) | 0xff800000u : (v[i][j / 2] & 0xffff0000u) | 0xff80u;
-        }
+      for (int j = 0; j < VE; ++j) {
+        const uint32_t gone = j < from || j >= to ? 0xffffffffu : 0u;
+        if (sizeof(T) == 4) v[i][j] = (v[i][j] & ~gone) | (gone & 0xff800000u);
+        else { const uint32_t half = gone & (j % 2 ? 0xffff0000u : 0xffffu); v[i][j / 2] = (v[i][j / 2] & ~half) | (half & 0xff80ff80u); }
+      }
     }
 #pragma unroll
     for (int j = 0; j < VE; ++j) m = maximum(m, element<T>(v[i], j));
@@ -260,8 +282,7 @@ __global__ __launch_bounds__(NT) void log_probs_long_kernel(LogProbsArgs a) {
   }
   if (a.top == 0) return;
   // values only: elements equal to the bound go to the list as well
-  const uint64_t bound = lower_bound_of_top<NT>(key_of(m, 0xffffffffu), a.top, sh);
-  const float least = bound ? key_value(bound) : -kInf;
+  const float least = lower_bound_of_top<NT>(m, a.top, sh);
   const T* x = reinterpret_cast<const T*>(row);
   const int lo = max(0, first * VE - head), hi = min(V, (first + own) * VE - head);      // the part's elements
   if (m >= least && m > -kInf) {
@@ -274,6 +295,7 @@ __global__ __launch_bounds__(NT) void log_probs_long_kernel(LogProbsArgs a) {
       for (int j = 1; j < VE; ++j) top = fmaxf(top, element<T>(v[i], j));
       hits |= top >= least ? 1u << i : 0u;
     }
+#pragma nounroll
     for (; hits; hits &= hits - 1) {
       const int at = e0 + (__ffs(hits) - 1) * NT * VE;
 #pragma unroll
@@ -316,8 +338,8 @@ __global__ __launch_bounds__(kJoinT) void log_probs_join_kernel(LogProbsArgs a) 
   const int count = a.parts * a.top;
   uint64_t best = 0;
   for (int i = threadIdx.x; i < count; i += kJoinT) best = keys[i] > best ? keys[i] : best;
-  const uint64_t bound = lower_bound_of_top<kJoinT>(best, a.top, sh);
-  for (int i = threadIdx.x; i < count; i += kJoinT) if (keys[i] && keys[i] >= bound) append<kJoinT>(keys[i], sh);
+  const float least = lower_bound_of_top<kJoinT>(best ? key_value(best) : -kInf, a.top, sh);
+  for (int i = threadIdx.x; i < count; i += kJoinT) if (keys[i] && key_value(keys[i]) >= least) append<kJoinT>(keys[i], sh);
   select_top<kJoinT>(a.top, sh,
     [&](uint64_t below) {
       uint64_t k = 0;
@@ -333,11 +355,11 @@ struct LogProbsPlan { int lanes, nt, vpt, parts, part_vectors; };
 LogProbsPlan log_probs_plan(int width, int64_t N, int64_t V) {
   if (V <= 64) return {16, 0, 0, 1, 0};
   if (V <= 1024) return {64, 0, 0, 1, 0};
-  static const int sizes[][2] = {{256, 1}, {256, 4}, {256, 16}, {512, 16}, {1024, 16}};
+  static const int sizes[][2] = {{256, 1}, {256, 4}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
   const int64_t vectors = V * width / 16 + 2;            // at most, with the row's start anywhere
   int64_t parts = (vectors + 1024 * 16 - 1) / (1024 * 16);
   if (N * parts < 128 && vectors > 4096) {
-    const int64_t want = (256 + N - 1) / N, most = vectors / 512;
+    const int64_t want = (256 + N - 1) / N, most = (vectors + 255) / 256;
     if (parts < want) parts = want < most ? want : most;
   }
   const int64_t each = (vectors + parts - 1) / parts;
@@ -401,14 +423,14 @@ __global__ __launch_bounds__(kGradT) void log_probs_grad_kernel(LogProbsGradArgs
 
 template <typename T> void launch_log_probs(const LogProbsPlan& p, const LogProbsArgs& a, hipStream_t st) {
   const unsigned rows = (unsigned)a.N;
-  if (p.lanes == 16) { hipLaunchKernelGGL((log_probs_short_kernel<T, 16, 4>), dim3((rows + 15) / 16), dim3(kShortT), 0, st, a); return; }
-  if (p.lanes == 64) { hipLaunchKernelGGL((log_probs_short_kernel<T, 64, 16>), dim3((rows + 3) / 4), dim3(kShortT), 0, st, a); return; }
+  if (p.lanes == 16) { hipLaunchKernelGGL((log_probs_short_kernel<T, 16, 4>), dim3((rows + 3) / 4), dim3(kShortT), 0, st, a); return; }
+  if (p.lanes == 64) { hipLaunchKernelGGL((log_probs_short_kernel<T, 64, 16>), dim3(rows), dim3(kShortT), 0, st, a); return; }
 #define DAT_LP_SIZE(NT, VPT)                                                                                                        \
   if (p.nt == NT && p.vpt == VPT) {                                                                                                 \
     if (p.parts == 1) hipLaunchKernelGGL((log_probs_long_kernel<T, NT, VPT, true>), dim3(rows), dim3(NT), 0, st, a);                \
     else hipLaunchKernelGGL((log_probs_long_kernel<T, NT, VPT, false>), dim3(rows * (unsigned)p.parts), dim3(NT), 0, st, a);        \
   }
-  DAT_LP_SIZE(256, 1) DAT_LP_SIZE(256, 4) DAT_LP_SIZE(256, 16) DAT_LP_SIZE(512, 16) DAT_LP_SIZE(1024, 16)
+  DAT_LP_SIZE(256, 1) DAT_LP_SIZE(256, 4) DAT_LP_SIZE(256, 8) DAT_LP_SIZE(512, 8) DAT_LP_SIZE(1024, 8) DAT_LP_SIZE(1024, 16)
 #undef DAT_LP_SIZE
   if (p.parts > 1) hipLaunchKernelGGL(log_probs_join_kernel<T>, dim3(rows), dim3(kJoinT), 0, st, a);
 }
