@@ -1,6 +1,7 @@
 """ctypes binding of libdat.so with the same names as include/dat.h (without the dat_ prefix on
 methods of Model).  Raises if the library has not been built: there is no fallback path."""
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -410,37 +411,52 @@ def aggregate(q_list, scales_list, offsets_dev, d, bits, out=None, stream=None):
     return out
 
 
-class _On:
-    """Runs a call on the tensors' device, on `stream` or on that device's current stream; what the call allocates belongs to it."""
+# (the stream's handle without making a Stream object of it, where torch offers that)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
-    def __init__(self, stream, *tensors):
-        device = tensors[0].device
-        for t in tensors:
-            if t is not None and (not t.is_cuda or t.device != device):
-                raise ValueError("all tensors of a call belong on one GPU: %s and %s" % (device, t.device))
-        if stream is not None and stream.device != device:
-            raise ValueError("the stream belongs to %s, the tensors are on %s" % (stream.device, device))
-        self._device, self._ctx = torch.cuda.device(device), None if stream is None else torch.cuda.stream(stream)
+
+class _On:
+    """Runs a call on the tensors' device, on `stream` or on that device's current stream; what the call allocates belongs to it.
+    (The usual call, on the current device and stream, enters no context: those cost as much as a small kernel.)"""
+
+    def __init__(self, stream, first, *others):
+        self._device = device = first.get_device()
+        self._stream, self._within = stream, ()
+        for t in others:
+            if t is not None and t.get_device() != device:
+                raise ValueError("all tensors of a call belong on one GPU: %s and %s" % (first.device, t.device))
+        if device < 0:
+            raise ValueError("the tensors of a call belong on a GPU, not on %s" % (first.device,))
+        if stream is not None and stream.device != first.device:
+            raise ValueError("the stream belongs to %s, the tensors are on %s" % (stream.device, first.device))
 
     def __enter__(self):
-        self._device.__enter__()
-        if self._ctx is not None:
-            self._ctx.__enter__()
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        if self._stream is not None:
+            self._within = (torch.cuda.stream(self._stream),)           # (changes the device as well)
+        elif self._device != torch.cuda.current_device():
+            self._within = (torch.cuda.device(self._device),)
+        else:
+            return _raw_stream(self._device)
+        for c in self._within:
+            c.__enter__()
+        return torch.cuda.current_stream().cuda_stream
 
     def __exit__(self, *exc):
-        if self._ctx is not None:
-            self._ctx.__exit__(*exc)
-        self._device.__exit__(*exc)
+        for c in self._within:
+            c.__exit__(*exc)
 
 
 def _want(name, t, dtypes, shape=None, contiguous=True, optional=False):
     """Checks a tensor argument of the calls below."""
     if t is None and optional:
         return
-    if t.dtype not in dtypes or (shape is not None and tuple(t.shape) != tuple(shape)) or (contiguous and not t.is_contiguous()):
+    if t.dtype not in dtypes or (shape is not None and t.shape != shape) or (contiguous and not t.is_contiguous()):
         raise ValueError("%s: %s %s%s, expected %s %s" % (name, t.dtype, tuple(t.shape), "" if t.is_contiguous() else " (not contiguous)",
                                                           " or ".join(str(d) for d in dtypes), "" if shape is None else tuple(shape)))
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
@@ -464,15 +480,15 @@ def adamw_state(d, num_tensors, bits=32, device="cuda"):
             torch.zeros(adamw_slots(d, num_tensors), 2, dtype=torch.int16, device=device))
 
 
-def _adamw_table(offsets_dev, d, num_tensors, m, v, scales):
+def _adamw_table(offsets_dev, d, m, v, scales):
     """(pointer, tensors) of a table, and the checks of the moments."""
     _want("m", m, (torch.float32, torch.uint8), (d,))
     _want("v", v, (m.dtype,), (d,))
     if isinstance(offsets_dev, tuple):
-        ptr, T = C.c_void_p(offsets_dev[0]), offsets_dev[1]
+        ptr, T = offsets_dev[0], offsets_dev[1]
     else:
         _want("offsets_dev", offsets_dev, (torch.int64,))
-        ptr, T = _ptr(offsets_dev), offsets_dev.numel() - 1
+        ptr, T = _at(offsets_dev), offsets_dev.numel() - 1
     if m.dtype == torch.uint8:
         if scales is None:
             raise ValueError("8-bit moments need their scales")
@@ -488,22 +504,22 @@ def adamw_update(theta, grads, m, v, offsets_dev, lr, t, scales=None, seed=0, be
     _want("theta", theta, (torch.float32,), (d,))
     _want("grads", grads, _FLOATS, (d,))
     _want("theta_bf16", theta_bf16, (torch.bfloat16,), (d,), optional=True)
-    ptr, T = _adamw_table(offsets_dev, d, None, m, v, scales)
+    ptr, T = _adamw_table(offsets_dev, d, m, v, scales)
     _want("decay", decay, (torch.float32,), (T,), optional=True)
     with _On(stream, theta, grads, m, v, scales, decay, theta_bf16, None if isinstance(offsets_dev, tuple) else offsets_dev) as st:
-        _check(_lib.dat_adamw_update(_ptr(theta), _ptr(grads), _code(grads), ptr, T, d, 8 if m.dtype == torch.uint8 else 32, _ptr(m), _ptr(v),
-                                     _ptr(scales), int(seed) & 0xFFFFFFFFFFFFFFFF, lr, beta1, beta2, eps, weight_decay, _ptr(decay),
-                                     int(t), _ptr(theta_bf16), st), "dat_adamw_update")
+        _check(_lib.dat_adamw_update(_at(theta), _at(grads), _code(grads), ptr, T, d, 8 if m.dtype == torch.uint8 else 32, _at(m), _at(v),
+                                     _at(scales), int(seed) & 0xFFFFFFFFFFFFFFFF, lr, beta1, beta2, eps, weight_decay, _at(decay),
+                                     int(t), _at(theta_bf16), st), "dat_adamw_update")
 
 
 def adamw_moments(m, v, scales, offsets_dev, stream=None):
     """The fp32 values that 8-bit moments stand for."""
     _want("m", m, (torch.uint8,))
     d = m.numel()
-    ptr, T = _adamw_table(offsets_dev, d, None, m, v, scales)
+    ptr, T = _adamw_table(offsets_dev, d, m, v, scales)
     with _On(stream, m, v, scales, None if isinstance(offsets_dev, tuple) else offsets_dev) as st:
         m_out, v_out = torch.empty(d, device=m.device), torch.empty(d, device=m.device)
-        _check(_lib.dat_adamw_moments(_ptr(m), _ptr(v), _ptr(scales), ptr, T, d, _ptr(m_out), _ptr(v_out), st), "dat_adamw_moments")
+        _check(_lib.dat_adamw_moments(_at(m), _at(v), _at(scales), ptr, T, d, _at(m_out), _at(v_out), st), "dat_adamw_moments")
     return m_out, v_out
 
 
@@ -525,13 +541,15 @@ def log_probs(logits, labels=None, top=0, stream=None):
     N, V = logits.shape
     _want("labels", labels, (torch.int32,), (N,), optional=True)
     with _On(stream, logits, labels) as st:
-        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=logits.device)  # noqa: E731
-        logp, entropy, lse = None if labels is None else new(N), new(N), new(N)
-        top_logp, top_index = (new(N, top), new(N, top, dtype=torch.int32)) if top > 0 else (None, None)
+        device = logits.device
+        lse = torch.empty(N, device=device)
+        entropy, logp = torch.empty_like(lse), None if labels is None else torch.empty_like(lse)
+        top_logp = torch.empty(N, top, device=device) if top > 0 else None
+        top_index = torch.empty(N, top, dtype=torch.int32, device=device) if top > 0 else None
         size = int(_lib.dat_log_probs_workspace(N, V, top))
-        ws = new(size, dtype=torch.uint8) if size else None
-        _check(_lib.dat_log_probs(_ptr(logits), _code(logits), N, V, ld, _ptr(labels), top, _ptr(logp), _ptr(entropy), _ptr(lse),
-                                  _ptr(top_logp), _ptr(top_index), _ptr(ws), size, st), "dat_log_probs")
+        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+        _check(_lib.dat_log_probs(_at(logits), _code(logits), N, V, ld, _at(labels), top, _at(logp), _at(entropy), _at(lse),
+                                  _at(top_logp), _at(top_index), _at(ws), size, st), "dat_log_probs")
     return logp, entropy, lse, top_logp, top_index
 
 
@@ -550,15 +568,19 @@ def log_probs_backward(logits, labels, lse, entropy=None, dlogp=None, dentropy=N
             dlogits = torch.empty(N, V, dtype=logits.dtype, device=logits.device)
         ldd = _rows("dlogits", dlogits, (N, V))
         _want("dlogits", dlogits, (logits.dtype,), contiguous=False)
-        _check(_lib.dat_log_probs_backward(_ptr(logits), _code(logits), N, V, ld, None if dlogp is None else _ptr(labels), _ptr(lse),
-                                           None if dentropy is None else _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), ldd, st),
+        _check(_lib.dat_log_probs_backward(_at(logits), _code(logits), N, V, ld, None if dlogp is None else _at(labels), _at(lse),
+                                           None if dentropy is None else _at(entropy), _at(dlogp), _at(dentropy), _at(dlogits), ldd, st),
                "dat_log_probs_backward")
     return dlogits
 
 
+@functools.lru_cache(maxsize=4096)
+def _gn_workspace_bytes(pass_, dtype, B, H, W, channels, groups):
+    return int(_lib.dat_group_norm_workspace(pass_, dtype, B, H, W, channels, groups))
+
+
 def _gn_workspace(pass_, x, groups):
-    B, H, W, Cc = x.shape
-    size = int(_lib.dat_group_norm_workspace(pass_, _code(x), B, H, W, Cc, groups))
+    size = _gn_workspace_bytes(pass_, _code(x), *x.shape, groups)
     return (torch.empty(size, dtype=torch.uint8, device=x.device) if size else None), size
 
 
@@ -574,10 +596,11 @@ def group_norm_forward(x, gamma, beta, groups, act=ACT_NONE, eps=1e-5, y=None, s
     with _On(stream, x, gamma, beta, y) as st:
         if y is None:
             y = torch.empty_like(x)
-        mean, rstd = (torch.empty(B, max(groups, 0), device=x.device) for _ in range(2))
+        mean = torch.empty(B, max(groups, 0), device=x.device)
+        rstd = torch.empty_like(mean)
         ws, size = _gn_workspace(0, x, groups)
-        _check(_lib.dat_group_norm_forward(_ptr(x), _ptr(gamma), _ptr(beta), _code(x), B, H, W, Cc, groups, eps, act, _ptr(y), _ptr(mean),
-                                           _ptr(rstd), _ptr(ws), size, st), "dat_group_norm_forward")
+        _check(_lib.dat_group_norm_forward(_at(x), _at(gamma), _at(beta), _code(x), B, H, W, Cc, groups, eps, act, _at(y), _at(mean),
+                                           _at(rstd), _at(ws), size, st), "dat_group_norm_forward")
     return y, mean, rstd
 
 
@@ -599,8 +622,8 @@ def group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, act=ACT_NONE, dx
         dgamma = torch.empty(Cc, device=x.device) if dgamma is None else dgamma
         dbeta = torch.empty(Cc, device=x.device) if dbeta is None else dbeta
         ws, size = _gn_workspace(1, x, groups)
-        _check(_lib.dat_group_norm_backward(_ptr(x), _ptr(dy), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd), _code(x), B, H, W, Cc, groups,
-                                            act, _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), size, st), "dat_group_norm_backward")
+        _check(_lib.dat_group_norm_backward(_at(x), _at(dy), _at(gamma), _at(beta), _at(mean), _at(rstd), _code(x), B, H, W, Cc, groups,
+                                            act, _at(dx), _at(dgamma), _at(dbeta), _at(ws), size, st), "dat_group_norm_backward")
     return dx, dgamma, dbeta
 
 

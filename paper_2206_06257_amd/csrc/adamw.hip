@@ -6,6 +6,7 @@
 #include "kernels.h"
 #include "tensor_table.h"
 #include "philox.h"
+#include "lanes.h"
 
 namespace dat {
 namespace {
@@ -27,23 +28,30 @@ struct __attribute__((packed, aligned(4))) Float4U { float x[4]; };
 struct __attribute__((packed, aligned(2))) Half4U { bf16_t x[4]; };
 struct __attribute__((packed, aligned(1))) Byte4U { uint8_t x[4]; };
 
-template <typename V, typename E> __device__ __forceinline__ V load4(const E* p, int count) {
-  V v;
-  if (count >= 4) return *reinterpret_cast<const V*>(p);
+template <typename V, typename E> __device__ __forceinline__ void load4(const E* p, int count, E (&x)[4]) {
+  if (count >= 4) {
+    const V v = *reinterpret_cast<const V*>(p);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v.x[i] = i < count ? p[i] : E(0);
-  return v;
+    for (int i = 0; i < 4; ++i) x[i] = v.x[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i < count ? p[i] : E(0);
+  }
 }
-template <typename V, typename E> __device__ __forceinline__ void store4(E* p, const V& v, int count) {
-  if (count >= 4) { *reinterpret_cast<V*>(p) = v; return; }
+template <typename V, typename E> __device__ __forceinline__ void store4(E* p, const E (&x)[4], int count) {
+  if (count >= 4) {
+    V v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) if (i < count) p[i] = v.x[i];
+    for (int i = 0; i < 4; ++i) v.x[i] = x[i];
+    *reinterpret_cast<V*>(p) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < count) p[i] = x[i];
+  }
 }
 
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, s));
-  return x;
+  return (uint32_t)lanes_reduce<64>((int)x, [](int a, int b) { return (int)max((uint32_t)a, (uint32_t)b); });
 }
 
 // s of a block: one above T(largest), so that rounding up stays in range; -1 where a value is not finite.
@@ -81,6 +89,60 @@ __device__ __forceinline__ int tensor_of_slot(const int64_t* off, int T, int64_t
   return lo;
 }
 
+// One block; WHOLE: all of its 256 elements are there, so that no load stands behind a branch, where the next would wait for it.
+template <int BITS, bool WHOLE, typename G, typename GV>
+__device__ __forceinline__ void adamw_block(const AdamwArgs& a, int slot, int t, int64_t e0, int64_t left, int lane) {
+  const int64_t e = e0 + 4 * lane;
+  const int count = WHOLE ? 4 : (int)max((int64_t)0, min((int64_t)4, left - 4 * lane));
+  const AdamwParams& hp = a.hp;
+  const float wd = a.decay ? __fmul_rn(hp.wd, a.decay[t]) : hp.wd;
+  float th[4], m[4], v[4];
+  G g4[4];
+  load4<Float4U>(a.theta + e, count, th);
+  load4<GV>((const G*)a.g + e, count, g4);
+  if constexpr (BITS == 8) {
+    const int sm = a.scales[2 * (int64_t)slot], sv = a.scales[2 * (int64_t)slot + 1];
+    uint8_t cm[4], cv[4];
+    load4<Byte4U>((const uint8_t*)a.m + e, count, cm);
+    load4<Byte4U>((const uint8_t*)a.v + e, count, cv);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { m[i] = i < count ? decode_m(cm[i], sm) : 0.0f; v[i] = i < count ? decode_v(cv[i], sv) : 0.0f; }
+  } else {
+    load4<Float4U>((const float*)a.m + e, count, m);
+    load4<Float4U>((const float*)a.v + e, count, v);
+  }
+  bf16_t half[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float g;
+    if constexpr (sizeof(G) == 2) g = bf2f(g4[i]); else g = g4[i];
+    m[i] = __fadd_rn(__fmul_rn(hp.b1, m[i]), __fmul_rn(hp.om1, g));
+    v[i] = __fadd_rn(__fmul_rn(hp.b2, v[i]), __fmul_rn(hp.om2, __fmul_rn(g, g)));
+    const float u = __fdiv_rn(__fmul_rn(m[i], hp.c1), __fadd_rn(sqrtf(__fmul_rn(v[i], hp.c2)), hp.eps));
+    th[i] = __fsub_rn(th[i], __fmul_rn(hp.lr, __fadd_rn(u, __fmul_rn(wd, th[i]))));
+    half[i] = f2bf(th[i]);
+  }
+  store4<Float4U>(a.theta + e, th, count);
+  if (a.copy) store4<Half4U>(a.copy + e, half, count);
+  if constexpr (BITS == 8) {
+    uint32_t bm = 0, bv = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (i < count) { bm = max(bm, abs_bits(m[i])); bv = max(bv, abs_bits(v[i])); }
+    const int sm = block_scale(wave_max(bm)), sv = block_scale(wave_max(bv));
+    const PhiloxWords w = philox_block((uint64_t)slot * 64 + lane, a.seed, kRandomStream);
+    const uint32_t word[4] = {w.w0, w.w1, w.w2, w.w3};
+    uint8_t cm[4], cv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { cm[i] = encode_m(m[i], word[i] & 0xffffu, sm); cv[i] = encode_v(v[i], word[i] >> 16, sv); }
+    store4<Byte4U>((uint8_t*)a.m + e, cm, count);
+    store4<Byte4U>((uint8_t*)a.v + e, cv, count);
+    if (lane == 0) { a.scales[2 * (int64_t)slot] = (int16_t)sm; a.scales[2 * (int64_t)slot + 1] = (int16_t)sv; }
+  } else {
+    store4<Float4U>((float*)a.m + e, m, count);
+    store4<Float4U>((float*)a.v + e, v, count);
+  }
+}
+
 template <int BITS, typename G, typename GV>
 __global__ __launch_bounds__(kT) void adamw_kernel(AdamwArgs a) {
   const int lane = threadIdx.x & 63;
@@ -89,55 +151,24 @@ __global__ __launch_bounds__(kT) void adamw_kernel(AdamwArgs a) {
   const int t = tensor_of_slot(a.off, a.T, slot);
   const int64_t e0 = a.off[t] + (slot - first_slot(a.off, t)) * kBlock;
   const int64_t left = a.off[t + 1] - e0;
-  if (left <= 0) return;
+  if (left >= kBlock) adamw_block<BITS, true, G, GV>(a, slot, t, e0, left, lane);
+  else if (left > 0) adamw_block<BITS, false, G, GV>(a, slot, t, e0, left, lane);
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void moments_block(const uint8_t* m, const uint8_t* v, const int16_t* scales, int slot, int64_t e0, int64_t left,
+                                              int lane, float* m_out, float* v_out) {
   const int64_t e = e0 + 4 * lane;
-  const int count = (int)max((int64_t)0, min((int64_t)4, left - 4 * lane));
-  const AdamwParams& hp = a.hp;
-  const float wd = a.decay ? __fmul_rn(hp.wd, a.decay[t]) : hp.wd;
-  Float4U th = load4<Float4U>(a.theta + e, count);
-  const GV g4 = load4<GV>((const G*)a.g + e, count);
-  Float4U m4, v4;
-  if constexpr (BITS == 8) {
-    const int sm = a.scales[2 * (int64_t)slot], sv = a.scales[2 * (int64_t)slot + 1];
-    const Byte4U cm = load4<Byte4U>((const uint8_t*)a.m + e, count), cv = load4<Byte4U>((const uint8_t*)a.v + e, count);
+  const int count = WHOLE ? 4 : (int)max((int64_t)0, min((int64_t)4, left - 4 * lane));
+  const int sm = scales[2 * (int64_t)slot], sv = scales[2 * (int64_t)slot + 1];
+  uint8_t cm[4], cv[4];
+  float fm[4], fv[4];
+  load4<Byte4U>(m + e, count, cm);
+  load4<Byte4U>(v + e, count, cv);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { m4.x[i] = i < count ? decode_m(cm.x[i], sm) : 0.0f; v4.x[i] = i < count ? decode_v(cv.x[i], sv) : 0.0f; }
-  } else {
-    m4 = load4<Float4U>((const float*)a.m + e, count);
-    v4 = load4<Float4U>((const float*)a.v + e, count);
-  }
-  Half4U half;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float g;
-    if constexpr (sizeof(G) == 2) g = bf2f(g4.x[i]); else g = g4.x[i];
-    const float m = __fadd_rn(__fmul_rn(hp.b1, m4.x[i]), __fmul_rn(hp.om1, g));
-    const float v = __fadd_rn(__fmul_rn(hp.b2, v4.x[i]), __fmul_rn(hp.om2, __fmul_rn(g, g)));
-    const float u = __fdiv_rn(__fmul_rn(m, hp.c1), __fadd_rn(sqrtf(__fmul_rn(v, hp.c2)), hp.eps));
-    const float x = th.x[i];
-    th.x[i] = __fsub_rn(x, __fmul_rn(hp.lr, __fadd_rn(u, __fmul_rn(wd, x))));
-    half.x[i] = f2bf(th.x[i]);
-    m4.x[i] = m; v4.x[i] = v;
-  }
-  store4(a.theta + e, th, count);
-  if (a.copy) store4(a.copy + e, half, count);
-  if constexpr (BITS == 8) {
-    uint32_t bm = 0, bv = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) if (i < count) { bm = max(bm, abs_bits(m4.x[i])); bv = max(bv, abs_bits(v4.x[i])); }
-    const int sm = block_scale(wave_max(bm)), sv = block_scale(wave_max(bv));
-    const PhiloxWords w = philox_block((uint64_t)slot * 64 + lane, a.seed, kRandomStream);
-    const uint32_t word[4] = {w.w0, w.w1, w.w2, w.w3};
-    Byte4U cm, cv;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { cm.x[i] = encode_m(m4.x[i], word[i] & 0xffffu, sm); cv.x[i] = encode_v(v4.x[i], word[i] >> 16, sv); }
-    store4((uint8_t*)a.m + e, cm, count);
-    store4((uint8_t*)a.v + e, cv, count);
-    if (lane == 0) { a.scales[2 * (int64_t)slot] = (int16_t)sm; a.scales[2 * (int64_t)slot + 1] = (int16_t)sv; }
-  } else {
-    store4((float*)a.m + e, m4, count);
-    store4((float*)a.v + e, v4, count);
-  }
+  for (int i = 0; i < 4; ++i) { fm[i] = decode_m(cm[i], sm); fv[i] = decode_v(cv[i], sv); }
+  store4<Float4U>(m_out + e, fm, count);
+  store4<Float4U>(v_out + e, fv, count);
 }
 
 __global__ __launch_bounds__(kT) void adamw_moments_kernel(const uint8_t* __restrict__ m, const uint8_t* __restrict__ v,
@@ -149,16 +180,8 @@ __global__ __launch_bounds__(kT) void adamw_moments_kernel(const uint8_t* __rest
   const int t = tensor_of_slot(off, T, slot);
   const int64_t e0 = off[t] + (slot - first_slot(off, t)) * kBlock;
   const int64_t left = off[t + 1] - e0;
-  if (left <= 0) return;
-  const int64_t e = e0 + 4 * lane;
-  const int count = (int)max((int64_t)0, min((int64_t)4, left - 4 * lane));
-  const int sm = scales[2 * (int64_t)slot], sv = scales[2 * (int64_t)slot + 1];
-  const Byte4U cm = load4<Byte4U>(m + e, count), cv = load4<Byte4U>(v + e, count);
-  Float4U fm, fv;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { fm.x[i] = decode_m(cm.x[i], sm); fv.x[i] = decode_v(cv.x[i], sv); }
-  store4(m_out + e, fm, count);
-  store4(v_out + e, fv, count);
+  if (left >= kBlock) moments_block<true>(m, v, scales, slot, e0, left, lane, m_out, v_out);
+  else if (left > 0) moments_block<false>(m, v, scales, slot, e0, left, lane, m_out, v_out);
 }
 
 inline unsigned blocks_for(int64_t slots) { return (unsigned)((slots + kWaves - 1) / kWaves); }
