@@ -12,6 +12,7 @@
 //             pass read last.
 #include <type_traits>
 #include "kernels.h"
+#include "lanes.h"
 
 namespace dat {
 namespace {
@@ -501,26 +502,10 @@ template <typename T, int VE, bool BACK> struct Range {   // BACK: images from t
   }
 };
 
-// Sums of VE values over the threads of a vector; result in the threads with ty = 0.  Lanes of a wavefront that share a vector
-// are joined in registers first.
-template <int M, int VE> __device__ __forceinline__ void range_sums(float (&v)[M][VE], int sv, int rows, int tx, int ty, float* s_red) {
-  const int left = lay_columns<kT, M, VE>(v, sv, rows, s_red);
-  if (ty == 0) {
-#pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        float s = 0.0f;
-        for (int r = 0; r < left; ++r) s += s_red[(m * kT + r * sv + tx) * VE + j];
-        v[m][j] = s;
-      }
-  }
-}
-
 // Every channel's mean and sum of squared deviations within the range: part[(b, chunk)][0..1][c].
 template <typename T, int VE>
 __global__ __launch_bounds__(kT) void gn_stats_kernel(GnArgs a) {
-  __shared__ float s_red[VE * kT], s_mean[VE * kT];
+  __shared__ float s_red[VE * kT], s_mean[VE * 32];      // (a slice has at most 32 vectors)
   const Range<T, VE, false> r(a);
   const typename Range<T, VE, false>::V* x = reinterpret_cast<const typename Range<T, VE, false>::V*>(a.x) + r.base;
   typename Range<T, VE, false>::V v[kHeld];
@@ -536,16 +521,15 @@ __global__ __launch_bounds__(kT) void gn_stats_kernel(GnArgs a) {
 #pragma unroll
       for (int j = 0; j < VE; ++j) acc[0][j] += f[j];
     }
-  range_sums<1, VE>(acc, r.sv, r.rows, r.tx, r.ty, s_red);
   const float n = (float)(r.p1 - r.chunk * a.chunk);
-  if (r.ty == 0) {
-#pragma unroll
-    for (int j = 0; j < VE; ++j) { acc[0][j] = __fdiv_rn(acc[0][j], n); s_mean[j * kT + r.tx] = acc[0][j]; }
-  }
+  const int w = r.sv * VE;
+  float* part = a.part + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + (r.c - r.tx * VE);
+  int rows = lay_columns<kT, 1, VE>(acc, r.sv, r.rows, s_red);
+  sum_columns<kT, 1>(s_red, 0, w, rows, 1, w, [&](int c, const float (&sum)[1]) { s_mean[c] = part[c] = __fdiv_rn(sum[0], n); });
   __syncthreads();
   float mean[VE];
 #pragma unroll
-  for (int j = 0; j < VE; ++j) { mean[j] = s_mean[j * kT + r.tx]; acc[0][j] = 0.0f; }
+  for (int j = 0; j < VE; ++j) { mean[j] = s_mean[r.tx * VE + j]; acc[0][j] = 0.0f; }
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
     if (r.p0 + i * r.rows < r.p1) {
@@ -553,37 +537,50 @@ __global__ __launch_bounds__(kT) void gn_stats_kernel(GnArgs a) {
 #pragma unroll
       for (int j = 0; j < VE; ++j) { const float d = f[j] - mean[j]; acc[0][j] = fmaf(d, d, acc[0][j]); }
     }
-  range_sums<1, VE>(acc, r.sv, r.rows, r.tx, r.ty, s_red);
-  if (r.ty == 0) {
-    float* part = a.part + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + r.c;
-#pragma unroll
-    for (int j = 0; j < VE; ++j) { part[j] = mean[j]; part[a.C + j] = acc[0][j]; }
-  }
+  rows = lay_columns<kT, 1, VE>(acc, r.sv, r.rows, s_red);
+  sum_columns<kT, 1>(s_red, 0, w, rows, 1, w, [&](int c, const float (&sum)[1]) { part[a.C + c] = sum[0]; });
 }
 
-// One wavefront per image and group: means and squared deviations of its ranges and channels into one, by the deviations of the
-// means from their own mean.
-__global__ __launch_bounds__(64) void gn_join_stats_kernel(GnArgs a) {
-  const int b = blockIdx.x / a.G, g = blockIdx.x - b * a.G, entries = a.chunks * a.Cg;
+// The joining kernels: one workgroup per image and group.  Threads lie along the group's channels, as many as it has up to kT (in
+// powers of two), and what is left of them along the ranges.
+struct JoinLanes {
+  int width, rows, c, k;
+  __device__ __forceinline__ explicit JoinLanes(int Cg) {
+    width = 1;
+    while (width < Cg && width < kT) width <<= 1;
+    rows = kT / width; c = threadIdx.x & (width - 1); k = threadIdx.x / width;
+  }
+};
+__device__ __forceinline__ float block_sum(float v, float* s) {
+  v = lanes_sum<64>(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// Means and squared deviations of a group's ranges and channels into one, by the deviations of the means from their own mean.
+__global__ __launch_bounds__(kT) void gn_join_stats_kernel(GnArgs a) {
+  __shared__ float s_sum[kT / 64];
+  const int b = blockIdx.x / a.G, g = blockIdx.x - b * a.G;
   const float* part = a.part + (int64_t)b * a.chunks * 2 * a.C + g * a.Cg;
+  const JoinLanes l(a.Cg);
   const float n = (float)a.P * (float)a.Cg;
   float s = 0.0f;
-  for (int e = threadIdx.x; e < entries; e += 64) {
-    const int k = e / a.Cg, c = e - k * a.Cg;
-    s = fmaf((float)(min(a.P, (k + 1) * a.chunk) - k * a.chunk), part[(int64_t)k * 2 * a.C + c], s);
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d);
-  const float mean = __fdiv_rn(s, n);
+  for (int c = l.c; c < a.Cg; c += l.width)
+#pragma unroll 4
+    for (int k = l.k; k < a.chunks; k += l.rows)
+      s = fmaf((float)(min(a.P, (k + 1) * a.chunk) - k * a.chunk), part[(int64_t)k * 2 * a.C + c], s);
+  const float mean = __fdiv_rn(block_sum(s, s_sum), n);
   s = 0.0f;
-  for (int e = threadIdx.x; e < entries; e += 64) {
-    const int k = e / a.Cg, c = e - k * a.Cg;
-    const float* q = part + (int64_t)k * 2 * a.C + c;
-    const float d = q[0] - mean;
-    s += fmaf((float)(min(a.P, (k + 1) * a.chunk) - k * a.chunk) * d, d, q[a.C]);
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d);
+  for (int c = l.c; c < a.Cg; c += l.width)
+#pragma unroll 4
+    for (int k = l.k; k < a.chunks; k += l.rows) {
+      const float* q = part + (int64_t)k * 2 * a.C + c;
+      const float d = q[0] - mean;
+      s += fmaf((float)(min(a.P, (k + 1) * a.chunk) - k * a.chunk) * d, d, q[a.C]);
+    }
+  s = block_sum(s, s_sum);
   if (threadIdx.x == 0) {
     a.mean[(int64_t)b * a.G + g] = mean;
     a.rstd[(int64_t)b * a.G + g] = rstd_of(s, n, a.eps);
@@ -641,39 +638,41 @@ __global__ __launch_bounds__(kT) void gn_grad_sums_kernel(GnArgs a, float* range
   }
 #pragma unroll
   for (int j = 0; j < VE; ++j) s[1][j] *= rstd[j];
-  range_sums<2, VE>(s, r.sv, r.rows, r.tx, r.ty, s_red);
-  if (r.ty == 0) {
-    float* out = ranges + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + r.c;
-#pragma unroll
-    for (int j = 0; j < VE; ++j) { out[j] = s[0][j]; out[a.C + j] = s[1][j]; }
-  }
+  float* out = ranges + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + (r.c - r.tx * VE);
+  const int cols = r.sv * VE, rows = lay_columns<kT, 2, VE>(s, r.sv, r.rows, s_red);
+  sum_columns<kT, 2>(s_red, kT * VE, cols, rows, 1, cols, [&](int c, const float (&sum)[2]) { out[c] = sum[0]; out[a.C + c] = sum[1]; });
 }
 
-// One workgroup per image and group: sums over the ranges, for every channel to part[0][b][c] and [1][b][c] (as the resident
-// kernel leaves them) and for the group, as means, to join[(b, g)][0..1].  A wavefront takes channels, its lanes the ranges.
+// Sums over the ranges: of every channel to part[0][b][c] and [1][b][c] (as the resident kernel leaves them), and of the group, as
+// means, to join[(b, g)][0..1].
 __global__ __launch_bounds__(kT) void gn_join_grad_kernel(GnArgs a, const float* ranges, float* join) {
-  __shared__ float s[2][kT / 64];
-  const int b = blockIdx.x / a.G, g = blockIdx.x % a.G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float s_sum[kT / 64], s_row[2][kT];
+  const int b = blockIdx.x / a.G, g = blockIdx.x - b * a.G;
   const float* q = ranges + (int64_t)b * a.chunks * 2 * a.C + g * a.Cg;
+  const JoinLanes l(a.Cg);
   float c1 = 0.0f, c2 = 0.0f;
-  for (int c = wave; c < a.Cg; c += kT / 64) {
+  for (int c0 = 0; c0 < a.Cg; c0 += l.width) {
+    const int c = c0 + l.c;
     float s1 = 0.0f, s2 = 0.0f;
-    for (int k = lane; k < a.chunks; k += 64) { s1 += q[(int64_t)k * 2 * a.C + c]; s2 += q[(int64_t)k * 2 * a.C + a.C + c]; }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) { s1 += __shfl_xor(s1, d); s2 += __shfl_xor(s2, d); }
-    if (lane == 0) {
+    if (c < a.Cg) {
+#pragma unroll 4
+      for (int k = l.k; k < a.chunks; k += l.rows) { s1 += q[(int64_t)k * 2 * a.C + c]; s2 += q[(int64_t)k * 2 * a.C + a.C + c]; }
+    }
+    s_row[0][threadIdx.x] = s1; s_row[1][threadIdx.x] = s2;
+    __syncthreads();
+    if (l.k == 0 && c < a.Cg) {
+      for (int r = 1; r < l.rows; ++r) { s1 += s_row[0][r * l.width + l.c]; s2 += s_row[1][r * l.width + l.c]; }
       float* part = a.part + (int64_t)b * a.C + g * a.Cg + c;
       part[0] = s1; part[(int64_t)a.B * a.C] = s2;
+      const float gamma = a.gamma ? a.gamma[g * a.Cg + c] : 1.0f;
+      c1 = fmaf(gamma, s1, c1); c2 = fmaf(gamma, s2, c2);
     }
-    const float gamma = a.gamma ? a.gamma[g * a.Cg + c] : 1.0f;
-    c1 = fmaf(gamma, s1, c1); c2 = fmaf(gamma, s2, c2);
+    __syncthreads();
   }
-  if (lane == 0) { s[0][wave] = c1; s[1][wave] = c2; }
-  __syncthreads();
-  if (threadIdx.x < 2) {
-    const float* v = s[threadIdx.x];
-    join[((int64_t)b * a.G + g) * 2 + threadIdx.x] = ((v[0] + v[1]) + (v[2] + v[3])) / ((float)a.P * (float)a.Cg);
-  }
+  const float n = (float)a.P * (float)a.Cg;
+  c1 = block_sum(c1, s_sum) / n;
+  c2 = block_sum(c2, s_sum) / n;
+  if (threadIdx.x == 0) { join[((int64_t)b * a.G + g) * 2] = c1; join[((int64_t)b * a.G + g) * 2 + 1] = c2; }
 }
 
 template <typename T, int VE, int ACT>
@@ -816,7 +815,7 @@ template <typename T> void launch_resident(bool backward, const Plan& p, const G
 template <typename T, int VE> void launch_forward_split(const GnArgs& a, dat_act act, hipStream_t st) {
   const dim3 grid((unsigned)((int64_t)a.B * a.chunks * a.slices));
   hipLaunchKernelGGL((gn_stats_kernel<T, VE>), grid, dim3(kT), 0, st, a);
-  hipLaunchKernelGGL(gn_join_stats_kernel, dim3((unsigned)((int64_t)a.B * a.G)), dim3(64), 0, st, a);
+  hipLaunchKernelGGL(gn_join_stats_kernel, dim3((unsigned)((int64_t)a.B * a.G)), dim3(kT), 0, st, a);
   DAT_GN_ACT(act, hipLaunchKernelGGL((gn_apply_kernel<T, VE, ACT>), grid, dim3(kT), 0, st, a));
 }
 template <typename T, int VE> void launch_backward_split(const GnArgs& a, dat_act act, float* join, float* ranges, hipStream_t st) {

@@ -18,4 +18,13 @@ template <int L, typename F> __device__ __forceinline__ int lanes_reduce(int v, 
   }
   return v;
 }
+__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // a NaN stays
+template <int L> __device__ __forceinline__ float lanes_max(float v) {
+  return __int_as_float(lanes_reduce<L>(__float_as_int(v), [](int a, int b) { return __float_as_int(maximum(__int_as_float(a), __int_as_float(b))); }));
+}
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+  return __int_as_float(lanes_reduce<L>(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
+template <int L> __device__ __forceinline__ int lanes_min(int v) { return lanes_reduce<L>(v, [](int a, int b) { return min(a, b); }); }
+
 }  // namespace dat

@@ -24,7 +24,6 @@ template <> __device__ __forceinline__ float load1<bf16_t>(const bf16_t* p) { re
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = f2bf(v); }
 
-__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }   // a NaN stays
 __device__ __forceinline__ float minus_inf_to_zero(float m) { return m == -kInf ? 0.0f : m; }
 // Adds one logit to the sums for the maximum m (finite).
 __device__ __forceinline__ void add(float x, float m, float& s, float& w) {
@@ -59,13 +58,6 @@ struct LogProbsArgs {
   Part* part; uint64_t* keys;                // [N][parts], [N][parts][top]
 };
 
-template <int L> __device__ __forceinline__ float lanes_max(float v) {
-  return __int_as_float(lanes_reduce<L>(__float_as_int(v), [](int a, int b) { return __float_as_int(maximum(__int_as_float(a), __int_as_float(b))); }));
-}
-template <int L> __device__ __forceinline__ float lanes_sum(float v) {
-  return __int_as_float(lanes_reduce<L>(__float_as_int(v), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
-}
-template <int L> __device__ __forceinline__ int lanes_min(int v) { return lanes_reduce<L>(v, [](int a, int b) { return min(a, b); }); }
 __device__ __forceinline__ uint64_t wave_max(uint64_t k) {
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) { const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)k, d); k = o > k ? o : k; }
