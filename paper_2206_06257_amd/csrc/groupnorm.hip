@@ -739,19 +739,21 @@ Plan plan_of(bool backward, dat_dtype dtype, bool vectors, int B, int P, int C, 
   p.nv = C / p.ve;
   if (p.ve > 1) {
     const int unit = Cg / gcd(Cg, whole);              // vectors of the smallest slice of whole groups
-    // Tiles of up to 16 vectors a thread (backward: 8 of x and 8 of dy), in the smallest workgroup that takes rows of 64 bytes:
-    // several of them on a compute unit, each at its own stage.  Wider rows where the image is small; narrower ones where there
-    // would be fewer tiles than compute units want.
+    // Tiles of up to 16 vectors a thread (backward: 8 of x and 8 of dy), in the smallest workgroup that takes them: several on a
+    // compute unit, each at its own stage.  Rows of a slice: 128 bytes forward (512 x 32 x 32 x 64 bf16 28.6 us against 35.6 with
+    // 64, 128 x 32 x 32 x 160 fp32 48.6 against 60.5, 256 x 40 x 40 x 256 101.3 against 101.1), 64 where the image does not fit
+    // so, and backward, where the workgroup that takes 128 is alone on its unit (256 x 28 x 28 x 512 146 us against 189).  Wider
+    // where the image is small (256 x 7 x 7 x 2048 41 -> 23 us), narrower where there would be few tiles for 256 compute units.
     static const int fwd[][2] = {{256, 2}, {256, 8}, {256, 16}, {512, 16}, {1024, 16}}, bwd[][2] = {{256, 2}, {256, 8}, {512, 8}, {1024, 8}};
     const int (*sizes)[2] = backward ? bwd : fwd;
     const int count = backward ? 4 : 5, nv = p.nv;
     auto fits = [&](int sv, int i) { return sv <= sizes[i][0] && (P + sizes[i][0] / sv - 1) / (sizes[i][0] / sv) <= sizes[i][1]; };
     int sv = unit, i = 0;
     while (sv * 16 < 64 && 2 * sv <= nv) sv *= 2;
+    if (!backward && sv * 16 < 128 && 2 * sv <= nv && fits(2 * sv, count - 1)) sv *= 2;
     const int least = sv;
     while (2 * sv <= nv && fits(2 * sv, backward ? 1 : 2) && (int64_t)B * (nv / (2 * sv)) >= 1024) sv *= 2;
     if (sv == least) while (sv > unit && (int64_t)B * ((nv + sv - 1) / sv) < 512) sv /= 2;
-    if (sv < unit) sv = unit;
     while (i < count && !fits(sv, i)) ++i;
     if (i < count && sv <= kMaxSlice && sv * whole / Cg <= kMaxSliceGroups && (int64_t)P * C * width < kOob) {
       p.sv = sv; p.nt = sizes[i][0]; p.vpt = sizes[i][1];
