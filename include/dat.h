@@ -256,7 +256,7 @@ dat_status dat_lamb_update(dat_model* m, const float* grads, int use_adam, float
  *   (with 32 bits in that element alone), and so do the parameters it updates.
  * All pointers need the alignment of their elements only.  t, lr and seed are launch arguments: a captured graph repeats them.
  * Asynchronous on `stream`, no allocation.  DAT_ERR_ARG: null pointers, state_bits not 8 or 32, t < 1, b1 or b2 outside [0,1),
- * lr, eps or weight_decay negative or NaN, more than 2^31-1 slots.  d = 0: nothing happens.
+ * lr, eps or weight_decay negative or NaN, more than 2^31-1 slots.  d = 0: nothing happens.  (eps = 0 divides by zero where v is.)
  * dat_adamw_moments: the values that 8-bit moments stand for, device fp32 [d] each (a checkpoint, a change to 32 bits).
  * dat_model_adamw_update: the same step on a model's master parameters; conv and linear weights decay, biases, scales and shifts
  *   do not.  The moments live in the model (allocated on the first call, zero; `state_bits` is fixed from then on:
@@ -272,7 +272,8 @@ dat_status dat_model_adamw_update(dat_model* m, const float* grads, int state_bi
                                   float beta2, float eps, float weight_decay, int t, void* stream);
 
 /* ---- log probabilities of given labels ---------------------------------------------------------------
- * Rows of logits, device fp32 or bf16 [N][V], row n at logits + n*ld elements (ld >= V), any alignment of the rows:
+ * Rows of logits, device fp32 or bf16 [N][V], row n at logits + n*ld elements (ld >= V), any alignment of the rows (they are read in
+ * whole 16-byte blocks: those that hold an element of the row, no others):
  *   lse[n] = log sum_i exp(x_i);  logp[n] = x_y - lse, y = labels[n];  entropy[n] = -sum_i p_i log p_i, p = exp(x - lse);
  *   top_index[n][0..top-1] (int32), top_logp[n][0..top-1]: the `top` largest logits in descending order, equal ones by ascending
  *   index, and their log probabilities.
@@ -302,10 +303,12 @@ dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype, int64_t N
  * x, y, dy, dx: device, fp32 or bf16 by `dtype`, [B,H,W,C]; groups of C/groups consecutive channels, each normalised over the
  * H*W*C/groups values of one image (no sample enters another's result):
  *   xhat = (x - mean) rstd,  rstd = 1/sqrt(var + eps) (biased variance),  z = xhat gamma + beta,  y = act(z);
- *   act: none, ReLU max(z, 0), SiLU z/(1 + exp(-z)).  One fp32 rounding per operation as written; y is rounded once to `dtype`.
- * gamma, beta: device fp32 [C], both NULL for 1 and 0.  mean, rstd: device fp32 [B][groups], written by the forward call (from
- * deviations from the mean, not from a difference of squares) and read by the backward call.
- *   dat_group_norm_backward:  dz = dy act'(z), ReLU'(z) = [z > 0] with z evaluated as in the forward call (no sign differs);
+ *   act: none, ReLU max(z, 0), SiLU z/(1 + exp(-z)).  In fp32; y is rounded once to `dtype`.
+ * gamma, beta: device fp32 [C], both NULL for 1 and 0.  mean, rstd: device fp32 [B][groups], written by the forward call and read by the
+ * backward call.  The variance is that of deviations from the mean (bf16: the difference E x^2 - mean^2, from exact squares, where
+ * mean^2 <= 4 var).  A NaN or an infinity in x spoils its own image's group (mean, rstd, y, dx) and what sums over it.
+ *   dat_group_norm_backward:  dz = dy act'(z), ReLU'(z) = [z > 0], z = ((x - mean) rstd) gamma + beta with one fp32 rounding per
+ *   operation (the forward call may have rounded a z next to zero to the other side);
  *   dbeta = sum dz, dgamma = sum dz xhat (device fp32 [C], both NULL to skip; written, not added to), sums in fp32 in a fixed order
  *   (the same bits on every call);  dx = rstd (h - mean(h) - xhat mean(h xhat)), h = gamma dz, means over the group.  y is not needed.
  * dx may be dy (same buffer), y may be x.  workspace: device, 16-byte aligned, dat_group_norm_workspace(pass, ...) bytes (pass 0 forward, 1
