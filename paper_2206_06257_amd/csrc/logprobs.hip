@@ -2,8 +2,10 @@
 //
 // With M = max x, s = sum 2^t and w = sum t 2^t, t = (x - M) log2 e:  lse = M + ln s,  logp_y = (x_y - M) - ln s,
 // H = ln s - ln 2 w / s.  The logits are read once: a workgroup holds its row, or a part of it, in registers; what comes of the
-// parts of a row is joined by a second, small kernel.  Bound by HBM (one read), beside it ten instructions a logit, four of them
-// the exponential's.
+// parts of a row is joined by a second, small kernel.  Bound by HBM (one read), beside it about twelve instructions a logit, four
+// of them the exponential's: 2039 x 50021 bf16 with eight alternatives 57 us = 3.6 TB/s (two workgroups of 1024 threads on a
+// compute unit; 64 us with two of 512 that hold twice as much).  Few long rows are latency: 3 x 131075 with 20 alternatives 12.6 us
+// in two launches.
 //
 // Alternatives are ordered by one 64-bit key, the logit (as an ordered integer) above the complement of the index, so that equal
 // logits go by ascending index and no two keys are equal.  The k-th largest of 64 groups' maxima is no larger than the k-th
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(kJoinT) void log_probs_join_kernel(LogProbsArgs a) 
     [&](int k, uint64_t key) { write_top(a, n, k, key, M, s); });
 }
 
-// Which kernel: short rows; one workgroup a row; or parts, where a row is longer than 1024 threads hold or where there would be
+// Which kernel: short rows (16 lanes to 64 logits, a wavefront to 1024: 256 x 1000 6.4 us against 10.8 for a workgroup a row); one workgroup a row; or parts, where a row is longer than 1024 threads hold or where there would be
 // few workgroups of many logits.
 struct LogProbsPlan { int lanes, nt, vpt, parts, part_vectors; };
 LogProbsPlan log_probs_plan(int width, int64_t N, int64_t V) {
@@ -369,7 +371,7 @@ __device__ __forceinline__ float grad1(float x, int i, const RowGrad& r) {
   return p == 0.0f ? d : fmaf(-r.b * p, q + r.H, d);
 }
 
-// Streaming, bound by HBM (one read, one write).  A thread takes vectors of 16 bytes from the row's start, at any alignment: global
+// Streaming, bound by HBM (one read, one write): 1021 x 32771 fp32 51 us = 5.2 TB/s.  A thread takes vectors of 16 bytes from the row's start, at any alignment: global
 // memory takes them whole.
 constexpr int kGradT = 256, kGradV = 4;      // vectors a thread
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Vector { T x[16 / sizeof(T)]; };

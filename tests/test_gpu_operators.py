@@ -125,6 +125,51 @@ def test_group_norm_bf16_means_of_every_size(dat, shape, offset):
     gn_check_forward(dat, x, gamma, beta, shape[4], 1, out, factor=5)
 
 
+@pytest.mark.parametrize("shape", [(2, 9, 9, 40, 5), (3, 28, 28, 64, 32), (2, 56, 56, 64, 8)])
+def test_group_norm_bf16_squares_out_of_range(dat, shape):
+    """Values of 1e19 a twentieth apart: their squares' sums are not fp32 numbers, those of the deviations are."""
+    x = (1e19 * (1 + 0.02 * randn(19, *shape[:4]))).to(torch.bfloat16)
+    out = dat.group_norm_forward(x, None, None, shape[4], 0)
+    assert int(torch.isfinite(out[0]).sum()) == x.numel() and int(torch.isfinite(out[2]).sum()) == out[2].numel()
+    gn_check_forward(dat, x, None, None, shape[4], 0, out)
+    out = dat.group_norm_forward(x.float(), None, None, shape[4], 0)
+    gn_check_forward(dat, x.float(), None, None, shape[4], 0, out)
+
+
+def test_beyond_32_bit_offsets(dat):
+    """Tensors of more than 2^31 elements: the last image, row and tensor come out as they do alone."""
+    B, H, C, G = 9, 512, 1024, 32
+    x = torch.empty(B, H, H, C, dtype=torch.bfloat16, device="cuda").normal_()
+    assert x.numel() > 1 << 31
+    dy = x.flip(0)
+    y, mean, rstd = dat.group_norm_forward(x, None, None, G, 2)
+    dx, _, _ = dat.group_norm_backward(x, dy, None, None, mean, rstd, G, 2)
+    y1, m1, r1 = dat.group_norm_forward(x[-1:].contiguous(), None, None, G, 2)
+    dx1, _, _ = dat.group_norm_backward(x[-1:].contiguous(), dy[-1:].contiguous(), None, None, m1, r1, G, 2)
+    assert torch.equal(y[-1:], y1) and torch.equal(mean[-1:], m1) and torch.equal(rstd[-1:], r1) and torch.equal(dx[-1:], dx1)
+    del dy, y, dx, y1, dx1
+    rows = x.numel() // 200006
+    z = x.view(-1)[: rows * 200006].view(rows, 200006)[:, :100003]
+    labels = torch.full((rows,), 100002, dtype=torch.int32, device="cuda")
+    full = dat.log_probs(z, labels, 3)
+    lp_check(z[-2:], labels[-2:], 3, [t[-2:] for t in full])
+    ones = torch.ones(rows, device="cuda")
+    dz = torch.empty_like(x).view(-1)[: rows * 200006].view(rows, 200006)[:, :100003]
+    dat.log_probs_backward(z, labels, full[2], full[1], ones, ones, dlogits=dz)
+    assert torch.equal(dz[-2:], dat.log_probs_backward(z[-2:].clone(), labels[-2:], full[2][-2:], full[1][-2:], ones[:2], ones[:2]))
+    del x, z, dz, full
+    torch.cuda.empty_cache()
+    d, tail = (1 << 31) + 1003, 777
+    theta, g = torch.ones(d, device="cuda"), torch.empty(d, device="cuda").normal_()
+    m, v, _ = dat.adamw_state(d, 2)
+    half = theta[-tail:].clone()
+    ms, vs, _ = dat.adamw_state(tail, 1)
+    dat.adamw_update(theta, g, m, v, torch.tensor([0, d - tail, d], device="cuda"), 0.1, 1)
+    dat.adamw_update(half, g[-tail:].clone(), ms, vs, torch.tensor([0, tail], device="cuda"), 0.1, 1)
+    assert torch.equal(theta[-tail:], half) and torch.equal(m[-tail:], ms) and torch.equal(v[-tail:], vs)
+    assert bool((theta[: 1 << 20] != 1).any()) and bool((theta[(1 << 31) - 5: 1 << 31] != 1).any())
+
+
 def test_group_norm_without_scale_and_in_place(dat):
     shape = (3, 14, 14, 64, 16)
     x, gamma, beta, dy = gn_inputs(shape, torch.bfloat16, 31)
