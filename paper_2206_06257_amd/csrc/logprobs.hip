@@ -4,7 +4,7 @@
 // H = ln s - ln 2 w / s.  The logits are read once: a workgroup holds its row, or a part of it, in registers; what comes of the
 // parts of a row is joined by a second, small kernel.  Bound by HBM (one read), beside it about twelve instructions a logit, four
 // of them the exponential's: 2039 x 50021 bf16 with eight alternatives 57 us = 3.6 TB/s (two workgroups of 1024 threads on a
-// compute unit; 64 us with two of 512 that hold twice as much).  Few long rows are latency: 3 x 131075 with 20 alternatives 12.6 us
+// compute unit; 64 us with two of 512 that hold twice as much).  Few long rows are latency: 3 x 131075 with 20 alternatives 12.4 us
 // in two launches.
 //
 // Alternatives are ordered by one 64-bit key, the logit (as an ordered integer) above the complement of the index, so that equal
@@ -330,16 +330,21 @@ __global__ __launch_bounds__(kJoinT) void log_probs_join_kernel(LogProbsArgs a) 
     [&](int k, uint64_t key) { write_top(a, n, k, key, M, s); });
 }
 
-// Which kernel: short rows (16 lanes to 64 logits, a wavefront to 1024: 256 x 1000 6.4 us against 10.8 for a workgroup a row); one workgroup a row; or parts, where a row is longer than 1024 threads hold or where there would be
-// few workgroups of many logits.
+// Which kernel.  16 lanes a row to 64 logits.  To 1024 logits a wavefront a row where there are more than 1024 rows (8192 x 1000
+// fp32 with five alternatives 17.4 us against 20.6 for a workgroup a row, 16384 x 100 19.6 against 33.9, 4096 x 300 bf16 9.9 against
+// 13.4; even at 2048 rows), a workgroup a row below (256 x 1000 4.7 us against 6.0, 256 x 100 4.8 against 5.8, 1024 x 300 5.3 against
+// 6.2).  Longer rows: a workgroup each; in parts where a row is longer than 1024 threads hold, and where there are at most 32 rows
+// of more than 2^15 logits, when a second launch costs less than a row's time in one workgroup (bf16: 3 x 131075 with 20
+// alternatives 12.4 us against 25.0, 8 x 50021 9.2 against 10.5, 32 x 131000 11.9 against 18.3, 48 x 50021 13.2 against 10.9; fp32:
+// 1 x 33000 7.7 against 10.8, 32 x 65000 10.1 against 11.5, 48 x 65000 12.7 against 11.8, 4 x 20000 8.0 against 7.5).
 struct LogProbsPlan { int lanes, nt, vpt, parts, part_vectors; };
 LogProbsPlan log_probs_plan(int width, int64_t N, int64_t V) {
   if (V <= 64) return {16, 0, 0, 1, 0};
-  if (V <= 1024) return {64, 0, 0, 1, 0};
+  if (V <= 1024 && N > 1024) return {64, 0, 0, 1, 0};
   static const int sizes[][2] = {{256, 1}, {256, 4}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
   const int64_t vectors = V * width / 16 + 2;            // at most, with the row's start anywhere
   int64_t parts = (vectors + 1024 * 16 - 1) / (1024 * 16);
-  if (N * parts < 128 && vectors > 4096) {
+  if (N * parts <= 32 && V > 32768) {
     const int64_t want = (256 + N - 1) / N, most = (vectors + 255) / 256;
     if (parts < want) parts = want < most ? want : most;
   }
@@ -371,8 +376,8 @@ __device__ __forceinline__ float grad1(float x, int i, const RowGrad& r) {
   return p == 0.0f ? d : fmaf(-r.b * p, q + r.H, d);
 }
 
-// Streaming, bound by HBM (one read, one write): 1021 x 32771 fp32 51 us = 5.2 TB/s.  A thread takes vectors of 16 bytes from the row's start, at any alignment: global
-// memory takes them whole.
+// Streaming, bound by HBM (one read, one write): 1021 x 32771 fp32 51 us = 5.2 TB/s.  A thread takes vectors of 16 bytes from the
+// row's start, at any alignment: global memory takes them whole.
 constexpr int kGradT = 256, kGradV = 4;      // vectors a thread
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Vector { T x[16 / sizeof(T)]; };
 template <typename T>

@@ -341,6 +341,32 @@ def test_log_probs_special_rows(dat, V):
     assert float(dx[0].abs().max()) == 0.0 and torch.isnan(dx[2]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,top", [(1024, 1000, 5), (1025, 1000, 5), (1027, 65, 32), (1100, 100, 3), (1030, 1024, 8), (2049, 321, 0),
+                                     (32, 32769, 4), (33, 32769, 4), (32, 32768, 2)])
+def test_log_probs_where_the_kernel_changes(dat, N, V, top, dtype):
+    for ld, mask in ((V, None), (V + 3, -float("inf"))):
+        x, labels = lp_rows(900 + N + V, N, V, dtype, ld, mask)
+        lp_check(x, labels, top, dat.log_probs(x, labels, top))
+
+
+@pytest.mark.parametrize("V", [65, 700, 1024])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_log_probs_special_rows_among_many(dat, V, dtype):
+    """Rows that are hard to select from or hold nothing, NaN and infinities, among more than a thousand."""
+    inf, low = float("inf"), torch.finfo(dtype).min
+    i = torch.arange(V, device="cuda", dtype=torch.float32)
+    x, labels = lp_rows(78, 1031, V, torch.float32)
+    for n, row in enumerate([torch.full_like(i, 1.5), i / V, -i / V, (i.long() % 2).float(), torch.where(i.long() % 3 == 0, -0.0, 0.0),
+                             torch.full_like(i, -inf), torch.full_like(i, low), torch.where(i == V // 2, -3.0, -inf),
+                             torch.where(i == V - 1, 2.0, low), torch.where(i == V - 1, float("nan"), i / V),
+                             torch.where(i == 0, inf, i / V)]):
+        x[n] = x[1030 - n] = row
+    x, labels[3], labels[4] = x.to(dtype), V, -1
+    for top in (0, 1, 6, 32):
+        lp_check(x, labels, top, dat.log_probs(x, labels, top))
+
+
 def test_log_probs_without_labels_and_rows(dat):
     x, labels = lp_rows(11, 6, 100, torch.float32)
     logp, H, lse, tl, ti = dat.log_probs(x)
