@@ -10,10 +10,10 @@
 //   split     an image's slice is too large for that: partial sums over ranges of pixels, a small kernel that joins them, and a
 //             second pass over the tensors, from the last image to the first: the last-level cache still holds what the first
 //             pass read last.
-// Forward, resident: 256 x 56 x 56 x 256 bf16 196 us = 4.2 TB/s (one workgroup a compute unit: nothing moves while it joins its
+// Forward, resident: 256 x 56 x 56 x 256 bf16 202 us = 4.1 TB/s (one workgroup a compute unit: nothing moves while it joins its
 // sums), 512 x 32 x 32 x 64 27 us = 5.0 TB/s; split (256 x 112 x 112 x 64) 264 us, three passes at 4.7 TB/s.
 // Backward, resident: 256 x 28 x 28 x 512 bf16 146 us = 4.2 TB/s; split: 85 x 112 x 112 x 64 with SiLU 158 us, five passes at
-// 4.3 TB/s (sums 67 us, half of it arithmetic; apply 78 us = 5.2 TB/s).
+// 4.3 TB/s (sums 69 us, half of it arithmetic; apply 78 us = 5.2 TB/s).
 #include <type_traits>
 #include "kernels.h"
 #include "lanes.h"
