@@ -256,7 +256,7 @@ dat_status dat_lamb_update(dat_model* m, const float* grads, int use_adam, float
  *   (with 32 bits in that element alone), and so do the parameters it updates.
  * All pointers need the alignment of their elements only.  t, lr and seed are launch arguments: a captured graph repeats them.
  * Asynchronous on `stream`, no allocation.  DAT_ERR_ARG: null pointers, state_bits not 8 or 32, t < 1, b1 or b2 outside [0,1),
- * lr, eps or weight_decay negative or NaN, more than 2^31-1 slots.  d = 0: nothing happens.  (eps = 0 divides by zero where v is.)
+ * lr, eps or weight_decay negative or NaN, more than 2^26 - 4 slots.  d = 0: nothing happens.  (eps = 0 divides by zero where v is.)
  * dat_adamw_moments: the values that 8-bit moments stand for, device fp32 [d] each (a checkpoint, a change to 32 bits).
  * dat_model_adamw_update: the same step on a model's master parameters; conv and linear weights decay, biases, scales and shifts
  *   do not.  The moments live in the model (allocated on the first call, zero; `state_bits` is fixed from then on:
@@ -289,7 +289,8 @@ dat_status dat_model_adamw_update(dat_model* m, const float* grads, int state_bi
  *   be the logits themselves (then ldd = ld); elements between the rows are not touched.
  * workspace: device, 16-byte aligned, dat_log_probs_workspace(N, V, top) bytes (may be 0, then NULL is allowed); nothing in it
  * outlives the call.  Asynchronous on `stream`, no allocation.  N = 0: nothing happens.  DAT_ERR_ARG: null or misaligned
- * pointers, N or top negative, top > DAT_MAX_TOP, V < 1, ld < V, a workspace that is too small; DAT_ERR_SHAPE: V > 2^30, N > 2^31-1. */
+ * pointers, N or top negative, top > DAT_MAX_TOP, V < 1, ld < V, a workspace that is too small; DAT_ERR_SHAPE: V > 2^30, N > 2^31-1, or
+ * more threads than the 2^32 of a launch (from 4 for a row of a few logits to 1024 for a row, or a part of one, of many). */
 #define DAT_MAX_TOP 32
 size_t dat_log_probs_workspace(int64_t N, int64_t V, int top);
 dat_status dat_log_probs(const void* logits, dat_dtype dtype, int64_t N, int64_t V, int64_t ld, const int32_t* labels, int top,
@@ -315,7 +316,7 @@ dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype, int64_t N
  * backward; may be 0, then NULL is allowed); nothing in it outlives the call.  Asynchronous on `stream`, no allocation.
  * B = 0: no output but dgamma = dbeta = 0.  DAT_ERR_ARG: null or misaligned pointers, sizes below 1 (B below 0), groups that
  * do not divide C, unknown act or dtype, eps negative or NaN, a workspace that is too small; DAT_ERR_SHAPE: H*W*C, B*groups or
- * B*C above 2^30. */
+ * B*C above 2^30, or tiles (groups, ranges of pixels) for more than a launch's 2^32 threads, 256 to 1024 each: from 2^22 on. */
 typedef enum { DAT_ACT_NONE = 0, DAT_ACT_RELU = 1, DAT_ACT_SILU = 2 } dat_act;
 size_t dat_group_norm_workspace(int pass, dat_dtype dtype, int B, int H, int W, int C, int groups);
 dat_status dat_group_norm_forward(const void* x, const float* gamma, const float* beta, dat_dtype dtype, int B, int H, int W,

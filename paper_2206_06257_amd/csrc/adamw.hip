@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kT) void adamw_moments_kernel(const uint8_t* __rest
   else if (left > 0) moments_block<false>(m, v, scales, slot, e0, left, lane, m_out, v_out);
 }
 
-inline unsigned blocks_for(int64_t slots) { return (unsigned)((slots + kWaves - 1) / kWaves); }
+inline int64_t blocks_for(int64_t slots) { return (slots + kWaves - 1) / kWaves; }
 
 }  // namespace
 
@@ -204,7 +204,7 @@ dat_status launch_adamw(float* theta, const void* g, int g_dtype, const int64_t*
                         int16_t* scales, uint64_t seed, const AdamwParams& hp, const float* decay, bf16_t* copy, hipStream_t st) {
   const int64_t slots = dat_adamw_slots(d, T);
   AdamwArgs a{theta, g, m, v, scales, off, decay, copy, T, (int)slots, seed, hp};
-  const dim3 grid(blocks_for(slots)), block(kT);
+  const dim3 grid((unsigned)blocks_for(slots)), block(kT);
   if (bits == 8 && g_dtype == DAT_BF16) hipLaunchKernelGGL((adamw_kernel<8, bf16_t, Half4U>), grid, block, 0, st, a);
   else if (bits == 8) hipLaunchKernelGGL((adamw_kernel<8, float, Float4U>), grid, block, 0, st, a);
   else if (g_dtype == DAT_BF16) hipLaunchKernelGGL((adamw_kernel<32, bf16_t, Half4U>), grid, block, 0, st, a);
@@ -231,7 +231,7 @@ extern "C" dat_status dat_adamw_update(float* theta, const void* grads, dat_dtyp
   if (!theta || !grads || !offsets_dev || !m || !v || (state_bits == 8 && !scales)) return DAT_ERR_ARG;
   if (!aligned(theta, 4) || !aligned(grads, grad_dtype == DAT_BF16 ? 2 : 4) || !aligned(offsets_dev, 8) || !aligned(scales, 2) ||
       !aligned(decay, 4) || !aligned(theta_bf16, 2) || (state_bits == 32 && (!aligned(m, 4) || !aligned(v, 4)))) return DAT_ERR_ARG;
-  if (dat_adamw_slots(d, num_tensors) > INT32_MAX - kWaves) return DAT_ERR_ARG;
+  if (!fits_launch(blocks_for(dat_adamw_slots(d, num_tensors)), kT)) return DAT_ERR_ARG;
   if (decay) hp.wd = 1.0f;
   return launch_adamw(theta, grads, grad_dtype, offsets_dev, num_tensors, d, state_bits, m, v, scales, seed, hp, decay, theta_bf16,
                       (hipStream_t)stream);
@@ -244,8 +244,8 @@ extern "C" dat_status dat_adamw_moments(const uint8_t* m, const uint8_t* v, cons
   if (!m || !v || !scales || !offsets_dev || !m_out || !v_out) return DAT_ERR_ARG;
   if (!aligned(scales, 2) || !aligned(offsets_dev, 8) || !aligned(m_out, 4) || !aligned(v_out, 4)) return DAT_ERR_ARG;
   const int64_t slots = dat_adamw_slots(d, num_tensors);
-  if (slots > INT32_MAX - kWaves) return DAT_ERR_ARG;
-  hipLaunchKernelGGL(adamw_moments_kernel, dim3(blocks_for(slots)), dim3(kT), 0, (hipStream_t)stream, m, v, scales, offsets_dev,
+  if (!fits_launch(blocks_for(slots), kT)) return DAT_ERR_ARG;
+  hipLaunchKernelGGL(adamw_moments_kernel, dim3((unsigned)blocks_for(slots)), dim3(kT), 0, (hipStream_t)stream, m, v, scales, offsets_dev,
                      num_tensors, (int)slots, m_out, v_out);
   DAT_LAUNCH_CHECK();
   return DAT_OK;

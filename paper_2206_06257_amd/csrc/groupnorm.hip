@@ -797,6 +797,11 @@ size_t workspace_of(const Plan& p, bool backward, int B, int C, int G) {
     else { constexpr int ACT = DAT_ACT_NONE; __VA_ARGS__; }                               \
   } while (0)
 
+bool fits_launches(const Plan& p, int B, int G) {
+  if (p.nt) return fits_launch((int64_t)B * p.slices + kXcds, p.nt);
+  return fits_launch((int64_t)B * p.chunks * p.slices, kT) && fits_launch((int64_t)B * G, kT);
+}
+
 inline unsigned tiles_of(const GnArgs& a) { return (unsigned)(((int64_t)a.B * a.slices + kXcds - 1) / kXcds * kXcds); }
 
 template <typename T, int GV> void launch_forward_resident(const Plan& p, const GnArgs& a, dat_act act, hipStream_t st) {
@@ -866,7 +871,7 @@ extern "C" dat_status dat_group_norm_forward(const void* x, const float* gamma, 
   const Plan p = plan_of(false, dtype, aligned(x, 16) && aligned(y, 16), B, H * W, C, groups);
   GnArgs a{x, nullptr, gamma, beta, nullptr, nullptr, y, mean, rstd, (float*)workspace, B, H * W, C, groups, C / groups,
            p.nv, p.sv, p.slices, p.chunk, p.chunks, eps};
-  if ((int64_t)B * p.slices * (p.nt ? 1 : p.chunks) > INT32_MAX) return DAT_ERR_SHAPE;
+  if (!fits_launches(p, B, groups)) return DAT_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   if (p.nt) {
     if (dtype == DAT_BF16) launch_resident<bf16_t>(false, p, a, act, st); else launch_resident<float>(false, p, a, act, st);
@@ -894,7 +899,7 @@ extern "C" dat_status dat_group_norm_backward(const void* x, const void* dy, con
   const Plan p = plan_of(true, dtype, aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16), B, H * W, C, groups);
   GnArgs a{x, dy, gamma, beta, mean, rstd, dx, nullptr, nullptr, (float*)workspace, B, H * W, C, groups, C / groups,
            p.nv, p.sv, p.slices, p.chunk, p.chunks, 0.0f};
-  if ((int64_t)B * p.slices * (p.nt ? 1 : p.chunks) > INT32_MAX) return DAT_ERR_SHAPE;
+  if (!fits_launches(p, B, groups) || !fits_launch((C + 63) / 64, 64 * kParamRows)) return DAT_ERR_SHAPE;
   if (p.nt && B > 0) {
     if (dtype == DAT_BF16) launch_resident<bf16_t>(true, p, a, act, st); else launch_resident<float>(true, p, a, act, st);
     DAT_LAUNCH_CHECK();

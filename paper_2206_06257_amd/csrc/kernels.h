@@ -212,6 +212,9 @@ struct LambParams {
 dat_status launch_lamb(float* theta, const float* g, float* m, float* v, float* u, const int64_t* off, int T, int64_t d,
                        const LambParams& hp, double* norms, hipStream_t st);
 
+// A launch has fewer than 2^32 threads along a dimension.
+inline bool fits_launch(int64_t blocks, int64_t threads) { return blocks <= INT32_MAX && blocks * threads <= UINT32_MAX; }
+
 struct AdamwParams {
   float lr, b1, b2, eps, wd;   // wd multiplies the tensor's decay where there is a table of them
   float om1, om2, c1, c2;      // 1-b, 1/(1-b^t)

@@ -9,8 +9,8 @@ template <int CTRL, int ROWS> __device__ __forceinline__ int dpp(int v) { return
 template <int L, typename F> __device__ __forceinline__ int lanes_reduce(int v, F f) {
   v = f(v, dpp<0xb1, 0xf>(v));                   // the other of two, of two pairs, of half a row, of a row of 16
   v = f(v, dpp<0x4e, 0xf>(v));
-  v = f(v, dpp<0x141, 0xf>(v));
-  v = f(v, dpp<0x140, 0xf>(v));
+  if (L >= 16) v = f(v, dpp<0x141, 0xf>(v));
+  if (L >= 16) v = f(v, dpp<0x140, 0xf>(v));
   if (L == 64) {
     const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47),
               d = __builtin_amdgcn_readlane(v, 63);

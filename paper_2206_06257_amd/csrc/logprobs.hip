@@ -85,7 +85,7 @@ __device__ __forceinline__ void write_top(const LogProbsArgs& a, int64_t n, int 
 }
 
 // ---- short rows: L lanes a row, E logits a lane ---------------------------------------------------------------------------
-constexpr int kShortT = 64;
+constexpr int kShortT = 256;
 template <typename T, int L, int E>
 __global__ __launch_bounds__(kShortT) void log_probs_short_kernel(LogProbsArgs a) {
   const int64_t n = (int64_t)blockIdx.x * (kShortT / L) + threadIdx.x / L;
@@ -330,17 +330,21 @@ __global__ __launch_bounds__(kJoinT) void log_probs_join_kernel(LogProbsArgs a) 
     [&](int k, uint64_t key) { write_top(a, n, k, key, M, s); });
 }
 
-// Which kernel.  16 lanes a row to 64 logits.  To 1024 logits a wavefront a row where there are more than 1024 rows (8192 x 1000
-// fp32 with five alternatives 17.4 us against 20.6 for a workgroup a row, 16384 x 100 19.6 against 33.9, 4096 x 300 bf16 9.9 against
-// 13.4; even at 2048 rows), a workgroup a row below (256 x 1000 4.7 us against 6.0, 256 x 100 4.8 against 5.8, 1024 x 300 5.3 against
-// 6.2).  Longer rows: a workgroup each; in parts where a row is longer than 1024 threads hold, and where there are at most 32 rows
-// of more than 2^15 logits, when a second launch costs less than a row's time in one workgroup (bf16: 3 x 131075 with 20
-// alternatives 12.4 us against 25.0, 8 x 50021 9.2 against 10.5, 32 x 131000 11.9 against 18.3, 48 x 50021 13.2 against 10.9; fp32:
-// 1 x 33000 7.7 against 10.8, 32 x 65000 10.1 against 11.5, 48 x 65000 12.7 against 11.8, 4 x 20000 8.0 against 7.5).
-struct LogProbsPlan { int lanes, nt, vpt, parts, part_vectors; };
+// Which kernel.  As few lanes a row as hold it, 4 to 16 logits (2^20 x 10 fp32 17.2 us against 55.1 with 16 lanes), 16 to 64 (65536 x 64
+// 6.4 against 16.9 with 64) and, where there are more than 1024 rows, to 256 (65536 x 100 with three alternatives 18.8 against 37.9;
+// 2048 x 100 5.0 against 4.3), then a wavefront to 1024 (8192 x 1000 with five alternatives 17.4 against 20.6 for a workgroup a
+// row, 4096 x 300 bf16 9.9 against 13.4; even at 2048 rows).  With fewer rows a workgroup each (256 x 1000 4.7 against 6.0 for a
+// wavefront, 256 x 100 4.8 against 5.8, 1024 x 300 5.3 against 6.2), and for longer ones; in parts where a row is longer than 1024
+// threads hold, and where there are at most 32 rows of more than 2^15 logits, when a second launch costs less than a row's time in
+// one workgroup (bf16: 3 x 131075 with 20 alternatives 12.4 us against 25.0, 8 x 50021 9.2 against 10.5, 32 x 131000 11.9 against
+// 18.3, 48 x 50021 13.2 against 10.9; fp32: 1 x 33000 7.7 against 10.8, 32 x 65000 10.1 against 11.5, 48 x 65000 12.7 against
+// 11.8, 4 x 20000 8.0 against 7.5).
+struct LogProbsPlan { int lanes, nt, vpt, parts, part_vectors; };     // lanes = 0: nt threads, vpt vectors each, else vpt logits a lane
 LogProbsPlan log_probs_plan(int width, int64_t N, int64_t V) {
-  if (V <= 64) return {16, 0, 0, 1, 0};
-  if (V <= 1024 && N > 1024) return {64, 0, 0, 1, 0};
+  if (V <= 16) return {4, 0, 4, 1, 0};
+  if (V <= 64) return {16, 0, 4, 1, 0};
+  if (V <= 256 && N > 1024) return {16, 0, 16, 1, 0};
+  if (V <= 1024 && N > 1024) return {64, 0, 16, 1, 0};
   static const int sizes[][2] = {{256, 1}, {256, 4}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
   const int64_t vectors = V * width / 16 + 2;            // at most, with the row's start anywhere
   int64_t parts = (vectors + 1024 * 16 - 1) / (1024 * 16);
@@ -407,10 +411,50 @@ __global__ __launch_bounds__(kGradT) void log_probs_grad_kernel(LogProbsGradArgs
   }
 }
 
+// Short rows: L lanes a row, kGradV vectors a lane at most.
+template <typename T, int L>
+__global__ __launch_bounds__(kGradT) void log_probs_grad_short_kernel(LogProbsGradArgs g) {
+  constexpr int VE = 16 / sizeof(T);
+  const int64_t n = (int64_t)blockIdx.x * (kGradT / L) + threadIdx.x / L;
+  if (n >= g.N) return;
+  const int V = (int)g.V, first = (int)(threadIdx.x % L) * VE;
+  if (first >= V) return;
+  const RowGrad r = row_grad(g, n);
+  const T* x = (const T*)g.x + n * g.ld;
+  T* dx = (T*)g.dx + n * g.ldd;
+  Vector<T> v[kGradV];
+#pragma unroll
+  for (int k = 0; k < kGradV; ++k) {
+    const int i = first + k * L * VE;
+    if (i + VE <= V) v[k] = *reinterpret_cast<const Vector<T>*>(x + i);
+    else {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) if (i + j < V) v[k].x[j] = x[i + j];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kGradV; ++k) {
+    const int i = first + k * L * VE;
+    if (i >= V) break;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) store1(&v[k].x[j], i + j < V ? grad1(load1(&v[k].x[j]), i + j, r) : 0.0f);
+    if (i + VE <= V) *reinterpret_cast<Vector<T>*>(dx + i) = v[k];
+    else {
+#pragma unroll
+      for (int j = 0; j < VE; ++j) if (i + j < V) dx[i + j] = v[k].x[j];
+    }
+  }
+}
+
 template <typename T> void launch_log_probs(const LogProbsPlan& p, const LogProbsArgs& a, hipStream_t st) {
   const unsigned rows = (unsigned)a.N;
-  if (p.lanes == 16) { hipLaunchKernelGGL((log_probs_short_kernel<T, 16, 4>), dim3((rows + 3) / 4), dim3(kShortT), 0, st, a); return; }
-  if (p.lanes == 64) { hipLaunchKernelGGL((log_probs_short_kernel<T, 64, 16>), dim3(rows), dim3(kShortT), 0, st, a); return; }
+#define DAT_LP_SHORT(L, E)                                                                                                          \
+  if (p.lanes == L && p.vpt == E) {                                                                                                 \
+    hipLaunchKernelGGL((log_probs_short_kernel<T, L, E>), dim3((rows + kShortT / L - 1) / (kShortT / L)), dim3(kShortT), 0, st, a); \
+    return;                                                                                                                         \
+  }
+  DAT_LP_SHORT(4, 4) DAT_LP_SHORT(16, 4) DAT_LP_SHORT(16, 16) DAT_LP_SHORT(64, 16)
+#undef DAT_LP_SHORT
 #define DAT_LP_SIZE(NT, VPT)                                                                                                        \
   if (p.nt == NT && p.vpt == VPT) {                                                                                                 \
     if (p.parts == 1) hipLaunchKernelGGL((log_probs_long_kernel<T, NT, VPT, true>), dim3(rows), dim3(NT), 0, st, a);                \
@@ -419,6 +463,19 @@ template <typename T> void launch_log_probs(const LogProbsPlan& p, const LogProb
   DAT_LP_SIZE(256, 1) DAT_LP_SIZE(256, 4) DAT_LP_SIZE(256, 8) DAT_LP_SIZE(512, 8) DAT_LP_SIZE(1024, 8) DAT_LP_SIZE(1024, 16)
 #undef DAT_LP_SIZE
   if (p.parts > 1) hipLaunchKernelGGL(log_probs_join_kernel<T>, dim3(rows), dim3(kJoinT), 0, st, a);
+}
+
+// Lanes a row of the gradient, 0: workgroups of one row.  2^20 x 10 fp32 20.8 us with 4 lanes, 64.1 with 16, 894 with a workgroup;
+// 16384 x 256 9.3 with 16, 14.0 with a workgroup; 256 x 100 3.2 and 2.7; longer rows: 16384 x 1000 24.9 with 64 lanes, 22.1 with a
+// workgroup.
+int log_probs_grad_lanes(int width, int64_t V) {
+  const int64_t vectors = (V * width + 15) / 16;
+  return vectors <= 4 * kGradV ? 4 : vectors <= 16 * kGradV ? 16 : 0;
+}
+template <typename T> void launch_log_probs_grad(int lanes, unsigned blocks, unsigned each, const LogProbsGradArgs& g, hipStream_t st) {
+  if (lanes == 4) hipLaunchKernelGGL((log_probs_grad_short_kernel<T, 4>), dim3(blocks), dim3(kGradT), 0, st, g);
+  else if (lanes == 16) hipLaunchKernelGGL((log_probs_grad_short_kernel<T, 16>), dim3(blocks), dim3(kGradT), 0, st, g);
+  else hipLaunchKernelGGL(log_probs_grad_kernel<T>, dim3(blocks), dim3(kGradT), 0, st, g, each);
 }
 
 }  // namespace
@@ -462,7 +519,8 @@ extern "C" dat_status dat_log_probs(const void* logits, dat_dtype dtype, int64_t
   const LogProbsPlan p = log_probs_plan(dtype == DAT_BF16 ? 2 : 4, N, V);
   LogProbsArgs a{logits, N, V, ld, labels, top, logp, entropy, lse, top_logp, top_index, p.parts, p.part_vectors, (Part*)workspace, nullptr};
   if (p.parts > 1) a.keys = reinterpret_cast<uint64_t*>(a.part + N * p.parts);
-  if (N * p.parts > INT32_MAX) return DAT_ERR_SHAPE;
+  const int64_t lanes = p.lanes ? p.lanes : (int64_t)p.parts * p.nt;
+  if (!fits_launch((N * lanes + kShortT - 1) / kShortT, kShortT) || (p.parts > 1 && !fits_launch(N, kJoinT))) return DAT_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   if (dtype == DAT_BF16) launch_log_probs<bf16_t>(p, a, st); else launch_log_probs<float>(p, a, st);
   DAT_LAUNCH_CHECK();
@@ -480,10 +538,12 @@ extern "C" dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype
   if (!aligned(labels, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(dlogp, 4) || !aligned(dentropy, 4)) return DAT_ERR_ARG;
   LogProbsGradArgs g{logits, N, V, ld, ldd, labels, lse, entropy, dlogp, dentropy, dlogits};
   hipStream_t st = (hipStream_t)stream;
-  const int64_t per = kGradT * kGradV * 16 / (dtype == DAT_BF16 ? 2 : 4), blocks = (V + per - 1) / per;
-  if (N * blocks > INT32_MAX) return DAT_ERR_SHAPE;
-  if (dtype == DAT_BF16) hipLaunchKernelGGL(log_probs_grad_kernel<bf16_t>, dim3((unsigned)(N * blocks)), dim3(kGradT), 0, st, g, (unsigned)blocks);
-  else hipLaunchKernelGGL(log_probs_grad_kernel<float>, dim3((unsigned)(N * blocks)), dim3(kGradT), 0, st, g, (unsigned)blocks);
+  const int lanes = log_probs_grad_lanes(dtype == DAT_BF16 ? 2 : 4, V);
+  const int64_t per = kGradT * kGradV * 16 / (dtype == DAT_BF16 ? 2 : 4), each = lanes ? 1 : (V + per - 1) / per;
+  const int64_t blocks = lanes ? (N + kGradT / lanes - 1) / (kGradT / lanes) : N * each;
+  if (!fits_launch(blocks, kGradT)) return DAT_ERR_SHAPE;
+  if (dtype == DAT_BF16) launch_log_probs_grad<bf16_t>(lanes, (unsigned)blocks, (unsigned)each, g, st);
+  else launch_log_probs_grad<float>(lanes, (unsigned)blocks, (unsigned)each, g, st);
   DAT_LAUNCH_CHECK();
   return DAT_OK;
 }

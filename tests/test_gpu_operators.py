@@ -399,6 +399,17 @@ def test_log_probs_backward(dat, N, V, dtype):
         assert torch.equal(own, dx)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V", [(100003, 10), (5, 4), (1301, 16), (1100, 17), (1500, 64), (70, 65), (900, 128), (513, 129), (1040, 256),
+                                 (257, 257), (130, 512), (65, 513)])
+def test_log_probs_of_short_rows(dat, N, V, dtype):
+    """Lengths and numbers of rows around the changes of the lanes a row takes, both directions."""
+    for ld, mask, top in ((V, None, 3), (V + 1, -float("inf"), min(V, 32))):
+        x, labels = lp_rows(500 + V, N, V, dtype, ld, mask)
+        lp_check(x, labels, top, dat.log_probs(x, labels, top))
+    test_log_probs_backward(dat, N, V, dtype)
+
+
 def test_log_probs_gradient_against_differences(dat):
     x, labels = lp_rows(400, 3, 9, torch.float32, scale=1.5)
     _, H, lse, _, _ = dat.log_probs(x, labels)

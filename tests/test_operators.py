@@ -80,6 +80,14 @@ def test_adamw_refuses(kw):
     assert adamw(**kw) == 1
 
 
+def test_more_threads_than_a_launch_has_are_refused():
+    assert lp(N=1 << 30) == 2 and lp(N=1 << 28, V=100, ld=100) == 2 and lp(N=1 << 23, V=20000, ld=20000) == 2
+    assert lp_bwd(N=1 << 30) == 2 and lp_bwd(N=1 << 24, V=2000, ld=2000, ldd=2000) == 2
+    assert adamw(d=1 << 34) == 1 and lib.dat_adamw_moments(P, P, P, P, 2, 1 << 34, P, P, None) == 1
+    small = dict(B=1 << 24, H=1, W=1, C_=64, groups=32, ws=P, size=1 << 40)
+    assert gn_fwd(**small) == 2 and gn_bwd(**small) == 2
+
+
 def test_nothing_to_do_is_no_error():
     assert adamw(d=0, theta=None, g=None, m=None, v=None) == 0
     assert lp(N=0, x=None, labels=None, logp=None, entropy=None, lse=None, tl=None, ti=None, ws=None, size=0) == 0
