@@ -108,15 +108,14 @@ __device__ __forceinline__ float gn_z(float xm, float rstd, float gamma, float b
   return __fadd_rn(__fmul_rn(__fmul_rn(xm, rstd), gamma), beta);
 }
 // 1 / (1 + e^-z) from the hardware's exponential and reciprocal (1 unit of 2^-23 each).  fp32 outputs: the rounding error of the
-// exponent z log2(e) goes back in, or it would grow with |z|.  Below z = -88.7 e^-z is infinite and the sigmoid 0 (it has to be, beside a
-// z of any size); what goes back in is kept finite there, as infinity less infinity is no number.
+// exponent z log2(e) goes back in, or it would grow with |z|: as a factor, not as a sum, which would be infinity less infinity below
+// z = -88.7, where e^-z is infinite.  The sigmoid is 0 there (it has to be, beside a z of any size).
 template <typename T> __device__ __forceinline__ float sigmoid(float z) {
   constexpr float kLog2e = 1.44269504088896340736f, kLog2eLow = 1.92596299112661746887e-8f, kLn2 = 0.69314718055994530942f;
-  constexpr float kLargest = 3.40282346638528859812e38f;
   if (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * z));
   const float y = -__builtin_amdgcn_fmed3f(z, -126.0f, 126.0f), t = y * kLog2e;
   const float low = fmaf(y, kLog2eLow, fmaf(y, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
-  return __builtin_amdgcn_rcpf(1.0f + fmaf(fminf(e, kLargest) * kLn2, low, e));
+  return __builtin_amdgcn_rcpf(fmaf(e, fmaf(kLn2, low, 1.0f), 1.0f));
 }
 template <typename T, int ACT> __device__ __forceinline__ float act_of(float z) {
   if (ACT == DAT_ACT_RELU) return __builtin_elementwise_maximum(z, 0.0f);      // NaN stays
