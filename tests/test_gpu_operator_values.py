@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests import plain_ops as po
-from tests.test_gpu_operators import U, assert_near, dat, gn_check_forward, gn_inputs, half, host, randn  # noqa: F401 (dat: fixture)
+from tests.test_gpu_operators import U, assert_near, dat, gn_check_backward, gn_check_forward, gn_inputs, half, host, randn  # noqa: F401 (dat: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,39 @@ def test_group_norm_silu_of_huge_values(dat):  # noqa: F811
             y = host(dat.group_norm_forward(x.to(dtype), gamma, torch.zeros_like(gamma), 1, 2)[0]).reshape(-1)
             # (mean 0, variance 1: z = +-size, but for eps and roundings, 1e-5 of it)
             assert (np.abs(y[0::2]) <= size * 2.0 ** -100).all() and (np.abs(y[1::2] - size) <= (1e-5 + half(dtype)) * size).all(), (dtype, size)
+
+
+# (all resident, all with threads beyond the last pixel)
+@pytest.mark.parametrize("shape", [(2, 9, 9, 40, 5), (3, 15, 15, 512, 32), (1, 1, 1, 64, 8), (2, 30, 30, 64, 16), (5, 7, 7, 64, 32)])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_group_norm_backward_with_far_means(dat, shape, act, dtype):  # noqa: F811
+    """Means of many spreads, where z of a zero lies far from every value's: threads beyond the last pixel hold zeros."""
+    B, H, W, C, G = shape
+    _, gamma, beta, dy = gn_inputs(shape, dtype, 400)
+    for means in (90.0, 95.0, 110.0, 125.0, 1000.0):
+        for sign in (1, -1):
+            x = (sign * means + randn(401, B, H, W, C)).to(dtype)
+            _, mean, rstd = dat.group_norm_forward(x, gamma, beta, G, act)
+            out = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, G, act)
+            if act == 2:
+                silu_check_backward(x, dy, gamma, beta, mean, rstd, G, out)
+            else:
+                gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, act, out)
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_group_norm_backward_of_large_constants(dat, dtype, act):  # noqa: F811
+    """Every value 2^120: xhat = 0 and rstd = 1/sqrt(eps), but mean rstd is no fp32 number."""
+    shape, G = (2, 1, 2, 64, 8), 8
+    _, gamma, beta, dy = gn_inputs(shape, dtype, 410)
+    for sign in (1.0, -1.0):
+        x = torch.full(shape[:4], sign * 2.0 ** 120, device="cuda").to(dtype)
+        _, mean, rstd = dat.group_norm_forward(x, gamma, beta, G, act)
+        assert (mean == sign * 2.0 ** 120).all()
+        out = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, G, act)
+        if act == 2:
+            silu_check_backward(x, dy, gamma, beta, mean, rstd, G, out)
+        else:
+            gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, act, out)
