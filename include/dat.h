@@ -285,7 +285,9 @@ dat_status dat_model_adamw_update(dat_model* m, const float* grads, int state_bi
  *   A label outside [0, V) gives a NaN logp and, in the gradient, no one-hot term (as in every call that takes labels).
  * dat_log_probs_backward: dlogits[n][i] = dlogp[n] ([i = y] - p_i) - dentropy[n] p_i (log p_i + entropy[n]), rounded once to
  *   `dtype`; rows at dlogits + n*ldd.  labels, dlogp: device, together or both NULL; entropy, dentropy likewise.  lse: as the forward call
- *   wrote it.  p_i = 0 gives no entropy term; a row with nothing allowed gets zeros, one whose lse is NaN gets NaN.  dlogits may
+ *   wrote it; p_i = exp(x_i - lse) where |lse| <= 64, whose rounding moves p_i by at most 2^-19 of itself.  Beyond, where fp32 keeps too
+ *   little of the sum beside the maximum, both are taken from the row again (a second read; one workgroup does such a row).
+ *   p_i = 0 gives no entropy term; a row with nothing allowed gets zeros, one whose lse is NaN gets NaN.  dlogits may
  *   be the logits themselves (then ldd = ld); elements between the rows are not touched.
  * workspace: device, 16-byte aligned, dat_log_probs_workspace(N, V, top) bytes (may be 0, then NULL is allowed); nothing in it
  * outlives the call.  Asynchronous on `stream`, no allocation.  N = 0: nothing happens.  DAT_ERR_ARG: null or misaligned

@@ -110,6 +110,28 @@ def log_probs_backward(x, labels, lse, H, a, b):
     return out, size
 
 
+def softmax_gradient(x, labels, a, b):
+    """a ([i = y] - p) - b p (log p + H) of the rows' own softmax in 64 bits: (gradient, p, log p, H)."""
+    x = np.asarray(x, np.float64)
+    N, V = x.shape
+    out, ps, qs, hs = np.full((N, V), np.nan), np.zeros((N, V)), np.zeros((N, V)), np.zeros(N)
+    for n in range(N):
+        r = x[n]
+        if np.isnan(r).any() or (r == np.inf).any():
+            continue
+        out[n] = 0.0
+        if (r == -np.inf).all():
+            continue
+        q = r - r.max()
+        q = q - np.log(np.exp(q).sum())
+        p = np.exp(q)
+        fine = np.where(p > 0, q, 0.0)
+        H = -(p * fine).sum()
+        out[n] = a[n] * ((np.arange(V) == labels[n]) - p) - b[n] * p * (fine + H)
+        ps[n], qs[n], hs[n] = p, q, H
+    return out, ps, qs, hs
+
+
 # ---- AdamW ---------------------------------------------------------------------------------------------------------
 def philox(counter, seed, stream):
     """Words [n, 4] of Philox4x32-10 for uint64 counters."""

@@ -1,4 +1,5 @@
-"""Group norm, label log probabilities and AdamW on the GPU at values (not shapes) where they can go wrong.
+"""Group norm, label log probabilities and AdamW on the GPU at values (not shapes) where they can go wrong: activations far from
+zero, means far from the values' spread, sums next to the end of the range, logits with a large common offset.
 
 Tolerances count roundings as in test_gpu_operators.py."""
 import numpy as np
@@ -6,7 +7,7 @@ import pytest
 import torch
 
 from tests import plain_ops as po
-from tests.test_gpu_operators import U, assert_near, dat, gn_check_backward, gn_check_forward, gn_inputs, half, host, randn  # noqa: F401 (dat: fixture)
+from tests.test_gpu_operators import U, assert_near, dat, gn_check_backward, gn_check_forward, gn_inputs, half, host, lp_check, lp_rows, randn  # noqa: F401 (dat: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +98,81 @@ def test_group_norm_backward_of_large_constants(dat, dtype, act):  # noqa: F811
             silu_check_backward(x, dy, gamma, beta, mean, rstd, G, out)
         else:
             gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, act, out)
+
+
+# ---- log probabilities ---------------------------------------------------------------------------------------------
+def lp_check_gradient(x, labels, a, b, dx):
+    """Against the softmax's own gradient.  log p is off by (K + 4 log V) U from the sum, by 2 U |lse| where it comes from an lse of at
+    most 64 in size, and by 4 U of itself; p by that and 4 U."""
+    want, p, q, H = po.softmax_gradient(host(x), labels.cpu().numpy(), host(a), host(b))
+    V = x.shape[1]
+    hot = np.arange(V)[None, :] == labels.cpu().numpy()[:, None]
+    a, b, H = np.abs(host(a))[:, None], np.abs(host(b))[:, None], H[:, None]
+    K = V / 64 + 24 + 4 * np.log(V) + 4
+    with np.errstate(invalid="ignore"):
+        q = np.where(p > 0, np.abs(q), 0.0)
+    off = (K + 128 + 4 * q) * U
+    tol = a * (p * off + 2 * U * (hot + p)) + b * p * (off * (q + H + 1) + 3 * (K + 4) * (np.log(V) + 1) * U + 2 * U * (q + H))
+    tol += (a + 200 * b) * 2.0 ** -126 + half(dx.dtype) * 1.01 * (np.abs(want) + tol)
+    assert_near(host(dx), want, tol, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V", [(41, 1), (41, 2), (300, 5), (41, 16), (41, 17), (41, 64), (41, 65), (41, 128), (41, 129), (41, 256), (41, 257), (41, 1000),
+                                 (41, 4099), (41, 9001), (41, 70001)])
+def test_log_probs_gradient_beside_large_offsets(dat, N, V, dtype):  # noqa: F811
+    """Rows that a common offset moves far from zero, up to rows of the type's lowest and largest value: p is that of the softmax."""
+    low, high, inf = torch.finfo(dtype).min, torch.finfo(dtype).max, float("inf")
+    x = randn(500 + V, N, V)
+    offsets = [0.0, 30.0, 57.0, 63.9, 64.1, 90.0, 1e3, 3e4, 1e6, 1e12, 1e30]
+    for n in range(N):
+        o = offsets[(n // 2) % len(offsets)]
+        step = max(o * (half(dtype) * 2), 2.0 ** -6) if o >= 1e3 else 1.0       # values that differ by a few steps of the type
+        x[n] = (x[n] * step + o) * (1 if n % 2 else -1)
+    x[22], x[23], x[24], x[25] = low, high, 3e38, -3e38
+    x[26], x[27], x[28] = 1e6, -1e6, 65.0                                       # all alike
+    x[29] = torch.where(torch.arange(V, device="cuda") % 3 == 1, low, 1e5)      # masked by the lowest value, by -inf
+    x[30] = torch.where(torch.arange(V, device="cuda") % 3 == 1, -inf, 1e5)
+    x[31] = torch.where(torch.arange(V, device="cuda") % 3 == 1, -inf, low)
+    x[32] = torch.where(torch.arange(V, device="cuda") % 2 == 1, low, high)
+    x[33] = -inf
+    x[34, V // 2], x[35, 0] = float("nan"), inf
+    labels = torch.randint(0, V, (N,), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    a, b = randn(501, N), randn(502, N)
+    for ld in (V, V + 5):
+        z = torch.full((N, ld), 7.0, dtype=dtype, device="cuda")[:, :V].copy_(x)
+        _, H, lse, _, _ = dat.log_probs(z, labels)
+        dx = dat.log_probs_backward(z, labels, lse, H, a, b)
+        lp_check_gradient(z, labels, a, b, dx)
+        assert float(dx[33].abs().max()) == 0.0 and torch.isnan(dx[34:36]).all()
+        zero = torch.zeros_like(a)
+        lp_check_gradient(z, labels, a, zero, dat.log_probs_backward(z, labels, lse, None, a, None))
+        lp_check_gradient(z, labels, zero, b, dat.log_probs_backward(z, None, lse, H, None, b))
+        own = torch.full((N, ld), 7.0, dtype=dtype, device="cuda")              # in place, rows apart
+        own[:, :V] = z
+        dat.log_probs_backward(own[:, :V], labels, lse, H, a, b, dlogits=own[:, :V])
+        assert torch.equal(own[:, :V].nan_to_num(5.0), dx.nan_to_num(5.0)) and (own[:, V:] == 7.0).all()
+
+
+@pytest.mark.parametrize("V", [3, 700, 9001, 70000])
+def test_log_probs_special_rows_both_directions(dat, V):  # noqa: F811
+    """Rows that hold nothing, one class, NaN, infinities, the lowest and the largest values, and labels out of range."""
+    inf, nan = float("inf"), float("nan")
+    x, labels = lp_rows(77, 10, V, torch.float32)
+    x[0] = x[1] = -inf
+    x[1, V // 2] = -3.0
+    x[2, V - 1], x[3, 0] = nan, inf
+    x[4] = torch.finfo(torch.float32).min
+    x[5, : V - 1] = torch.finfo(torch.float32).min
+    x[6, labels[6]] = -inf
+    x[7], x[8] = 3e38, -1e-40
+    labels[1] = V // 2
+    for outside in (V, -1):
+        labels[9] = outside
+        for top in (2, min(V, 6)):
+            out = dat.log_probs(x, labels, top)
+            lp_check(x, labels, top, out)
+        a, b = randn(5, 10), randn(6, 10)
+        dx = dat.log_probs_backward(x, labels, out[2], out[1], a, b)
+        lp_check_gradient(x, labels, a, b, dx)
+        assert float(dx[0].abs().max()) == 0.0 and torch.isnan(dx[2:4]).all()

@@ -206,3 +206,18 @@ def test_buffer_stores_keep_their_data():
                     seen += 1
                     assert x[-2:] == ["0", "offen"] and lines[k + 1][:2] == ["s_nop", "3"], (name, x, lines[k + 1])
     assert seen >= 100
+
+
+def test_plain_softmax_gradient():
+    """Against the gradient from an exact lse, and rows of equal logits of any size: p = 1/V, and the gradient of a log probability sums
+    to zero over its row."""
+    rng = np.random.default_rng(1)
+    x, y, a, c = rng.standard_normal((4, 7)) * 3, np.array([0, 6, 3, -1]), rng.standard_normal(4), rng.standard_normal(4)
+    x[1, 2] = -np.inf
+    _, H, lse, _, _ = po.log_probs(x, y, 0)
+    got, p, q, h = po.softmax_gradient(x, y, a, c)
+    assert np.abs(got - po.log_probs_backward(x, y, lse, H, a, c)[0]).max() < 1e-13 and np.abs(h - H).max() < 1e-13
+    same = np.array([np.finfo(np.float32).min, -1e6, 3e38])[:, None] * np.ones((1, 5))
+    got, p, q, h = po.softmax_gradient(same, np.array([1, 2, 3]), np.ones(3), np.ones(3))
+    assert np.abs(p - 0.2).max() < 1e-15 and np.abs(got.sum(axis=1)).max() < 1e-14 and np.abs(h - np.log(5)).max() < 1e-14
+    assert np.abs(got[0] - [-0.2, 0.8, -0.2, -0.2, -0.2]).max() < 1e-14
