@@ -287,7 +287,10 @@ __global__ __launch_bounds__(NT) void gn_forward_resident_kernel(GnArgs a) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) t.load(x, i, v[i]);
   }
-  // threads add up their values' share of the mean: sums over the whole group would leave the range before the mean does
+  // A thread adds VPT VE values at most, as 2^-7 of them (exact, so the same bits), and what it hands on is its share of the mean: sums
+  // would leave the range before the mean does.
+  static_assert(VPT * VE <= 128, "of 2^-7 of their size");
+  constexpr float kPart = 0x1p-7f;
   const float share = 1.0f / ((float)a.P * (float)a.Cg);
   const int ncol = Gr::columns(a.Cg);
   const int ng = t.sv * VE / a.Cg, g_first = t.c_slice / a.Cg, w = t.sv * GV;
@@ -307,12 +310,12 @@ __global__ __launch_bounds__(NT) void gn_forward_resident_kernel(GnArgs a) {
 #pragma unroll
       for (int j = 0; j < VE; j += 2) {
         const int k = Gr::of(j);
-        acc[0][k] = dot_pairs(v[i][j / 2], 0x3f803f80u, acc[0][k]);
+        acc[0][k] = dot_pairs(v[i][j / 2], 0x3c003c00u, acc[0][k]);      // kPart
         acc[1][k] = dot_pairs(v[i][j / 2], v[i][j / 2], acc[1][k]);
       }
     }
 #pragma unroll
-    for (int k = 0; k < GV; ++k) { acc[0][k] *= share; acc[1][k] *= share; }
+    for (int k = 0; k < GV; ++k) { acc[0][k] *= share / kPart; acc[1][k] *= share; }
     const int rows = lay_columns<NT, 2, GV>(acc, t.sv, t.rows, s_red);
     sum_columns<NT, 2>(s_red, NT * GV, w, rows, ncol, ng, [&](int k, const float (&sum)[2]) {
       const float mu = sum[0], var = fmaf(-mu, mu, sum[1]), r = rstd_of(var, a.eps);
@@ -333,12 +336,12 @@ __global__ __launch_bounds__(NT) void gn_forward_resident_kernel(GnArgs a) {
 #pragma unroll
       for (int k = 0; k < GV; ++k) s[k] = 0.0f;
 #pragma unroll
-      for (int j = 0; j < VE; ++j) s[Gr::of(j)] += f[j];
+      for (int j = 0; j < VE; ++j) s[Gr::of(j)] = fmaf(f[j], kPart, s[Gr::of(j)]);
 #pragma unroll
       for (int k = 0; k < GV; ++k) acc[0][k] += s[k];
     }
 #pragma unroll
-    for (int k = 0; k < GV; ++k) acc[0][k] *= share;
+    for (int k = 0; k < GV; ++k) acc[0][k] *= share / kPart;
     const int rows = lay_columns<NT, 1, GV>(acc, t.sv, t.rows, s_red);
     sum_columns<NT, 1>(s_red, 0, w, rows, ncol, ng, [&](int k, const float (&sum)[1]) { s_mean[k] = sum[0]; });
     __syncthreads();
@@ -520,7 +523,10 @@ template <typename T, int VE, bool BACK> struct Range {   // BACK: images from t
   }
 };
 
-// Every channel's mean and sum of squared deviations within the range: part[(b, chunk)][0..1][c].
+// Every channel's mean and sum of squared deviations within the range: part[(b, chunk)][0..1][c].  A range has kHeld kT pixels at most:
+// as 2^-11 of their size (exact) their sum stays in range.
+static_assert(kHeld * kT <= 2048, "of 2^-11 of their size");
+constexpr float kRangePart = 0x1p-11f;
 template <typename T, int VE>
 __global__ __launch_bounds__(kT) void gn_stats_kernel(GnArgs a) {
   __shared__ float s_red[VE * kT], s_mean[VE * 32];      // (a slice has at most 32 vectors)
@@ -537,9 +543,9 @@ __global__ __launch_bounds__(kT) void gn_stats_kernel(GnArgs a) {
     if (r.p0 + i * r.rows < r.p1) {
       unpack<T, VE>(v[i], f);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) acc[0][j] += f[j];
+      for (int j = 0; j < VE; ++j) acc[0][j] = fmaf(f[j], kRangePart, acc[0][j]);
     }
-  const float n = (float)(r.p1 - r.chunk * a.chunk);
+  const float n = (float)(r.p1 - r.chunk * a.chunk) * kRangePart;
   const int w = r.sv * VE;
   float* part = a.part + ((int64_t)r.b * a.chunks + r.chunk) * 2 * a.C + (r.c - r.tx * VE);
   int rows = lay_columns<kT, 1, VE>(acc, r.sv, r.rows, s_red);

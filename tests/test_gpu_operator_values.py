@@ -100,6 +100,21 @@ def test_group_norm_backward_of_large_constants(dat, dtype, act):  # noqa: F811
             gn_check_backward(dat, x, dy, gamma, beta, mean, rstd, G, act, out)
 
 
+@pytest.mark.parametrize("shape", [(2, 9, 9, 40, 5), (3, 28, 28, 64, 32), (2, 8, 8, 64, 64), (1, 128, 128, 64, 2), (2, 9, 9, 35, 7), (1, 300, 300, 3, 1)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_group_norm_sums_stay_in_range(dat, shape, dtype):  # noqa: F811
+    """Values of 1e37 and 3e38, all alike: their sums are no fp32 numbers, their mean is, and nothing is left of their deviations from it but
+    the mean's rounding, whose square is none either: rstd = 0 (or 1/sqrt(eps) where the mean is exact), and y = beta both times."""
+    B, H, W, C, G = shape
+    _, gamma, beta, _ = gn_inputs(shape, dtype, 420)
+    for size in (1e37, -3e38):
+        x = torch.full(shape[:4], size, device="cuda").to(dtype)
+        y, mean, rstd = dat.group_norm_forward(x, gamma, beta, G, 0)
+        want = float(x.view(-1)[0])
+        assert_near(host(mean), np.full((B, G), want), (H * W * C // G / 64 + 32) * U * abs(want), "mean")
+        assert torch.equal(y, beta.expand(shape[:4]).to(dtype)) and torch.isfinite(rstd).all()
+
+
 # ---- log probabilities ---------------------------------------------------------------------------------------------
 def lp_check_gradient(x, labels, a, b, dx):
     """Against the softmax's own gradient.  log p is off by (K + 4 log V) U from the sum, by 2 U |lse| where it comes from an lse of at
