@@ -269,9 +269,10 @@ __device__ __forceinline__ void sum_columns(const float* s_red, int set, int w, 
 constexpr int kMaxSliceGroups = 512, kMaxSlice = 256;     // of a slice: groups, vectors
 
 // bf16 with two channels or more to a group: sums and sums of squares in one pass by dot products of pairs, exact products added
-// in fp32, and var = E x^2 - mean^2 where mean^2 <= 4 var, which costs at most a factor five of the sums' rounding errors; a slice
-// with a group whose mean is farther out takes the deviations from the mean, as all others do (fp32 has half the arithmetic for
-// its bytes).
+// in fp32, and var = E x^2 - mean^2 where mean^2 <= 4 var.  With sums that are off by a share d of their terms' magnitudes, that is off
+// by at most 14 d var: E x^2 = var + mean^2 <= 5 var by 5 d var, mean^2 by 2 |mean| d E|x| <= 2 (2 sd) d (sqrt 5 sd) = 9 d var.  A slice
+// with a group whose mean is farther out takes the deviations from the mean (d var), as all others do (fp32 has half the
+// arithmetic for its bytes).
 template <typename T, int ACT, int GV, int NT, int VPT>
 __global__ __launch_bounds__(NT) void gn_forward_resident_kernel(GnArgs a) {
   constexpr int VE = 16 / sizeof(T);

@@ -115,6 +115,51 @@ def test_group_norm_sums_stay_in_range(dat, shape, dtype):  # noqa: F811
         assert torch.equal(y, beta.expand(shape[:4]).to(dtype)) and torch.isfinite(rstd).all()
 
 
+@pytest.mark.parametrize("shape", [(2, 9, 9, 40, 5), (3, 28, 28, 64, 32), (3, 20, 20, 64, 16), (2, 56, 56, 64, 8), (2, 56, 56, 64, 32), (1, 56, 56, 256, 4),
+                                   (2, 100, 100, 64, 8), (1, 128, 128, 32, 1)])
+@pytest.mark.parametrize("offset", [0.0, 1.0, 1.8, 1.99, 2.01, 2.2])
+def test_group_norm_bf16_variance_of_large_groups(dat, shape, offset):  # noqa: F811
+    """Statistics within what a thread really adds: 16 vectors (a dot product of a pair rounds twice), then at most 64 terms in LDS and
+    trees of 6 and 6 lanes, 4 for shares and the square; both sides of the change from E x^2 - mean^2, which multiplies the sums' relative
+    error by (var + mean^2) / var + 2 |mean| E|x| / var <= 5 + 4 sqrt 5 < 14."""
+    B, H, W, C, G = shape
+    Cg = C // G
+    entries = 1 if Cg % 8 == 0 else 8 // Cg if Cg > 1 and 8 % Cg == 0 else 8
+    K = 128 / entries + 64 + 16
+    x = (randn(430, B, H, W, C) + offset).to(torch.bfloat16)
+    _, mean, rstd = dat.group_norm_forward(x, None, None, G, 0)
+    m, r = po.gn_stats(host(x), G, 1e-5)
+    size = np.abs(host(x)).reshape(B, -1, G, Cg).mean(axis=(1, 3))
+    assert_near(host(mean), m, K * U * size, "mean")
+    assert_near(host(rstd), r, (14 * K / 2 + 4) * U * r, "rstd")
+
+
+@pytest.mark.parametrize("shape", [(40, 9, 9, 40, 5), (40, 28, 28, 64, 32), (40, 56, 56, 64, 8), (40, 56, 56, 64, 32), (40, 15, 17, 96, 4), (40, 100, 100, 64, 8),
+                                   (40, 128, 128, 32, 1), (40, 23, 29, 35, 7), (40, 100, 101, 6, 2)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_group_norm_counts_every_value(dat, shape, dtype):  # noqa: F811
+    """Groups of zeros with a single one, at another pixel of every image (the first and last ones among them): what a sum leaves out or
+    counts twice is all of it.  eps = 0: rstd = 1 / sqrt((1 - 1/n) / n)."""
+    B, H, W, C, G = shape
+    P, Cg = H * W, C // G
+    n = P * Cg
+    gen = torch.Generator().manual_seed(3)
+    pixel = torch.cat([torch.arange(10), torch.arange(P - 10, P), torch.randint(0, P, (B - 20,), generator=gen)])
+    channel = torch.randint(0, Cg, (B, G), generator=gen) + Cg * torch.arange(G)[None, :]
+    x = torch.zeros(B, P, C)
+    x[torch.arange(B)[:, None], pixel[:, None], channel] = 1.0
+    x = x.view(shape[:4]).cuda().to(dtype)
+    _, mean, rstd = dat.group_norm_forward(x, None, None, G, 0, eps=0.0)
+    assert_near(host(mean), np.full((B, G), 1.0 / n), 4 * U / n, "mean")
+    want = 1 / np.sqrt((1 - 1 / n) / n)
+    # (the zeros' deviations have 1/n of the sum: their roundings, at most n of them, are U of it)
+    assert_near(host(rstd), np.full((B, G), want), 16 * U * want, "rstd")
+    _, dgamma, dbeta = dat.group_norm_backward(x, x, None, None, mean, rstd, G, 0)
+    count = x.float().sum(dim=(0, 1, 2))
+    assert torch.equal(dbeta, count)                                     # (small whole numbers: exact)
+    assert_near(host(dgamma), host(count) * (1 - 1 / n) * want, (B + 16) * U * host(count) * want, "dgamma")
+
+
 # ---- log probabilities ---------------------------------------------------------------------------------------------
 def lp_check_gradient(x, labels, a, b, dx):
     """Against the softmax's own gradient.  log p is off by (K + 4 log V) U from the sum, by 2 U |lse| where it comes from an lse of at
@@ -191,3 +236,28 @@ def test_log_probs_special_rows_both_directions(dat, V):  # noqa: F811
         dx = dat.log_probs_backward(x, labels, out[2], out[1], a, b)
         lp_check_gradient(x, labels, a, b, dx)
         assert float(dx[0].abs().max()) == 0.0 and torch.isnan(dx[2:4]).all()
+
+
+@pytest.mark.parametrize("V", [10, 16, 17, 63, 64, 65, 256, 257, 1000, 1025, 8193, 50021, 131075])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_log_probs_counts_every_logit(dat, V, dtype):  # noqa: F811
+    """One logit of 0 among logits of -64 (e^-64 < 2^-92), at the first and last places and elsewhere: it is the whole sum, in few rows
+    (parts of a row, a workgroup) and in many (lanes of a wavefront)."""
+    at = torch.cat([torch.arange(min(V, 17)), torch.arange(max(0, V - 17), V), torch.randint(0, V, (30,), generator=torch.Generator().manual_seed(V))])
+    few = len(at)
+    for repeat in (1, 20 if V <= 1024 else 1):
+        where = at.repeat(repeat).cuda()
+        N = few * repeat
+        for ld in (V, V + 3):
+            x = torch.full((N, ld), 7.0, dtype=dtype, device="cuda")[:, :V].fill_(-64.0)
+            x[torch.arange(N, device="cuda"), where] = 0.0
+            labels = where.to(torch.int32)
+            logp, H, lse, tl, ti = dat.log_probs(x, labels, 1)
+            for t in (logp, lse, tl):
+                assert float(t.abs().max()) <= 2 * U
+            assert torch.equal(ti[:, 0], labels) and float(H.abs().max()) <= 2 * U
+            dx = dat.log_probs_backward(x, ((where + 1) % V).to(torch.int32), lse, None, torch.ones(N, device="cuda"), None)
+            want = torch.zeros_like(x)                                   # the other label: 1 there, -1 at the only likely class
+            want[torch.arange(N, device="cuda"), (where + 1) % V] = 1.0
+            want[torch.arange(N, device="cuda"), where] = -1.0
+            assert float((dx - want).abs().max()) <= 8 * U
