@@ -288,7 +288,8 @@ dat_status dat_model_adamw_update(dat_model* m, const float* grads, int state_bi
  *   wrote it; p_i = exp(x_i - lse) where |lse| <= 64, whose rounding moves p_i by at most 2^-19 of itself.  Beyond, where fp32 keeps too
  *   little of the sum beside the maximum, both are taken from the row again (a second read; one workgroup does such a row).
  *   p_i = 0 gives no entropy term; a row with nothing allowed gets zeros, one whose lse is NaN gets NaN.  dlogits may
- *   be the logits themselves (then ldd = ld); elements between the rows are not touched.
+ *   be the logits themselves (then ldd = ld), or lie between their rows, but share no other element with them (DAT_ERR_ARG where ldd = ld,
+ *   the caller's to see to otherwise); elements between the rows are not touched.
  * workspace: device, 16-byte aligned, dat_log_probs_workspace(N, V, top) bytes (may be 0, then NULL is allowed); nothing in it
  * outlives the call.  Asynchronous on `stream`, no allocation.  N = 0: nothing happens.  DAT_ERR_ARG: null or misaligned
  * pointers, N or top negative, top > DAT_MAX_TOP, V < 1, ld < V, a workspace that is too small; DAT_ERR_SHAPE: V > 2^30, N > 2^31-1, or
@@ -314,10 +315,10 @@ dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype, int64_t N
  *   operation (the forward call may have rounded a z next to zero to the other side);
  *   dbeta = sum dz, dgamma = sum dz xhat (device fp32 [C], both NULL to skip; written, not added to), sums in fp32 in a fixed order
  *   (the same bits on every call);  dx = rstd (h - mean(h) - xhat mean(h xhat)), h = gamma dz, means over the group.  y is not needed.
- * dx may be dy (same buffer), y may be x.  workspace: device, 16-byte aligned, dat_group_norm_workspace(pass, ...) bytes (pass 0 forward, 1
+ * dx may be dy or x (same buffer), y may be x; buffers that overlap otherwise are refused.  workspace: device, 16-byte aligned, dat_group_norm_workspace(pass, ...) bytes (pass 0 forward, 1
  * backward; may be 0, then NULL is allowed); nothing in it outlives the call.  Asynchronous on `stream`, no allocation.
  * B = 0: no output but dgamma = dbeta = 0.  DAT_ERR_ARG: null or misaligned pointers, sizes below 1 (B below 0), groups that
- * do not divide C, unknown act or dtype, eps negative or NaN, a workspace that is too small; DAT_ERR_SHAPE: H*W*C, B*groups or
+ * do not divide C, outputs that overlap inputs (above), unknown act or dtype, eps negative or NaN, a workspace that is too small; DAT_ERR_SHAPE: H*W*C, B*groups or
  * B*C above 2^30, or tiles (groups, ranges of pixels) for more than a launch's 2^32 threads, 256 to 1024 each: from 2^22 on. */
 typedef enum { DAT_ACT_NONE = 0, DAT_ACT_RELU = 1, DAT_ACT_SILU = 2 } dat_act;
 size_t dat_group_norm_workspace(int pass, dat_dtype dtype, int B, int H, int W, int C, int groups);

@@ -882,6 +882,7 @@ extern "C" dat_status dat_group_norm_forward(const void* x, const float* gamma, 
   const size_t width = dtype == DAT_BF16 ? 2 : 4, need = dat_group_norm_workspace(0, dtype, B, H, W, C, groups);
   if (!aligned(x, width) || !aligned(y, width) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return DAT_ERR_ARG;
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return DAT_ERR_ARG;
+  if (overlaps(x, y, (size_t)B * H * W * C * width)) return DAT_ERR_ARG;
   if (B == 0) return DAT_OK;
   const Plan p = plan_of(false, dtype, aligned(x, 16) && aligned(y, 16), B, H * W, C, groups);
   GnArgs a{x, nullptr, gamma, beta, nullptr, nullptr, y, mean, rstd, (float*)workspace, B, H * W, C, groups, C / groups,
@@ -910,6 +911,7 @@ extern "C" dat_status dat_group_norm_backward(const void* x, const void* dy, con
   if (!aligned(x, width) || !aligned(dy, width) || !aligned(dx, width) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
       !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return DAT_ERR_ARG;
   if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return DAT_ERR_ARG;
+  if (overlaps(x, dx, (size_t)B * H * W * C * width) || overlaps(dy, dx, (size_t)B * H * W * C * width)) return DAT_ERR_ARG;
   hipStream_t st = (hipStream_t)stream;
   const Plan p = plan_of(true, dtype, aligned(x, 16) && aligned(dy, 16) && aligned(dx, 16), B, H * W, C, groups);
   GnArgs a{x, dy, gamma, beta, mean, rstd, dx, nullptr, nullptr, (float*)workspace, B, H * W, C, groups, C / groups,

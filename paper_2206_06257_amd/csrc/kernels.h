@@ -212,6 +212,12 @@ struct LambParams {
 dat_status launch_lamb(float* theta, const float* g, float* m, float* v, float* u, const int64_t* off, int T, int64_t d,
                        const LambParams& hp, double* norms, hipStream_t st);
 
+// Buffers of `bytes` that share some bytes, but not all.
+inline bool overlaps(const void* p, const void* q, size_t bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a != b && (a > b ? a - b : b - a) < bytes;
+}
+
 // A launch has fewer than 2^32 threads along a dimension.
 inline bool fits_launch(int64_t blocks, int64_t threads) { return blocks <= INT32_MAX && blocks * threads <= UINT32_MAX; }
 

@@ -587,6 +587,14 @@ dat_status check_rows(const void* x, dat_dtype dtype, int64_t N, int64_t V, int6
   if (V > (1ll << 30) || N > INT32_MAX || (N > 0 && ld > INT64_MAX / 8 / N)) return DAT_ERR_SHAPE;
   return DAT_OK;
 }
+
+// N rows of `row` bytes, `step` bytes apart, at p and at q: share some bytes, but not all.  (step N < 2^63: check_rows.)
+bool rows_overlap(const void* p, const void* q, uint64_t N, uint64_t row, uint64_t step) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  const uint64_t d = a > b ? a - b : b - a;
+  if (d == 0 || d >= (N - 1) * step + row) return false;
+  return d % step < row || (step - d % step < row && d < (N - 1) * step);      // beside the same row, and beside the next one
+}
 }  // namespace
 
 extern "C" dat_status dat_log_probs(const void* logits, dat_dtype dtype, int64_t N, int64_t V, int64_t ld, const int32_t* labels,
@@ -626,6 +634,8 @@ extern "C" dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype
   const int64_t per = kGradT * kGradV * 16 / (dtype == DAT_BF16 ? 2 : 4), each = lanes ? 1 : (V + per - 1) / per;
   const int64_t blocks = lanes ? (N + kGradT / lanes - 1) / (kGradT / lanes) : N * each;
   if (!fits_launch(blocks, kGradT)) return DAT_ERR_SHAPE;
+  const uint64_t width = dtype == DAT_BF16 ? 2 : 4;
+  if (ld == ldd && rows_overlap(logits, dlogits, N, V * width, ld * width)) return DAT_ERR_ARG;
   if (dtype == DAT_BF16) launch_log_probs_grad<bf16_t>(lanes, (unsigned)blocks, (unsigned)each, g, st);
   else launch_log_probs_grad<float>(lanes, (unsigned)blocks, (unsigned)each, g, st);
   DAT_LAUNCH_CHECK();

@@ -160,6 +160,17 @@ def test_group_norm_counts_every_value(dat, shape, dtype):  # noqa: F811
     assert_near(host(dgamma), host(count) * (1 - 1 / n) * want, (B + 16) * U * host(count) * want, "dgamma")
 
 
+@pytest.mark.parametrize("shape", [(3, 14, 14, 64, 16), (1, 128, 128, 64, 2), (2, 9, 9, 35, 7)])
+def test_group_norm_gradient_in_place_of_the_input(dat, shape):  # noqa: F811
+    G = shape[4]
+    x, gamma, beta, dy = gn_inputs(shape, torch.bfloat16, 440)
+    _, mean, rstd = dat.group_norm_forward(x, gamma, beta, G, 2)
+    want = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, G, 2)
+    own = x.clone()
+    got = dat.group_norm_backward(own, dy, gamma, beta, mean, rstd, G, 2, dx=own)
+    assert got[0] is own and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 # ---- log probabilities ---------------------------------------------------------------------------------------------
 def lp_check_gradient(x, labels, a, b, dx):
     """Against the softmax's own gradient.  log p is off by (K + 4 log V) U from the sum, by 2 U |lse| where it comes from an lse of at
@@ -261,3 +272,17 @@ def test_log_probs_counts_every_logit(dat, V, dtype):  # noqa: F811
             want[torch.arange(N, device="cuda"), (where + 1) % V] = 1.0
             want[torch.arange(N, device="cuda"), where] = -1.0
             assert float((dx - want).abs().max()) <= 8 * U
+
+
+def test_log_probs_gradient_between_the_rows_of_the_logits(dat):  # noqa: F811
+    for N, V in ((5, 10), (300, 77), (3, 9001)):
+        buf = torch.full((N, 2 * V + 3), 7.0, device="cuda")
+        x, labels = lp_rows(450, N, V, torch.float32)
+        buf[:, 1:V + 1] = x
+        out = dat.log_probs(buf[:, 1:V + 1], labels)
+        a = randn(451, N)
+        dat.log_probs_backward(buf[:, 1:V + 1], labels, out[2], None, a, None, dlogits=buf[:, V + 1:2 * V + 1])
+        assert torch.equal(buf[:, 1:V + 1], x) and (buf[:, 0] == 7.0).all() and (buf[:, 2 * V + 1:] == 7.0).all()
+        assert torch.equal(buf[:, V + 1:2 * V + 1], dat.log_probs_backward(x, labels, out[2], None, a, None))
+        with pytest.raises(dat.DatError):
+            dat.log_probs_backward(buf[:, 1:V + 1], labels, out[2], None, a, None, dlogits=buf[:, V:2 * V])

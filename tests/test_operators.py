@@ -221,3 +221,28 @@ def test_plain_softmax_gradient():
     got, p, q, h = po.softmax_gradient(same, np.array([1, 2, 3]), np.ones(3), np.ones(3))
     assert np.abs(p - 0.2).max() < 1e-15 and np.abs(got.sum(axis=1)).max() < 1e-14 and np.abs(h - np.log(5)).max() < 1e-14
     assert np.abs(got[0] - [-0.2, 0.8, -0.2, -0.2, -0.2]).max() < 1e-14
+
+
+def test_outputs_that_overlap_inputs_are_refused():
+    n = 2 * 4 * 4 * 16 * 4
+    for d in (4, 16, n - 4):
+        assert gn_fwd(y=P * 4 + d, x=P * 4) == 1 and gn_fwd(y=P * 4 - d, x=P * 4) == 1
+        assert gn_bwd(dx=P * 4 + d, x=P * 4, dy=P * 9) == 1 and gn_bwd(dx=P * 4 - d, dy=P * 4, x=P * 9) == 1
+    for d in (4, 36, 40, 44, 3 * 40 - 4):                  # three rows of ten, one behind the other
+        assert lp_bwd(dx=P + d) == 1 and lp_bwd(x=P + d, dx=P) == 1
+    for d in (4, 36, 48, 52, 88 + 4, 2 * 84 + 36):         # rows apart: 40 of 84 bytes
+        assert lp_bwd(dx=P + d, ld=21, ldd=21) == 1 and lp_bwd(x=P + d, dx=P, ld=21, ldd=21) == 1
+    assert lp_bwd(N=1, dx=P + 36, ld=1000, ldd=1000) == 1 and lp_bwd(dtype=1, dx=P + 2) == 1
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_rows_overlap_agrees_with_sets(seed):
+    """The refusals of interleaved rows, against the sets of elements (a copy of the rule: nothing may be launched here)."""
+    rng = np.random.default_rng(seed)
+    for _ in range(2000):
+        N, row = int(rng.integers(1, 5)), int(rng.integers(1, 7))
+        step, d = row + int(rng.integers(0, 8)), int(rng.integers(0, 60))
+        one = {n * step + i for n in range(N) for i in range(row)}
+        share = d != 0 and bool(one & {e + d for e in one})
+        rule = d != 0 and d < (N - 1) * step + row and (d % step < row or (step - d % step < row and d < (N - 1) * step))
+        assert share == rule, (N, row, step, d)
