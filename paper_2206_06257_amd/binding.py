@@ -448,8 +448,10 @@ class _On:
 
 def _want(name, t, dtypes, shape=None, contiguous=True, optional=False):
     """Checks a tensor argument of the calls below."""
-    if t is None and optional:
-        return
+    if t is None:
+        if optional:
+            return
+        raise ValueError("%s: needed here" % name)
     if t.dtype not in dtypes or (shape is not None and t.shape != shape) or (contiguous and not t.is_contiguous()):
         raise ValueError("%s: %s %s%s, expected %s %s" % (name, t.dtype, tuple(t.shape), "" if t.is_contiguous() else " (not contiguous)",
                                                           " or ".join(str(d) for d in dtypes), "" if shape is None else tuple(shape)))

@@ -246,3 +246,12 @@ def test_rows_overlap_agrees_with_sets(seed):
         share = d != 0 and bool(one & {e + d for e in one})
         rule = d != 0 and d < (N - 1) * step + row and (d % step < row or (step - d % step < row and d < (N - 1) * step))
         assert share == rule, (N, row, step, d)
+
+
+def test_binding_names_what_is_missing():
+    f, y, n, x, c = torch.zeros(4, 10), torch.zeros(4, dtype=torch.int32), torch.zeros(4), torch.zeros(2, 4, 4, 16), torch.zeros(16)
+    for name, call in (("labels", lambda: b.log_probs_backward(f, None, n, None, n)), ("entropy", lambda: b.log_probs_backward(f, y, n, None, None, n)),
+                       ("lse", lambda: b.log_probs_backward(f, y, None, None, n)), ("dy", lambda: b.group_norm_backward(x, None, c, c, c, c, 4)),
+                       ("mean", lambda: b.group_norm_backward(x, x, c, c, None, c, 4)), ("grads", lambda: b.adamw_update(n, None, n, n, y, 0.1, 1))):
+        with pytest.raises(ValueError, match=name):
+            call()
