@@ -3,8 +3,8 @@
 // Both widths walk the same slots: block j of 256 elements of tensor t has the slot off[t]/256 + t + j, strictly increasing in
 // (t, j) because floor((a+n)/256) + 1 >= floor(a/256) + ceil(n/256); a wavefront takes a slot, a lane four consecutive elements.
 // Streaming, bound by HBM: 28 bytes an element with 32-bit moments, 16 with 8-bit ones (+2 for the bf16 copy).  46.2 M parameters
-// with the copy, 32 bits: 268 us = 5.2 TB/s; 25.6 M, 8 bits: 98 us = 4.7 TB/s (beside the memory about 65 vector instructions an
-// element: IEEE square root and quotient, a quarter of a Philox block).  One block a wavefront: four behind one search of the
+// with the copy, 32 bits: 270 us = 5.1 TB/s; 25.6 M, 8 bits: 98 us = 4.7 TB/s (beside the memory 117 vector instructions an
+// element, 77 % of the cycles: IEEE square root and quotient, a quarter of a Philox block).  One block a wavefront: four behind one search of the
 // table take 129 and 340 us.
 #include "kernels.h"
 #include "tensor_table.h"

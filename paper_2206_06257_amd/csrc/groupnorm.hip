@@ -10,10 +10,10 @@
 //   split     an image's slice is too large for that: partial sums over ranges of pixels, a small kernel that joins them, and a
 //             second pass over the tensors, from the last image to the first: the last-level cache still holds what the first
 //             pass read last.
-// Forward, resident: 256 x 56 x 56 x 256 bf16 202 us = 4.1 TB/s (one workgroup a compute unit: nothing moves while it joins its
-// sums), 512 x 32 x 32 x 64 27 us = 5.0 TB/s; split (256 x 112 x 112 x 64) 264 us, three passes at 4.7 TB/s.
-// Backward, resident: 256 x 28 x 28 x 512 bf16 146 us = 4.2 TB/s; split: 85 x 112 x 112 x 64 with SiLU 158 us, five passes at
-// 4.3 TB/s (sums 69 us, half of it arithmetic; apply 78 us = 5.2 TB/s).
+// Forward, resident: 256 x 56 x 56 x 256 bf16 200 us = 4.1 TB/s (one workgroup a compute unit: nothing moves while it joins its
+// sums), 512 x 32 x 32 x 64 28 us = 4.8 TB/s; split (256 x 112 x 112 x 64) 260 us, three passes at 4.7 TB/s.
+// Backward, resident: 256 x 28 x 28 x 512 bf16 144 us = 4.3 TB/s; split: 85 x 112 x 112 x 64 with SiLU 158 us, five passes at
+// 4.3 TB/s (sums 70 us = 3.9 TB/s, the vector units issuing for half of it; apply 79 us = 5.2 TB/s).
 #include <type_traits>
 #include "kernels.h"
 #include "lanes.h"
@@ -78,7 +78,8 @@ template <typename T> __device__ __forceinline__ void pack4(const float (&f)[4],
   }
 }
 // Held vectors are unpacked anew in every pass: without this the compiler unpacks them where they are loaded, or keeps the
-// unpacked values of one pass for the next, twice the registers, and spills.
+// unpacked values of one pass for the next, twice the registers, and spills.  (With 1024 threads, 128 registers each, two forms
+// spill all the same: bf16 forward with four groups to a vector 29 registers, backward with eight and an activation 6.)
 __device__ __forceinline__ void forget(u32x4& v) { asm volatile("" : "+v"(v)); }
 __device__ __forceinline__ void forget(float& v) { asm volatile("" : "+v"(v)); }
 
@@ -768,7 +769,8 @@ Plan plan_of(bool backward, dat_dtype dtype, bool vectors, int B, int P, int C, 
     // compute unit, each at its own stage.  Rows of a slice: 128 bytes forward (512 x 32 x 32 x 64 bf16 28.6 us against 35.6 with
     // 64, 128 x 32 x 32 x 160 fp32 48.6 against 60.5, 256 x 40 x 40 x 256 101.3 against 101.1), 64 where the image does not fit
     // so, and backward, where the workgroup that takes 128 is alone on its unit (256 x 28 x 28 x 512 146 us against 189).  Wider
-    // where the image is small (256 x 7 x 7 x 2048 41 -> 23 us), narrower where there would be few tiles for 256 compute units.
+    // where the image is small (256 x 7 x 7 x 2048 41 -> 23 us), narrower where there would be few tiles for 256 compute units, but not
+    // where 64 bytes do not fit: such maps (bf16 backward from 56 x 56 up) go the split way, slices of 32 or 16 are not tried.
     static const int fwd[][2] = {{256, 2}, {256, 8}, {256, 16}, {512, 16}, {1024, 16}}, bwd[][2] = {{256, 2}, {256, 8}, {512, 8}, {1024, 8}};
     const int (*sizes)[2] = backward ? bwd : fwd;
     const int count = backward ? 4 : 5, nv = p.nv;

@@ -2,9 +2,9 @@
 //
 // With M = max x, s = sum 2^t and w = sum t 2^t, t = (x - M) log2 e:  lse = M + ln s,  logp_y = (x_y - M) - ln s,
 // H = ln s - ln 2 w / s.  The logits are read once: a workgroup holds its row, or a part of it, in registers; what comes of the
-// parts of a row is joined by a second, small kernel.  Bound by HBM (one read), beside it about twelve instructions a logit, four
-// of them the exponential's: 2039 x 50021 bf16 with eight alternatives 57 us = 3.6 TB/s (two workgroups of 1024 threads on a
-// compute unit; 64 us with two of 512 that hold twice as much).  Few long rows are latency: 3 x 131075 with 20 alternatives 12.4 us
+// parts of a row is joined by a second, small kernel.  Bound by HBM (one read) and the vector units, twenty instructions a logit in
+// bf16, alternatives included: 2039 x 50021 bf16 with eight of them 57 us = 3.6 TB/s, issuing for 82 % of it (two workgroups of 1024
+// threads on a compute unit; 64 us with two of 512 that hold twice as much).  Few long rows are latency: 3 x 131075 with 20 alternatives 12.4 us
 // in two launches.
 //
 // Alternatives are ordered by one 64-bit key, the logit (as an ordered integer) above the complement of the index, so that equal
