@@ -310,7 +310,8 @@ dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype, int64_t N
  *   act: none, ReLU max(z, 0), SiLU z/(1 + exp(-z)).  In fp32; y is rounded once to `dtype`.
  * gamma, beta: device fp32 [C], both NULL for 1 and 0.  mean, rstd: device fp32 [B][groups], written by the forward call and read by the
  * backward call.  The variance is that of deviations from the mean (bf16: the difference E x^2 - mean^2, from exact squares, where
- * mean^2 <= 4 var); where it is no fp32 number (certain up to deviations of 2^58) rstd is 0.  A NaN or an infinity in x spoils its own image's group (mean, rstd, y, dx) and what sums over it.
+ * mean^2 <= 4 var); where it is no fp32 number (certain up to deviations of 2^58) rstd is 0, and
+ * where eps is 0 and the variance 0 in fp32 rstd is infinite.  A NaN or an infinity in x spoils its own image's group (mean, rstd, y, dx) and what sums over it.
  *   dat_group_norm_backward:  dz = dy act'(z), ReLU'(z) = [z > 0], z = ((x - mean) rstd) gamma + beta with one fp32 rounding per
  *   operation (the forward call may have rounded a z next to zero to the other side);
  *   dbeta = sum dz, dgamma = sum dz xhat (device fp32 [C], both NULL to skip; written, not added to), sums in fp32 in a fixed order
