@@ -467,8 +467,14 @@ __global__ __launch_bounds__(NT) void gn_backward_resident_kernel(GnArgs a) {
     s_g[0][k] = __fdiv_rn(sum[0], n); s_g[1][k] = __fdiv_rn(sum[1], n);
   });
   __syncthreads();
-  // dx = rstd (gamma dz - c1 - xhat c2) = (rstd gamma) dz + ((x - mean) (-rstd^2 c2) - rstd c1)
+  // dx = rstd (gamma dz - c1 - xhat c2) = (rstd gamma) dz + ((x - mean) (-rstd^2 c2) - rstd c1).  A group of one value does not depend on
+  // it: the terms cancel but for their rounding, and with rstd = 0 altogether (x - mean is 0, z = beta all the same; images of one pixel
+  // take the smallest tile).
   float q1[GV], q2[GV];
+  if (VPT == 2 && n == 1.0f) {
+#pragma unroll
+    for (int k = 0; k < GV; ++k) rstd[k] = 0.0f;
+  }
 #pragma unroll
   for (int k = 0; k < GV; ++k) { q1[k] = -rstd[k] * s_g[0][g[k] - g_first]; q2[k] = -(rstd[k] * rstd[k]) * s_g[1][g[k] - g_first]; }
   float scale[VE];
@@ -714,7 +720,7 @@ __global__ __launch_bounds__(kT) void gn_grad_apply_kernel(GnArgs a, const float
 #pragma unroll
   for (int j = 0; j < VE; ++j) {
     const int64_t g = (int64_t)r.b * a.G + (r.c + j) / a.Cg;
-    mean[j] = a.mean_in[g]; rstd[j] = a.rstd_in[g];
+    mean[j] = a.mean_in[g]; rstd[j] = a.P * a.Cg == 1 ? 0.0f : a.rstd_in[g];      // (as in the resident kernel)
     q1[j] = -rstd[j] * join[2 * g]; q2[j] = -(rstd[j] * rstd[j]) * join[2 * g + 1];
   }
 #pragma unroll 4

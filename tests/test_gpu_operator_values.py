@@ -171,6 +171,27 @@ def test_group_norm_gradient_in_place_of_the_input(dat, shape):  # noqa: F811
     assert got[0] is own and all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("shape", [(5, 1, 1, 64, 64), (98, 1, 1, 320, 320), (5, 1, 1, 35, 35)])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_group_norm_of_single_values(dat, shape, act, dtype):  # noqa: F811
+    """A group of one value: y = act(beta) whatever the value, so its gradient is 0, and the scale's."""
+    x, gamma, beta, dy = gn_inputs(shape, dtype, 460)
+    y, mean, rstd = dat.group_norm_forward(x, gamma, beta, shape[4], act)
+    assert_near(host(y), np.broadcast_to(po.gn_act(host(beta), act), shape[:4]), (half(dtype) + 16 * U) * (np.abs(host(beta)) + 1), "y")
+    dx, dgamma, dbeta = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, shape[4], act)
+    assert int(torch.count_nonzero(dx)) == 0 and int(torch.count_nonzero(dgamma)) == 0 and torch.isfinite(dx).all()
+    slope = torch.ones_like(beta) if act == 0 else (beta > 0).float() if act == 1 else torch.sigmoid(beta) * (1 + beta * (1 - torch.sigmoid(beta)))
+    terms = dy.float()[:, 0, 0] * slope
+    assert_near(host(dbeta), host(terms.double().sum(dim=0)), 64 * U * host(terms.abs().sum(dim=0)) + 32 * U, "dbeta")
+    x[1, 0, 0, 3], x[2, 0, 0, 4] = float("nan"), float("inf")
+    y, mean, rstd = dat.group_norm_forward(x, gamma, beta, shape[4], act)
+    dx = dat.group_norm_backward(x, dy, gamma, beta, mean, rstd, shape[4], act)[0]
+    bad = torch.zeros(shape[:4], dtype=torch.bool, device="cuda")
+    bad[1, 0, 0, 3] = bad[2, 0, 0, 4] = True
+    assert torch.isnan(dx[bad]).all() and int(torch.count_nonzero(dx[~bad])) == 0
+
+
 # ---- log probabilities ---------------------------------------------------------------------------------------------
 def lp_check_gradient(x, labels, a, b, dx):
     """Against the softmax's own gradient.  log p is off by (K + 4 log V) U from the sum, by 2 U |lse| where it comes from an lse of at
