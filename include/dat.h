@@ -310,17 +310,18 @@ dat_status dat_log_probs_backward(const void* logits, dat_dtype dtype, int64_t N
  *   act: none, ReLU max(z, 0), SiLU z/(1 + exp(-z)).  In fp32; y is rounded once to `dtype`.
  * gamma, beta: device fp32 [C], both NULL for 1 and 0.  mean, rstd: device fp32 [B][groups], written by the forward call and read by the
  * backward call.  The variance is that of deviations from the mean (bf16: the difference E x^2 - mean^2, from exact squares, where
- * mean^2 <= 4 var); where it is no fp32 number (certain up to deviations of 2^58) rstd is 0, and
- * where eps is 0 and the variance 0 in fp32 rstd is infinite.  A NaN or an infinity in x spoils its own image's group (mean, rstd, y, dx) and what sums over it.
+ * mean^2 <= 4 var); where it is no fp32 number (it is one up to deviations of 2^58) rstd is 0, and where eps is 0 and the variance 0 in
+ * fp32 rstd is infinite.  A NaN or an infinity in x spoils its own image's group (mean, rstd, y, dx) and what sums over it.
  *   dat_group_norm_backward:  dz = dy act'(z), ReLU'(z) = [z > 0], z = ((x - mean) rstd) gamma + beta with one fp32 rounding per
  *   operation (the forward call may have rounded a z next to zero to the other side);
  *   dbeta = sum dz, dgamma = sum dz xhat (device fp32 [C], both NULL to skip; written, not added to), sums in fp32 in a fixed order
  *   (the same bits on every call);  dx = rstd (h - mean(h) - xhat mean(h xhat)), h = gamma dz, means over the group.  y is not needed.
- * dx may be dy or x (same buffer), y may be x; buffers that overlap otherwise are refused.  workspace: device, 16-byte aligned, dat_group_norm_workspace(pass, ...) bytes (pass 0 forward, 1
- * backward; may be 0, then NULL is allowed); nothing in it outlives the call.  Asynchronous on `stream`, no allocation.
+ * dx may be dy or x (same buffer), y may be x; buffers that overlap otherwise are refused.  workspace: device, 16-byte aligned,
+ * dat_group_norm_workspace(pass, ...) bytes (pass 0 forward, 1 backward; may be 0, then NULL is allowed); nothing in it outlives the
+ * call.  Asynchronous on `stream`, no allocation.
  * B = 0: no output but dgamma = dbeta = 0.  DAT_ERR_ARG: null or misaligned pointers, sizes below 1 (B below 0), groups that
- * do not divide C, outputs that overlap inputs (above), unknown act or dtype, eps negative or NaN, a workspace that is too small; DAT_ERR_SHAPE: H*W*C, B*groups or
- * B*C above 2^30, or tiles (groups, ranges of pixels) for more than a launch's 2^32 threads, 256 to 1024 each: from 2^22 on. */
+ * do not divide C, outputs that overlap inputs (above), unknown act or dtype, eps negative or NaN, a workspace that is too small;
+ * DAT_ERR_SHAPE: H*W*C, B*groups or B*C above 2^30, or tiles (groups, ranges of pixels) for more than a launch's 2^32 threads, 256 to 1024 each: from 2^22 on. */
 typedef enum { DAT_ACT_NONE = 0, DAT_ACT_RELU = 1, DAT_ACT_SILU = 2 } dat_act;
 size_t dat_group_norm_workspace(int pass, dat_dtype dtype, int B, int H, int W, int C, int groups);
 dat_status dat_group_norm_forward(const void* x, const float* gamma, const float* beta, dat_dtype dtype, int B, int H, int W,

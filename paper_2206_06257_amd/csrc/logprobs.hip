@@ -385,8 +385,8 @@ __device__ __forceinline__ float grad1(float x, int i, const RowGrad& r) {
 constexpr int kGradT = 256, kGradV = 4;      // vectors a thread
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Vector { T x[16 / sizeof(T)]; };
 
-// An lse far from zero has lost what it knows of the sum (beside 1e6 a sixteenth of log s, at the type's lowest value all of it), and
-// p = e^(x - lse) with it.  Up to 64 its rounding moves p by at most 2^-19; beyond, maximum and sum are taken from the row again,
+// An lse far from zero has lost what it knows of the sum (at 1e6 it is rounded to sixteenths, at the type's lowest value nothing is
+// left), and p = e^(x - lse) with it.  Up to 64 its rounding moves p by at most 2^-19; beyond, maximum and sum are taken from the row again,
 // p = e^((x - M) - ln s), by the threads of one workgroup or the lanes of a short row: a second read, for such rows alone (all rows
 // at lse = 100: 1021 x 32771 fp32 90 us against 45, 16384 x 1000 37 against 21, 64 x 262144 379 against 21).
 // (By its bits, as numbers of a scalar register: finite, and more than 64 in size.)
