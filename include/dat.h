@@ -332,6 +332,45 @@ dat_status dat_group_norm_backward(const void* x, const void* dy, const float* g
                                    void* dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
                                    void* stream);
 
+/* ---- attention with its gradients ---------------------------------------------------------------------------
+ * Tensors of heads: element (b, t, h, d) is data[b * batch + t * token + h * head + d], strides in elements (0 repeats; a dimension of
+ * one has any); data 16-byte aligned, strides multiples of 16 bytes.  q, o, d_o, dq: [B][Sq][H][D]; k, v, dk, dv: [B][Sk][Hkv][D]; fp32
+ * or bf16 by `dtype`; query head h reads key head h / (H / Hkv).  With offsets (device int32 [B + 1], not decreasing, both or neither)
+ * the sequences are packed: Sq and Sk are all tokens, sequence b has the queries offsets_q[b] .. offsets_q[b + 1] - 1 and the keys
+ * offsets_k[b] .. offsets_k[b + 1] - 1 (either may be none), `batch` is not read; tokens in no sequence are not read and their rows of the
+ * outputs stay as they were.  Offsets beyond the tensors are taken as the tensors' ends.
+ * Query i of a sequence of Lq queries and Lk keys stands at c = i + Lk - Lq and sees the keys j with c - left <= j <= c + right; -1: no
+ * limit on that side; left = -1, right = 0 is causal.
+ *   forward:   S = scale q k^T over what a row sees, lse = log sum_j exp S_j, P = exp(S - lse), o = P v; a row that sees nothing has o = 0,
+ *              lse = -inf.  lse: device fp32 [B][H][Sq] ([H][Sq] packed).
+ *   backward:  D = sum_d d_o o, dP = d_o v^T, dS = P (dP - D); dq = scale dS k, dk = scale dS^T q and dv = P^T d_o, over all heads that
+ *              share the key head.  P is made again from q, k and lse; sums in a fixed order (the same bits on every call).
+ * Sums, statistics and S, P, dP, dS in fp32; bf16 rounds P and dS to bf16 where they enter a product, and the outputs once.  What a row
+ * does not see does not enter it, whatever it holds; where it sees a value that is not finite, elements of its result may be NaN where
+ * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row NaN).
+ * Outputs overlap neither inputs nor each other (parts of one tensor between each other are fine).  workspace: device, 16-byte aligned,
+ * dat_attention_workspace(pass, shape) bytes (pass 0 forward, 1 backward; may be 0, then NULL is allowed); nothing in it outlives the
+ * call.  Asynchronous on `stream`, no allocation.
+ * DAT_ERR_ARG: null or misaligned pointers, negative sizes, H no multiple of Hkv, outputs that overlap (above) or whose strides lay
+ * elements on one another, scale not positive and finite, a window side below -1, one of the offsets without the other, a workspace that
+ * is too small; DAT_ERR_SHAPE: D above 128 or no multiple of 8, a length from 2^30 on, token strides from 2^23 bytes on, more tiles
+ * of 128 rows than a launch takes. */
+typedef struct { void* data; int64_t batch, token, head; } dat_heads;
+typedef struct {
+  dat_dtype dtype;
+  int32_t B, Sq, Sk, H, Hkv, D;
+  float scale;
+  int32_t left, right;
+  const int32_t* offsets_q;      /* device, or NULL with offsets_k */
+  const int32_t* offsets_k;
+} dat_attention;
+size_t dat_attention_workspace(int pass, const dat_attention* shape);
+dat_status dat_attention_forward(const dat_attention* shape, const dat_heads* q, const dat_heads* k, const dat_heads* v,
+                                 const dat_heads* o, float* lse, void* stream);
+dat_status dat_attention_backward(const dat_attention* shape, const dat_heads* q, const dat_heads* k, const dat_heads* v,
+                                  const dat_heads* o, const float* lse, const dat_heads* d_o, const dat_heads* dq,
+                                  const dat_heads* dk, const dat_heads* dv, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- convolution kernels on their own (bf16 storage, fp32 accumulate on MFMA) --------------
  * The three contractions behind dat_attack / dat_step, exposed for per-shape parity tests and
  * timing.  Tensors are device bf16 (uint16 bit patterns): x [B,H,W,Cin], w [Cout,k,k,Cin],

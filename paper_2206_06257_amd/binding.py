@@ -2,6 +2,7 @@
 methods of Model).  Raises if the library has not been built: there is no fallback path."""
 import ctypes as C
 import functools
+import math
 import os
 
 import numpy as np
@@ -27,7 +28,7 @@ EXPORTS = [
     "dat_attack_kl", "dat_step_reg", "dat_model_set_option", "dat_make_xadv",
     "dat_conv_backward_weight_static", "dat_conv_backward_weight_static_limit", "dat_set_kernel_option", "dat_conv_plan", "dat_model_grad_scales", "dat_quantize_scaled",
     "dat_adamw_slots", "dat_adamw_update", "dat_adamw_moments", "dat_model_adamw_update", "dat_log_probs_workspace", "dat_log_probs",
-    "dat_log_probs_backward", "dat_group_norm_workspace", "dat_group_norm_forward", "dat_group_norm_backward",
+    "dat_log_probs_backward", "dat_attention_workspace", "dat_attention_forward", "dat_attention_backward", "dat_group_norm_workspace", "dat_group_norm_forward", "dat_group_norm_backward",
     "dat_inspect_counts", "dat_inspect_op", "dat_inspect_tensor", "dat_inspect_read", "dat_inspect_bn",
 ]
 
@@ -48,6 +49,15 @@ def _load():
 
 
 _lib = _load()
+
+
+class _Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("B", C.c_int32), ("Sq", C.c_int32), ("Sk", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
+                ("scale", C.c_float), ("left", C.c_int32), ("right", C.c_int32), ("offsets_q", C.c_void_p), ("offsets_k", C.c_void_p)]
 
 
 class _Init(C.Structure):
@@ -99,6 +109,10 @@ _lib.dat_group_norm_workspace.restype = C.c_size_t
 _lib.dat_group_norm_workspace.argtypes = [_i] * 7
 _lib.dat_group_norm_forward.argtypes = [_vp, _vp, _vp] + [_i] * 6 + [_f, _i, _vp, _vp, _vp, _vp, C.c_size_t, _vp]
 _lib.dat_group_norm_backward.argtypes = [_vp] * 6 + [_i] * 7 + [_vp, _vp, _vp, _vp, C.c_size_t, _vp]
+_lib.dat_attention_workspace.restype = C.c_size_t
+_lib.dat_attention_workspace.argtypes = [_i, C.POINTER(_Attention)]
+_lib.dat_attention_forward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp, _vp]
+_lib.dat_attention_backward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp] + [C.POINTER(_Heads)] * 4 + [_vp, C.c_size_t, _vp]
 _lib.dat_attack_kl.argtypes = [_vp, _vp, _i, _f, _f, _i, _Init, _vp, _vp, _vp]
 _lib.dat_step_reg.argtypes = [_vp, _vp, _vp, _vp, _i, _f, _i, _vp, _vp, _vp]
 _lib.dat_profile_enable.argtypes = [_vp, _i]
@@ -627,6 +641,79 @@ def group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, act=ACT_NONE, dx
         _check(_lib.dat_group_norm_backward(_at(x), _at(dy), _at(gamma), _at(beta), _at(mean), _at(rstd), _code(x), B, H, W, Cc, groups,
                                             act, _at(dx), _at(dgamma), _at(dbeta), _at(ws), size, st), "dat_group_norm_backward")
     return dx, dgamma, dbeta
+
+
+def _heads(t):
+    """Strides of [B, S, H, D] or [T, H, D]; a dimension of one has any."""
+    st = t.stride()
+    return _Heads(t.data_ptr(), st[0] if t.dim() == 4 else 0, st[-3], st[-2])
+
+
+def _want_heads(name, t, dtype, shape, optional=False):
+    """Checks a tensor of heads: any strides but one between the elements of a head."""
+    if t is None and optional:
+        return
+    _want(name, t, (dtype,), None if shape is None else torch.Size(shape), contiguous=False)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: the elements of a head have to lie beside one another, strides are %s" % (name, tuple(t.stride())))
+
+
+def _attention(q, k, v, scale, window, offsets_q, offsets_k):
+    """The checks that both directions share -> (shape, batched)."""
+    _want("q", q, _FLOATS, contiguous=False)
+    batched = offsets_q is None
+    if batched != (offsets_k is None):
+        raise ValueError("offsets_q and offsets_k: both or neither")
+    if q.dim() != (4 if batched else 3):
+        raise ValueError("q: expected %s, got %s" % ("[B, S, H, D]" if batched else "[T, H, D]", tuple(q.shape)))
+    if k.dim() != q.dim() or k.shape[-1] != q.shape[-1] or (batched and k.shape[0] != q.shape[0]):
+        raise ValueError("k: %s does not go with q %s" % (tuple(k.shape), tuple(q.shape)))
+    _want_heads("q", q, q.dtype, q.shape)
+    _want_heads("k", k, q.dtype, k.shape)
+    _want_heads("v", v, q.dtype, k.shape)
+    if not batched:
+        _want("offsets_q", offsets_q, (torch.int32,), contiguous=True)
+        _want("offsets_k", offsets_k, (torch.int32,), offsets_q.shape)
+        if offsets_q.dim() != 1 or offsets_q.numel() < 1:
+            raise ValueError("offsets_q: expected [B + 1], got %s" % (tuple(offsets_q.shape),))
+    left, right = window
+    D = q.shape[-1]
+    B = q.shape[0] if batched else offsets_q.numel() - 1
+    return _Attention(_code(q), B, q.shape[-3], k.shape[-3], q.shape[-2], k.shape[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale, left, right,
+                      _at(offsets_q), _at(offsets_k)), batched
+
+
+def _lse_shape(q, batched):
+    return (q.shape[0], q.shape[2], q.shape[1]) if batched else (q.shape[1], q.shape[0])
+
+
+def attention_forward(q, k, v, scale=None, window=(-1, -1), offsets_q=None, offsets_k=None, o=None, stream=None):
+    """q [B, Sq, H, D], k and v [B, Sk, Hkv, D], or packed sequences [T, H, D] with int32 offsets [B + 1]; fp32 or bf16, any strides
+    between tokens and heads -> (o like q, lse fp32 [B, H, Sq] or [H, T]).  window = (left, right): keys that a query sees beside its own
+    place, -1 for all of them, (-1, 0) is causal; scale: 1 / sqrt(D) for None.  See dat_attention_forward."""
+    shape, batched = _attention(q, k, v, scale, window, offsets_q, offsets_k)
+    _want_heads("o", o, q.dtype, q.shape, optional=True)
+    with _On(stream, q, k, v, o, offsets_q, offsets_k) as st:
+        if o is None:
+            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty(_lse_shape(q, batched), device=q.device)
+        _check(_lib.dat_attention_forward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), st), "dat_attention_forward")
+    return o, lse
+
+
+def attention_backward(q, k, v, o, lse, do, scale=None, window=(-1, -1), offsets_q=None, offsets_k=None, dq=None, dk=None, dv=None, stream=None):
+    """Gradients of attention_forward's o from its o and lse and the incoming gradient do -> (dq, dk, dv)."""
+    shape, batched = _attention(q, k, v, scale, window, offsets_q, offsets_k)
+    for name, t, like in (("o", o, q), ("do", do, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+        _want_heads(name, t, q.dtype, like.shape, optional=name in ("dq", "dk", "dv"))
+    _want("lse", lse, (torch.float32,), torch.Size(_lse_shape(q, batched)))
+    with _On(stream, q, k, v, o, lse, do, dq, dk, dv, offsets_q, offsets_k) as st:
+        dq, dk, dv = (torch.empty(like.shape, dtype=q.dtype, device=q.device) if t is None else t for t, like in ((dq, q), (dk, k), (dv, k)))
+        size = int(_lib.dat_attention_workspace(1, shape))
+        ws = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+        _check(_lib.dat_attention_backward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), _heads(do), _heads(dq), _heads(dk), _heads(dv),
+                                           _at(ws), size, st), "dat_attention_backward")
+    return dq, dk, dv
 
 
 def philox_uniform(start, n, seed, stream_id, device="cuda"):
