@@ -371,6 +371,55 @@ dat_status dat_attention_backward(const dat_attention* shape, const dat_heads* q
                                   const dat_heads* o, const float* lse, const dat_heads* d_o, const dat_heads* dq,
                                   const dat_heads* dk, const dat_heads* dv, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- norm and rotation of queries and keys -----------------------------------------------------------------------
+ * Every head of q [B][S][H][D] and k [B][S][Hkv][D] (tensors of heads as above; Hkv or H may be 0, their pointers then NULL):
+ *   r = 1 / sqrt(mean x^2 + eps), n = x r gamma (norm = 1; 0: n = x); then pair p of elements (a, b) turns by the angle
+ *   w = position[axis(p)] frequency[p], (a cos w - b sin w, a sin w + b cos w).
+ * axes 0 to 4; the first sections[0] pairs go by the first axis, and so on; the elements of pair p are p and p + pairs
+ * (DAT_ROTARY_HALVES) or 2p and 2p + 1 (DAT_ROTARY_PAIRS), pairs = the sections' sum; elements from 2 pairs on do not turn.
+ * positions: device int32 [B][S][axes]; frequencies: device fp32 [pairs], radians a step, below 2^32 (not read where pairs = 0); angles are formed and
+ * reduced in 64 bits.  gamma_q, gamma_k: device fp32 [D], NULL for 1.  In fp32, each output rounded once to `dtype`.
+ *   backward: dn = dy turned back, h = dn gamma, xhat = x r; dx = r (h - xhat mean(h xhat)) (norm = 0: dx = dn, q and k are not read and may be NULL);
+ *   dgamma_q, dgamma_k (device fp32 [D], either may be NULL; written, not added to): sums of dn xhat over tokens and heads, in a fixed
+ *   order; norm = 0 leaves them as they were.
+ * yq may be q and yk may be k (same strides); dq may be q or dyq, dk k or dyk; buffers that share elements otherwise are refused.  A
+ * head of zeros with eps = 0 becomes NaN; a NaN or an infinity spoils its head (and the scales' gradients).
+ * workspace: device, 16-byte aligned, dat_norm_rotary_workspace(pass, shape) bytes (pass 0 forward, 1 backward; may be 0, then NULL is
+ * allowed); nothing in it outlives the call.  Asynchronous on `stream`, no allocation.  B or S = 0: no output but dgamma = 0.
+ * DAT_ERR_ARG: null or misaligned pointers, negative sizes, no head at all, more than 4 axes, more pairs than D / 2, unknown dtype or layout, norm
+ * neither 0 nor 1, eps negative, NaN or infinite, buffers that overlap (above), a workspace that is too small; DAT_ERR_SHAPE: D above 256 or
+ * no multiple of 8, an odd number of pairs in halves, more than 2^30 tokens or 2^20 heads. */
+typedef enum { DAT_ROTARY_HALVES = 0, DAT_ROTARY_PAIRS = 1 } dat_rotary_layout;
+typedef struct {
+  dat_dtype dtype;
+  int32_t B, S, H, Hkv, D;
+  int32_t axes, sections[4];
+  int32_t layout, norm;
+  float eps;
+} dat_rotary;
+size_t dat_norm_rotary_workspace(int pass, const dat_rotary* shape);
+dat_status dat_norm_rotary_forward(const dat_rotary* shape, const dat_heads* q, const dat_heads* k, const float* gamma_q, const float* gamma_k,
+                                   const int32_t* positions, const float* frequencies, const dat_heads* yq, const dat_heads* yk,
+                                   void* stream);
+dat_status dat_norm_rotary_backward(const dat_rotary* shape, const dat_heads* q, const dat_heads* k, const float* gamma_q, const float* gamma_k,
+                                    const int32_t* positions, const float* frequencies, const dat_heads* dyq, const dat_heads* dyk,
+                                    const dat_heads* dq, const dat_heads* dk, float* dgamma_q, float* dgamma_k, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/* ---- the norm of all gradients, and clipping ------------------------------------------------------------------------
+ * T gradient tensors anywhere on the device, given by device tables that a program keeps: pointers_dev [T] (addresses), types_dev [T]
+ * (dat_dtype: fp32 or bf16, aligned to an element), offsets_dev [T + 1] (elements before each tensor; offsets_dev[T] = total).  Tensors
+ * do not overlap; they may be empty.
+ *   norm = sqrt(sum over all elements of g^2), squares and sums in 64 bits in a fixed order (device fp32 [1], rounded once);
+ *   where norm > largest, every g becomes g c, c = largest / norm rounded to fp32 and the product to the tensor's type; else nothing is written.
+ *   A NaN norm makes every gradient NaN, an infinite one 0 (an infinite gradient NaN).  largest infinite: the norm alone.
+ * workspace: device, 8-byte aligned, dat_clip_gradients_workspace(T, total) bytes; nothing in it outlives the call.  Asynchronous on
+ * `stream`, no allocation.  DAT_ERR_ARG: null or misaligned pointers, T below 1, total negative, largest negative or NaN, a
+ * workspace that is too small; DAT_ERR_SHAPE: more than 2^31 blocks of 8192 elements. */
+size_t dat_clip_gradients_workspace(int num_tensors, int64_t total);
+dat_status dat_clip_gradients(const uint64_t* pointers_dev, const uint8_t* types_dev, const int64_t* offsets_dev, int num_tensors,
+                              int64_t total, float largest, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- convolution kernels on their own (bf16 storage, fp32 accumulate on MFMA) --------------
  * The three contractions behind dat_attack / dat_step, exposed for per-shape parity tests and
  * timing.  Tensors are device bf16 (uint16 bit patterns): x [B,H,W,Cin], w [Cout,k,k,Cin],

@@ -17,6 +17,7 @@ PHI_CE, PHI_TRADES_KL = 0, 1
 F32, BF16 = 0, 1
 INIT_ZERO, INIT_UNIFORM, INIT_GIVEN = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
 MAX_TOP = 32
 
 EXPORTS = [
@@ -28,7 +29,9 @@ EXPORTS = [
     "dat_attack_kl", "dat_step_reg", "dat_model_set_option", "dat_make_xadv",
     "dat_conv_backward_weight_static", "dat_conv_backward_weight_static_limit", "dat_set_kernel_option", "dat_conv_plan", "dat_model_grad_scales", "dat_quantize_scaled",
     "dat_adamw_slots", "dat_adamw_update", "dat_adamw_moments", "dat_model_adamw_update", "dat_log_probs_workspace", "dat_log_probs",
-    "dat_log_probs_backward", "dat_attention_workspace", "dat_attention_forward", "dat_attention_backward", "dat_group_norm_workspace", "dat_group_norm_forward", "dat_group_norm_backward",
+    "dat_log_probs_backward", "dat_attention_workspace", "dat_attention_forward", "dat_attention_backward",
+    "dat_norm_rotary_workspace", "dat_norm_rotary_forward", "dat_norm_rotary_backward", "dat_clip_gradients_workspace", "dat_clip_gradients",
+    "dat_group_norm_workspace", "dat_group_norm_forward", "dat_group_norm_backward",
     "dat_inspect_counts", "dat_inspect_op", "dat_inspect_tensor", "dat_inspect_read", "dat_inspect_bn",
 ]
 
@@ -58,6 +61,11 @@ class _Heads(C.Structure):
 class _Attention(C.Structure):
     _fields_ = [("dtype", C.c_int), ("B", C.c_int32), ("Sq", C.c_int32), ("Sk", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32),
                 ("scale", C.c_float), ("left", C.c_int32), ("right", C.c_int32), ("offsets_q", C.c_void_p), ("offsets_k", C.c_void_p)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("B", C.c_int32), ("S", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("axes", C.c_int32),
+                ("sections", C.c_int32 * 4), ("layout", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float)]
 
 
 class _Init(C.Structure):
@@ -113,6 +121,13 @@ _lib.dat_attention_workspace.restype = C.c_size_t
 _lib.dat_attention_workspace.argtypes = [_i, C.POINTER(_Attention)]
 _lib.dat_attention_forward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp, _vp]
 _lib.dat_attention_backward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp] + [C.POINTER(_Heads)] * 4 + [_vp, C.c_size_t, _vp]
+_lib.dat_norm_rotary_workspace.restype = C.c_size_t
+_lib.dat_norm_rotary_workspace.argtypes = [_i, C.POINTER(_Rotary)]
+_lib.dat_norm_rotary_forward.argtypes = [C.POINTER(_Rotary)] + [C.POINTER(_Heads)] * 2 + [_vp] * 4 + [C.POINTER(_Heads)] * 2 + [_vp]
+_lib.dat_norm_rotary_backward.argtypes = [C.POINTER(_Rotary)] + [C.POINTER(_Heads)] * 2 + [_vp] * 4 + [C.POINTER(_Heads)] * 4 + [_vp, _vp, _vp, C.c_size_t, _vp]
+_lib.dat_clip_gradients_workspace.restype = C.c_size_t
+_lib.dat_clip_gradients_workspace.argtypes = [_i, _i64]
+_lib.dat_clip_gradients.argtypes = [_vp, _vp, _vp, _i, _i64, _f, _vp, _vp, C.c_size_t, _vp]
 _lib.dat_attack_kl.argtypes = [_vp, _vp, _i, _f, _f, _i, _Init, _vp, _vp, _vp]
 _lib.dat_step_reg.argtypes = [_vp, _vp, _vp, _vp, _i, _f, _i, _vp, _vp, _vp]
 _lib.dat_profile_enable.argtypes = [_vp, _i]
@@ -714,6 +729,124 @@ def attention_backward(q, k, v, o, lse, do, scale=None, window=(-1, -1), offsets
         _check(_lib.dat_attention_backward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), _heads(do), _heads(dq), _heads(dk), _heads(dv),
                                            _at(ws), size, st), "dat_attention_backward")
     return dq, dk, dv
+
+
+def rotary_frequencies(sections, base=10000.0, device="cuda"):
+    """fp32 [pairs]: base^(-i / n) for the i-th of an axis's n pairs, axis after axis."""
+    return torch.cat([base ** (-torch.arange(n, dtype=torch.float64) / n) for n in sections]).float().to(device) if sections else torch.empty(0, device=device)
+
+
+def _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm, like=None):
+    """The checks that both directions share -> shape.  q, or (where it is not given) the gradient `like`, has the sizes."""
+    first, second = (q, k) if like is None else like
+    one = second if first is None else first
+    if one is None:
+        raise ValueError("q or k: one of them is needed")
+    _want("q" if first is not None else "k", one, _FLOATS, contiguous=False)
+    if one.dim() not in (3, 4):
+        raise ValueError("q: expected [B, S, H, D] or [T, H, D], got %s" % (tuple(one.shape),))
+    D, lead = one.shape[-1], tuple(one.shape[:-2])
+    if second is not None and (second.dim() != one.dim() or tuple(second.shape[:-2]) != lead or second.shape[-1] != D):
+        raise ValueError("k: %s does not go with q %s" % (tuple(second.shape), tuple(one.shape)))
+    for name, t in (("q", first), ("k", second)):
+        _want_heads(name, t, one.dtype, None, optional=True)
+    for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
+        _want(name, t, (torch.float32,), (D,), optional=True)
+    sections = list(sections)
+    if len(sections) > 4:
+        raise ValueError("sections: at most 4 axes, got %r" % (sections,))
+    pairs = sum(sections)
+    _want("positions", positions, (torch.int32,), lead + (len(sections),), optional=pairs == 0)
+    _want("frequencies", frequencies, (torch.float32,), (pairs,), optional=pairs == 0)
+    B, S = lead if len(lead) == 2 else (1, lead[0])
+    return _Rotary(_code(one), B, S, 0 if first is None else first.shape[-2], 0 if second is None else second.shape[-2], D, len(sections),
+                   (C.c_int32 * 4)(*sections), layout, int(bool(norm)), eps)
+
+
+def _heads_or_none(t):
+    return None if t is None else _heads(t)
+
+
+def norm_rotary_forward(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout=ROTARY_HALVES, eps=1e-6, norm=True, yq=None, yk=None, stream=None):
+    """Norm of every head of q [B, S, H, D] and k [B, S, Hkv, D] (or [T, H, D]; fp32 or bf16, any strides between tokens and heads; either may be
+    None), its scale (fp32 [D] or None) and the rotation by positions int32 [.., axes]: sections[a] pairs go by axis a, with one
+    frequency (fp32, radians a step) each -> (yq, yk).  yq may be q, yk may be k.  See dat_norm_rotary_forward."""
+    shape = _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm)
+    first = k if q is None else q
+    for name, t, like in (("yq", yq, q), ("yk", yk, k)):
+        if like is not None:
+            _want_heads(name, t, first.dtype, like.shape, optional=True)
+    with _On(stream, first, k, gamma_q, gamma_k, positions, frequencies, yq, yk) as st:
+        yq, yk = (None if like is None else torch.empty(like.shape, dtype=like.dtype, device=like.device) if t is None else t for t, like in ((yq, q), (yk, k)))
+        _check(_lib.dat_norm_rotary_forward(shape, _heads_or_none(q), _heads_or_none(k), _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies),
+                                            _heads_or_none(yq), _heads_or_none(yk), st), "dat_norm_rotary_forward")
+    return yq, yk
+
+
+def norm_rotary_backward(q, k, gamma_q, gamma_k, positions, frequencies, sections, dyq, dyk, layout=ROTARY_HALVES, eps=1e-6, norm=True, dq=None, dk=None,
+                         dgamma_q=None, dgamma_k=None, stream=None):
+    """Gradients of norm_rotary_forward for the incoming gradients dyq and dyk -> (dq, dk, dgamma_q, dgamma_k); the last two are None where there is
+    no such scale.  dq may be q or dyq, dk may be k or dyk.  Without the norm q and k are not needed."""
+    shape = _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm, like=(dyq, dyk))
+    first = dyk if dyq is None else dyq
+    for name, t, like, needed in (("q", q, dyq, norm), ("k", k, dyk, norm), ("dq", dq, dyq, False), ("dk", dk, dyk, False)):
+        if like is not None:
+            _want_heads(name, t, first.dtype, like.shape, optional=not needed)
+    D = first.shape[-1]
+    for name, t in (("dgamma_q", dgamma_q), ("dgamma_k", dgamma_k)):
+        _want(name, t, (torch.float32,), (D,), optional=True)
+    with _On(stream, first, dyk, q, k, gamma_q, gamma_k, positions, frequencies, dq, dk, dgamma_q, dgamma_k) as st:
+        device = first.device
+        dq, dk = (None if like is None else torch.empty(like.shape, dtype=like.dtype, device=device) if t is None else t for t, like in ((dq, dyq), (dk, dyk)))
+        dgamma_q, dgamma_k = (torch.empty(D, device=device) if t is None and norm and gamma is not None and like is not None else t
+                              for t, gamma, like in ((dgamma_q, gamma_q, dyq), (dgamma_k, gamma_k, dyk)))
+        size = int(_lib.dat_norm_rotary_workspace(1, shape))
+        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
+        _check(_lib.dat_norm_rotary_backward(shape, _heads_or_none(q), _heads_or_none(k), _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies),
+                                             _heads_or_none(dyq), _heads_or_none(dyk), _heads_or_none(dq), _heads_or_none(dk), _at(dgamma_q), _at(dgamma_k),
+                                             _at(ws), size, st), "dat_norm_rotary_backward")
+    return dq, dk, dgamma_q, dgamma_k
+
+
+class GradientTable:
+    """Gradient tensors (fp32 or bf16, contiguous, on one GPU, none on another) as clip_gradients takes them; keeps them alive."""
+
+    def __init__(self, tensors):
+        self.tensors = tensors = list(tensors)
+        if not tensors:
+            raise ValueError("a table needs a tensor at least")
+        for n, t in enumerate(tensors):
+            _want("tensor %d" % n, t, _FLOATS)
+            if t.device != tensors[0].device or t.get_device() < 0:
+                raise ValueError("tensor %d: all tensors belong on one GPU, not on %s" % (n, t.device))
+        places = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), n) for n, t in enumerate(tensors) if t.numel())
+        for (_, end, a), (start, _, c) in zip(places, places[1:]):
+            if start < end:
+                raise ValueError("tensors %d and %d share elements" % (a, c))
+        device, sizes = tensors[0].device, [t.numel() for t in tensors]
+        self.total = sum(sizes)
+        self.pointers = torch.tensor([t.data_ptr() for t in tensors], dtype=torch.int64, device=device)
+        self.types = torch.tensor([_code(t) for t in tensors], dtype=torch.uint8, device=device)
+        self.offsets = torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), dtype=torch.int64, device=device)
+
+
+def gradient_table(tensors):
+    """The table of gradient tensors that clip_gradients works on; a program makes it once (see GradientTable)."""
+    return GradientTable(tensors)
+
+
+def clip_gradients(table, largest, norm=None, stream=None):
+    """norm = sqrt(sum of all squares) of the table's tensors (fp32 [1]); where it is above `largest` they are scaled down to it, in place.
+    largest = inf: the norm alone.  See dat_clip_gradients."""
+    _want("norm", norm, (torch.float32,), (1,), optional=True)
+    with _On(stream, table.pointers, norm) as st:
+        if norm is None:
+            norm = torch.empty(1, device=table.pointers.device)
+        size = int(_lib.dat_clip_gradients_workspace(len(table.tensors), table.total))
+        ws = torch.empty(size, dtype=torch.uint8, device=table.pointers.device)
+        _check(_lib.dat_clip_gradients(_at(table.pointers), _at(table.types), _at(table.offsets), len(table.tensors), table.total, largest, _at(norm), _at(ws),
+                                       size, st), "dat_clip_gradients")
+    return norm
 
 
 def philox_uniform(start, n, seed, stream_id, device="cuda"):

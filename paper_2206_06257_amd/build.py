@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdat.so")
-SOURCES = ["status.cpp", "quantize.hip", "pgd.hip", "layers.hip", "conv_direct.hip", "conv_mfma.hip", "model.hip", "optim.hip", "adamw.hip", "logprobs.hip", "groupnorm.hip", "attention.hip"]
+SOURCES = ["status.cpp", "quantize.hip", "pgd.hip", "layers.hip", "conv_direct.hip", "conv_mfma.hip", "model.hip", "optim.hip", "adamw.hip", "logprobs.hip", "groupnorm.hip", "attention.hip", "rotary.hip", "clip.hip"]
 # -ffp-contract=off: the elementwise kernels promise one rounding per fp32 operation.
 # packed-fp32 instructions are disabled for every translation unit.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -61,10 +61,11 @@ inline bool heads_overlap(const dat_heads& x, const HeadsShape& sx, const dat_he
   return same ? nested_overlap(gap / (int64_t)width, dx, dy, 0, sx.D) : true;
 }
 
-// Alignment of 16-byte vectors; strides at least 0.
-inline bool heads_vectors(const dat_heads& t, size_t width) {
+// Alignment of 16-byte vectors; strides at least 0 (that of a dimension of one is not looked at).
+inline bool heads_vectors(const dat_heads& t, const HeadsShape& s, size_t width) {
   const int64_t v = 16 / (int64_t)width;
-  return t.data && aligned(t.data, 16) && t.batch >= 0 && t.token >= 0 && t.head >= 0 && t.batch % v == 0 && t.token % v == 0 && t.head % v == 0;
+  auto fine = [&](int64_t count, int64_t stride) { return count <= 1 || (stride >= 0 && stride % v == 0); };
+  return t.data && aligned(t.data, 16) && fine(s.batch, t.batch) && fine(s.tokens, t.token) && fine(s.heads, t.head);
 }
 
 }  // namespace dat

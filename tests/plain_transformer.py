@@ -71,3 +71,54 @@ def attention_backward(q, k, v, o, lse, do, scale, window, half):
         tol[1][:, kv] += scale * (es + n * U * np.abs(ds)).T @ np.abs(qh) + (1 + scale) * Lq * TINY
         tol[2][:, kv] += (ep + n * U * p).T @ np.abs(gh) + Lq * TINY
     return out, tol
+
+
+# ---- norm and rotation, x [T, H, D], positions [T, A] -------------------------------------------------------------------
+def angles(positions, frequencies, sections):
+    """[T, pairs]; frequencies are fp32 numbers, so that the products have at most 55 bits: formed in long double."""
+    axis = np.repeat(np.arange(len(sections)), sections)
+    w = np.asarray(positions, np.longdouble)[:, axis] * np.asarray(frequencies, np.longdouble)
+    return np.asarray(np.remainder(w, 2 * np.longdouble("3.14159265358979323846264338327950288")), np.float64)
+
+
+def _places(D, pairs, halves):
+    p = np.arange(pairs)
+    return (p, p + pairs) if halves else (2 * p, 2 * p + 1)
+
+
+def turned(n, w, halves, back=False):
+    """The pairs of n [T, H, D] turned by w [T, pairs], and |a| + |b| of each element's pair."""
+    out, size = n.copy(), np.abs(n)
+    a, b = _places(n.shape[-1], w.shape[1], halves)
+    c, s = np.cos(w)[:, None], np.sin(w)[:, None] * (-1 if back else 1)
+    out[..., a] = n[..., a] * c - n[..., b] * s
+    out[..., b] = n[..., a] * s + n[..., b] * c
+    size[..., a] = size[..., b] = np.abs(n[..., a]) + np.abs(n[..., b])
+    return out, size
+
+
+def norm_rotary(x, gamma, w, halves, eps, norm=True):
+    """y and the magnitudes its errors scale with."""
+    if norm:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * (1.0 if gamma is None else gamma)
+    return turned(x, w, halves)
+
+
+def norm_rotary_backward(x, dy, gamma, w, halves, eps, norm=True):
+    """dx, dgamma and the magnitudes their errors scale with."""
+    dn, size = turned(dy, w, halves, back=True)
+    if not norm:
+        return dn, None, size, None
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    xhat, g = x * r, np.ones(x.shape[-1]) if gamma is None else gamma
+    h, hs = dn * g, size * np.abs(g)
+    dx = r * (h - xhat * (h * xhat).mean(-1, keepdims=True))
+    dx_size = r * (hs + np.abs(xhat) * (hs * np.abs(xhat)).mean(-1, keepdims=True))
+    return dx, (dn * xhat).sum((0, 1)), dx_size, (size * np.abs(xhat)).sum((0, 1))
+
+
+# ---- clipping ------------------------------------------------------------------------------------------------------------
+def clip(tensors, largest):
+    norm = np.sqrt(sum((np.asarray(t, np.float64) ** 2).sum() for t in tensors))
+    c = largest / norm if norm > largest else 1.0
+    return norm, [np.asarray(t, np.float64) * c for t in tensors], c

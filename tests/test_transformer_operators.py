@@ -1,5 +1,4 @@
-"""Refusals of the attention calls (no GPU needed: nothing is launched) and their plain forms against differences."""
-import ctypes as C
+"""Refusals of the attention, norm-and-rotation and clipping calls (no GPU needed: nothing is launched), and their plain forms against differences."""
 import math
 
 import numpy as np
@@ -122,3 +121,104 @@ def test_plain_attention_gradient_against_differences(Lq, Lk, window):
             u = rng.standard_normal(grads[n].shape)
             ends = [f(*[t + s * 1e-6 * u if i == n else t for i, t in enumerate((q, k, v))]) for s in (1, -1)]
             assert abs((ends[0] - ends[1]) / 2e-6 - (grads[n] * u).sum()) < 1e-7 * (1 + np.abs(grads[n] * u).sum())
+
+
+# ---- norm and rotation ---------------------------------------------------------------------------------------------------
+ROT = dict(dtype=0, B=2, S=10, H=4, Hkv=2, D=32, axes=2, sections=(8, 8, 0, 0), layout=0, norm=1, eps=1e-6)
+
+
+def rot(backward=False, positions=P, freq=P, gq=P, gk=P, dgq=P, dgk=P, ws=P, size=1 << 40, t=None, null=(), **kw):
+    d = dict(ROT, **kw)
+    shape = b._Rotary(d["dtype"], d["B"], d["S"], d["H"], d["Hkv"], d["D"], d["axes"], (b.C.c_int32 * 4)(*d["sections"]), d["layout"], d["norm"], d["eps"])
+    x = {}
+    for n, name in enumerate(("q", "k", "yq", "yk", "dq", "dk")):
+        H = d["H"] if name in ("q", "yq", "dq") else d["Hkv"]
+        x[name] = None if name in null else heads(n, d["S"], H, d["D"], **(t[1] if t and t[0] == name else {}))
+    if not backward:
+        return lib.dat_norm_rotary_forward(shape, x["q"], x["k"], gq, gk, positions, freq, x["yq"], x["yk"], None)
+    return lib.dat_norm_rotary_backward(shape, x["q"], x["k"], gq, gk, positions, freq, x["yq"], x["yk"], x["dq"], x["dk"], dgq, dgk, ws, size, None)
+
+
+ROT_REFUSED = [(1, dict(dtype=2)), (1, dict(B=-1)), (1, dict(S=-1)), (1, dict(H=-1)), (1, dict(H=0, Hkv=0)), (1, dict(D=0)), (1, dict(axes=-1)), (1, dict(axes=5)),
+               (1, dict(sections=(-8, 8, 0, 0))), (1, dict(sections=(8, 9, 0, 0))), (1, dict(layout=2)), (1, dict(norm=2)), (1, dict(eps=-1.0)), (1, dict(eps=math.nan)), (1, dict(eps=math.inf)),
+               (2, dict(D=36)), (2, dict(D=264)), (2, dict(sections=(8, 7, 0, 0))), (2, dict(B=1 << 16, S=1 << 15)), (2, dict(H=1 << 20)),
+               (1, dict(positions=None)), (1, dict(freq=None)), (1, dict(positions=P + 2)), (1, dict(freq=P + 1)), (1, dict(gq=P + 2)), (1, dict(gk=P + 1)),
+               (1, dict(null=("q",))), (1, dict(null=("yk",))), (1, dict(t=("q", dict(data=P + 8)))), (1, dict(t=("k", dict(token=33)))), (1, dict(t=("yq", dict(head=-32)))),
+               (1, dict(dtype=1, t=("q", dict(head=36))))]
+
+
+@pytest.mark.parametrize("status,kw", ROT_REFUSED + [(1, dict(t=("yq", dict(token=0)))), (1, dict(t=("yq", dict(data=P + 16)))), (1, dict(t=("yk", dict(data=P + 2 * FAR + 64)))),
+                                                      (1, dict(t=("yk", dict(data=P)))), (1, dict(t=("yq", dict(data=P, token=256))))])
+def test_norm_rotary_forward_refuses(status, kw):
+    assert rot(**kw) == status
+
+
+@pytest.mark.parametrize("status,kw", ROT_REFUSED + [(1, dict(ws=None)), (1, dict(ws=P + 8)), (1, dict(size=100)), (1, dict(dgq=P + 2)), (1, dict(dgk=P + 1)), (1, dict(null=("dq",))),
+                                                      (1, dict(t=("dq", dict(token=0)))), (1, dict(t=("dq", dict(data=P + 16)))), (1, dict(t=("dk", dict(data=P + 4 * FAR)))),
+                                                      (1, dict(t=("dk", dict(data=P + 2 * FAR))))])
+def test_norm_rotary_backward_refuses(status, kw):
+    assert rot(backward=True, **kw) == status
+
+
+def test_norm_rotary_has_nothing_to_do():
+    assert rot(B=0) == 0 and rot(S=0, positions=None, freq=None) == 0 and rot(backward=True, S=0, dgq=None, dgk=None, ws=None, size=0) == 0
+    shape = b._Rotary(0, 2, 10, 4, 2, 32, 2, (b.C.c_int32 * 4)(8, 8, 0, 0), 0, 1, 1e-6)
+    assert lib.dat_norm_rotary_workspace(0, shape) == 0 and lib.dat_norm_rotary_workspace(1, shape) >= 2 * 32 * 4 and lib.dat_norm_rotary_workspace(1, None) == 0
+    assert lib.dat_norm_rotary_forward(None, None, None, None, None, None, None, None, None, None) == 1
+
+
+def test_norm_rotary_binding_refuses():
+    q, k, g = torch.zeros(5, 4, 32), torch.zeros(5, 2, 32), torch.ones(32)
+    pos, f = torch.zeros(5, 2, dtype=torch.int32), torch.zeros(16)
+    for call in (lambda: b.norm_rotary_forward(q, k, g, g, pos, f, [8, 8]), lambda: b.norm_rotary_forward(q, k, g[:8], g, pos, f, [8, 8]), lambda: b.norm_rotary_forward(q, k, g, g, pos.long(), f, [8, 8]),
+                 lambda: b.norm_rotary_forward(q, k, g, g, pos[:4], f, [8, 8]), lambda: b.norm_rotary_forward(q, k, g, g, pos, f, [16]), lambda: b.norm_rotary_forward(q, k, g, g, pos, f[:8], [8, 8]),
+                 lambda: b.norm_rotary_forward(q, k[:4], g, g, pos, f, [8, 8]), lambda: b.norm_rotary_forward(q, k.bfloat16(), g, g, pos, f, [8, 8]), lambda: b.norm_rotary_forward(None, None, g, g, pos, f, [8, 8]),
+                 lambda: b.norm_rotary_forward(q, k, g, g, None, f, [8, 8]), lambda: b.norm_rotary_forward(q, k, g, g, pos, f, [2, 2, 4, 4, 4]), lambda: b.norm_rotary_forward(q[0], k[0], g, g, pos, f, [8, 8]),
+                 lambda: b.norm_rotary_forward(q.half(), None, g, g, pos, f, [8, 8]), lambda: b.norm_rotary_forward(q, k, g, g, pos, f, [8, 8], yq=k),
+                 lambda: b.norm_rotary_backward(None, k, g, g, pos, f, [8, 8], q, k), lambda: b.norm_rotary_backward(q, k, g, g, pos, f, [8, 8], k, k),
+                 lambda: b.norm_rotary_backward(q, k, g, g, pos, f, [8, 8], q, k, dgamma_q=g[:3]), lambda: b.norm_rotary_backward(q, k, g, g, pos, f, [8, 8], q, k)):
+        with pytest.raises((ValueError, AttributeError)):
+            call()
+
+
+def test_rotary_frequencies():
+    f = b.rotary_frequencies([2, 4], 100.0, device="cpu")
+    assert torch.allclose(f, torch.tensor([1.0, 0.1, 1.0, 100 ** -0.25, 0.1, 100 ** -0.75])) and b.rotary_frequencies([], device="cpu").numel() == 0
+
+
+@pytest.mark.parametrize("halves", [True, False])
+@pytest.mark.parametrize("norm", [True, False])
+def test_plain_rotation_gradient_against_differences(halves, norm):
+    rng = np.random.default_rng(3)
+    x, gamma, dy, w = rng.standard_normal((3, 2, 12)), 1 + 0.2 * rng.standard_normal(12), rng.standard_normal((3, 2, 12)), rng.uniform(-9, 9, (3, 5))
+    dx, dg = pt.norm_rotary_backward(x, dy, gamma, w, halves, 1e-3, norm)[:2]
+    f = lambda x, g: (pt.norm_rotary(x, g, w, halves, 1e-3, norm)[0] * dy).sum()  # noqa: E731
+    for n, grad in enumerate((dx, dg) if norm else (dx,)):
+        for _ in range(4):
+            u = rng.standard_normal(grad.shape)
+            ends = [f(*[t + s * 1e-6 * u if i == n else t for i, t in enumerate((x, gamma))]) for s in (1, -1)]
+            assert abs((ends[0] - ends[1]) / 2e-6 - (grad * u).sum()) < 1e-7 * (1 + np.abs(grad * u).sum())
+
+
+# ---- clipping --------------------------------------------------------------------------------------------------------------
+def clip(pointers=P, types=P, off=P, T=3, total=100, largest=1.0, norm=P, ws=P, size=1 << 30):
+    return lib.dat_clip_gradients(pointers, types, off, T, total, largest, norm, ws, size, None)
+
+
+@pytest.mark.parametrize("status,kw", [
+    (1, dict(pointers=None)), (1, dict(types=None)), (1, dict(off=None)), (1, dict(norm=None)), (1, dict(ws=None)), (1, dict(T=0)), (1, dict(total=-1)), (1, dict(largest=-1.0)),
+    (1, dict(largest=math.nan)), (1, dict(pointers=P + 4)), (1, dict(off=P + 4)), (1, dict(norm=P + 2)), (1, dict(ws=P + 4)), (1, dict(size=3)), (2, dict(total=1 << 45))])
+def test_clip_gradients_refuses(status, kw):
+    assert clip(**kw) == status
+
+
+def test_clip_gradients_binding_refuses():
+    assert lib.dat_clip_gradients_workspace(0, 5) == 0 and lib.dat_clip_gradients_workspace(3, -1) == 0 and lib.dat_clip_gradients_workspace(3, 100) >= 8
+    for bad in ([], [torch.zeros(3)], [torch.zeros(3, dtype=torch.float16)], [None]):
+        with pytest.raises(ValueError):
+            b.gradient_table(bad)
+
+
+def test_plain_clip():
+    norm, out, c = pt.clip([np.array([3.0]), np.array([0.0, 4.0])], 2.5)
+    assert norm == 5.0 and c == 0.5 and out[1][1] == 2.0 and pt.clip([np.array([3.0])], 3.0)[2] == 1.0
