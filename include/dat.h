@@ -366,7 +366,7 @@ typedef struct {
 } dat_attention;
 size_t dat_attention_workspace(int pass, const dat_attention* shape);
 dat_status dat_attention_forward(const dat_attention* shape, const dat_heads* q, const dat_heads* k, const dat_heads* v,
-                                 const dat_heads* o, float* lse, void* stream);
+                                 const dat_heads* o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 dat_status dat_attention_backward(const dat_attention* shape, const dat_heads* q, const dat_heads* k, const dat_heads* v,
                                   const dat_heads* o, const float* lse, const dat_heads* d_o, const dat_heads* dq,
                                   const dat_heads* dk, const dat_heads* dv, void* workspace, size_t workspace_bytes, void* stream);

@@ -119,7 +119,7 @@ _lib.dat_group_norm_forward.argtypes = [_vp, _vp, _vp] + [_i] * 6 + [_f, _i, _vp
 _lib.dat_group_norm_backward.argtypes = [_vp] * 6 + [_i] * 7 + [_vp, _vp, _vp, _vp, C.c_size_t, _vp]
 _lib.dat_attention_workspace.restype = C.c_size_t
 _lib.dat_attention_workspace.argtypes = [_i, C.POINTER(_Attention)]
-_lib.dat_attention_forward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp, _vp]
+_lib.dat_attention_forward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp, _vp, C.c_size_t, _vp]
 _lib.dat_attention_backward.argtypes = [C.POINTER(_Attention)] + [C.POINTER(_Heads)] * 4 + [_vp] + [C.POINTER(_Heads)] * 4 + [_vp, C.c_size_t, _vp]
 _lib.dat_norm_rotary_workspace.restype = C.c_size_t
 _lib.dat_norm_rotary_workspace.argtypes = [_i, C.POINTER(_Rotary)]
@@ -712,7 +712,9 @@ def attention_forward(q, k, v, scale=None, window=(-1, -1), offsets_q=None, offs
         if o is None:
             o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty(_lse_shape(q, batched), device=q.device)
-        _check(_lib.dat_attention_forward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), st), "dat_attention_forward")
+        size = int(_lib.dat_attention_workspace(0, shape))
+        ws = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+        _check(_lib.dat_attention_forward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), _at(ws), size, st), "dat_attention_forward")
     return o, lse
 
 

@@ -22,7 +22,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef short v4s16 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void* lds_void_ptr;
 typedef __amdgpu_buffer_rsrc_t BufRsrc;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -41,11 +40,13 @@ struct AttnArgs {
   int B, Sq, Sk, H, Hkv, G, D, left, right;
   float scale, c;                                        // c = scale / ln 2
   int rows_per_group, groups, xcd;                       // tiles of a group of heads; groups; 1: a contiguous share of the work for each XCD
-  int64_t items, rows;                                   // rows = B * H * Sq (H * Sq packed)
+  int parts;                                             // workgroups that share the walk of a tile
+  int64_t items, rows, key_rows;                         // rows = B * H * Sq (H * Sq packed), key_rows = B * Hkv * Sk
+  float* part;                                           // their results in fp32: [parts][rows][D], then [parts][rows][2] (forward: m c and l)
 };
 
 // One tile of a result: sequence, heads and rows.
-struct Place { int b, hk, g, row0, q0, k0, Lq, Lk; };
+struct Place { int b, hk, g, part, row0, q0, k0, Lq, Lk; };
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
@@ -63,8 +64,9 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, int per, Place& p)
   int64_t item = blockIdx.x;
   if (a.xcd) item = (int64_t)(blockIdx.x & 7) * ((a.items + 7) >> 3) + (blockIdx.x >> 3);
   if (item >= a.items) return false;
-  const int t = (int)(item / per);
-  p.g = (int)(item - (int64_t)t * per);
+  const int t = (int)(item / (per * a.parts)), within = (int)(item - (int64_t)t * per * a.parts);
+  p.g = within / a.parts;
+  p.part = within - p.g * a.parts;
   const int group = t / a.rows_per_group;
   int tile = a.rows_per_group - 1 - (t - group * a.rows_per_group);
   if (!QUERIES) tile = t - group * a.rows_per_group;      // early keys are seen by the most queries
@@ -98,6 +100,9 @@ __device__ __forceinline__ char* rows_of(const HeadsArg& t, int b, int first, in
 }
 __device__ __forceinline__ int64_t stat_row(const AttnArgs& a, const Place& p, int head) {
   return a.off_q ? (int64_t)head * a.Sq + p.q0 : ((int64_t)p.b * a.H + head) * a.Sq;
+}
+__device__ __forceinline__ int64_t key_row(const AttnArgs& a, const Place& p) {
+  return a.off_q ? (int64_t)p.hk * a.Sk + p.k0 : ((int64_t)p.b * a.Hkv + p.hk) * a.Sk;
 }
 __device__ __forceinline__ BufRsrc buffer_at(const char* p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), 0, (int)0x80000000u, 0x00020000);
@@ -142,6 +147,23 @@ __device__ __forceinline__ void halves(float x, float& low, float& high) {
 __device__ __forceinline__ float both_sum(float x) { float a, b; halves(x, a, b); return a + b; }
 __device__ __forceinline__ float both_max(float x) { float a, b; halves(x, a, b); return fmaxf(a, b); }
 
+__device__ __forceinline__ u32x4 descriptor(const char* p) {      // (buffer_at's, as four dwords)
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, 0x80000000u, 0x00020000u};
+}
+__device__ __forceinline__ uint32_t lds_at(const unsigned char* p) { return (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)p); }
+
+// Loads straight into LDS, lane l's bytes at `to` + l * BYTES.  Written as one asm statement because the compiler otherwise waits for all such
+// loads in flight before the next LDS read, the next tile's too; wait_tile() waits for them.  No register is written.  The wait states are
+// those that a descriptor just written by a vector instruction, and M0 (which nothing else here uses), need before they are used.
+template <int BYTES> __device__ __forceinline__ void load_to_lds(const u32x4& d, uint32_t off, uint32_t to) {
+  static_assert(BYTES == 4 || BYTES == 16, "one or four dwords a lane");
+  if constexpr (BYTES == 16)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(d), "s"(to) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(d), "s"(to) : "memory");
+}
+
 // ---- LDS tiles ---------------------------------------------------------------------------------------------------------------
 // A tile holds kTile rows of a head as they are in memory, rows of 128, 256 or 512 bytes (what lies behind D is zero), their 16-byte
 // slots permuted: slot s of row r is at s ^ flip(r).  Row fragments (16 bytes of each of 32 rows) then spread over all banks, and so
@@ -164,28 +186,37 @@ template <int ROWB, int NW> struct TileLoad {
       off[i] = slot * 16 < row_bytes ? (uint32_t)(r * stride + slot * 16) : kOob;
     }
   }
-  __device__ __forceinline__ void load(const char* base, int rows, unsigned char* tile, int wave, int lane) const {
-    const BufRsrc r = buffer_at(base);
+  __device__ __forceinline__ void load(const char* base, int rows, uint32_t tile, int wave, int lane) const {
+    const u32x4 r = descriptor(base);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       uint32_t at = off[i];
       if (rows < kTile) at = row(i, wave, lane) < rows ? at : kOob;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_ptr)(tile + (i * NW + wave) * 1024), 16, (int)at, 0, 0, 0);
+      load_to_lds<16>(r, at, tile + (i * NW + wave) * 1024);
     }
   }
 };
 
-// Row fragment: elements 16 kk + 8 (lane / 32) .. + 7 of row `r0` + lane % 32.
-template <typename T, int ROWB> struct RowReader {
-  int base, mask;
-  __device__ __forceinline__ void init(int lane) { base = (lane & 31) * ROWB; mask = flip<ROWB>(lane & 31) << 4 ^ ((lane >> 5) * 8 * (int)sizeof(T)); }
-  __device__ __forceinline__ Frag<T> read(const unsigned char* tile, int r0, int kk) const {
+// Readers hold LDS addresses, one for each k-step or block (the permutation is an XOR, which no offset can stand in for); the stage, the
+// tile and the rows go into the instruction's offset.
+template <typename V> __device__ __forceinline__ V lds_read(uint32_t at, int offset) {
+  return *((__attribute__((address_space(3))) const V*)(uintptr_t)(at + (uint32_t)offset));
+}
+
+// Row fragment: elements 16 kk + 8 (lane / 32) .. + 7 of the row lane % 32 behind `offset`.
+template <typename T, int ROWB, int KK> struct RowReader {
+  uint32_t at[KK];
+  __device__ __forceinline__ void init(uint32_t lds, int lane) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      at[kk] = lds + (lane & 31) * ROWB + ((flip<ROWB>(lane & 31) << 4) ^ ((lane >> 5) * 8 * (int)sizeof(T)) ^ (kk * 16 * (int)sizeof(T)));
+  }
+  __device__ __forceinline__ Frag<T> read(int offset, int kk) const {
     Frag<T> f;
-    const unsigned char* p = tile + r0 * ROWB + base;
     if constexpr (sizeof(T) == 2) {
-      f.u = *reinterpret_cast<const u32x4*>(p + (mask ^ (kk * 32)));
+      f.u = lds_read<u32x4>(at[kk], offset);
     } else {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(p + (mask ^ (kk * 64))), b = *reinterpret_cast<const u32x4*>(p + (mask ^ (kk * 64 + 16)));
+      const u32x4 a = lds_read<u32x4>(at[kk], offset), b = lds_read<u32x4>(at[kk] ^ 16, offset);
 #pragma unroll
       for (int j = 0; j < 4; ++j) { f.f[j] = __uint_as_float(a[j]); f.f[4 + j] = __uint_as_float(b[j]); }
     }
@@ -193,39 +224,52 @@ template <typename T, int ROWB> struct RowReader {
   }
 };
 
-// Transposed fragment: element 32 blk + lane % 32 of rows r0 + 4 h + 0..3 and r0 + 8 + 4 h + 0..3 (h = lane / 32).  bf16: inside every
-// group of 16 lanes the transposing read hands lane i element i % 4 of the 8-byte chunks named by lanes i / 4 + 0, 4, 8, 12.
-template <typename T, int ROWB> struct ColReader {
-  int base[2], mask[2];
-  __device__ __forceinline__ void init(int lane) {
-    const int g = lane >> 4, s = lane & 15;
+// Transposed fragment: element 32 blk + lane % 32 of the rows 4 h + 0..3 and 8 + 4 h + 0..3 (h = lane / 32) behind `offset` (a multiple of
+// 16 rows, which leaves the permutation as it is).  bf16: inside every group of 16 lanes the transposing read hands lane i element i % 4 of
+// the 8-byte chunks named by lanes i / 4 + 0, 4, 8, 12.
+template <typename T, int ROWB, int NB> struct ColReader {
+  uint32_t at[2][sizeof(T) == 2 ? NB : 4];
+  __device__ __forceinline__ void init(uint32_t lds, int lane) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int r = 8 * e + 4 * (g >> 1) + (s >> 2);            // (rows r0 = 0, 16, .. leave the flip as it is)
-      base[e] = r * ROWB;
-      mask[e] = (flip<ROWB>(r) << 4) ^ ((g & 1) * 32 + (s & 3) * 8);
+      if constexpr (sizeof(T) == 2) {
+        const int g = lane >> 4, s = lane & 15, r = 8 * e + 4 * (g >> 1) + (s >> 2);
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) at[e][blk] = lds + r * ROWB + ((flip<ROWB>(r) << 4) ^ ((g & 1) * 32 + (s & 3) * 8) ^ (blk * 64));
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int r = 8 * e + 4 * (lane >> 5) + x;
+          at[e][x] = lds + r * ROWB + ((((lane & 31) >> 2) ^ flip<ROWB>(r)) << 4) + (lane & 3) * 4;
+        }
+      }
     }
   }
-  __device__ __forceinline__ Frag<T> read(const unsigned char* tile, int r0, int blk, int lane) const {
+  __device__ __forceinline__ void shift(int by) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int x = 0; x < (sizeof(T) == 2 ? NB : 4); ++x) at[e][x] += by;
+  }
+  __device__ __forceinline__ Frag<T> read(int offset, int blk) const {
     Frag<T> f;
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const v4s16 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s16*)(tile + r0 * ROWB + base[e] + (mask[e] ^ (blk * 64))));
-        const u32x2 y = __builtin_bit_cast(u32x2, x);
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s16*)(uintptr_t)(at[e][blk] + (uint32_t)offset)));
         f.u[2 * e] = y[0]; f.u[2 * e + 1] = y[1];
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int r = r0 + 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3), d = 32 * blk + (lane & 31);
-        f.f[j] = *reinterpret_cast<const float*>(tile + r * ROWB + (((d >> 2) ^ flip<ROWB>(r)) << 4) + (d & 3) * 4);
-      }
+      for (int j = 0; j < 8; ++j) f.f[j] = lds_read<float>(at[j >> 2][j & 3] ^ (blk * 128), offset);
     }
     return f;
   }
 };
+
+// Fragments that are read ahead of their use (the matrix cores are busy 32 cycles with a bf16 product, 512 with an fp32 one; an LDS read
+// takes over a hundred).
+template <typename T> constexpr int fragments_ahead() { return sizeof(T) == 2 ? 8 : 2; }
 
 // Fragments of 32 rows in memory as an operand whose columns are rows: elements 16 kk + 8 (lane / 32) .. of row lane % 32.
 template <typename T> __device__ __forceinline__ Frag<T> load_row(BufRsrc r, uint32_t row_off, bool there, int kk, int lane, int D) {
@@ -327,19 +371,55 @@ __device__ __forceinline__ void keys_seen(const AttnArgs& a, const Place& p, int
   lo = max(0, c0 - a.left);
   hi = min(p.Lk - 1, c1 + a.right);
 }
+// The loads of a wave's own rows, waited for once: where the compiler does not see them done before the loop it waits for them in there, and for
+// the tiles in flight with them.
+__device__ __forceinline__ void wait_own() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+  __builtin_amdgcn_sched_barrier(0);
+}
 __device__ __forceinline__ void wait_tile() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
 }
 
+template <int N> struct Stage { static constexpr int value = N; };
 template <typename T, int NB> constexpr int row_bytes() { return (NB <= 2 ? 64 : 128) * (int)sizeof(T); }
+
+// ---- the walk along a tile's other axis --------------------------------------------------------------------------------------
+// Two stages of LDS: while the waves compute on one, the other fills.  step(stage, n) computes tile n of the walk from a stage known at
+// compile time; fetch(n, stage) loads it.  Careful: every tile into the first stage, copy() makes the finite copy of it in the
+// second, and the columns are read from there.
+template <typename F, typename S, typename C> __device__ __forceinline__ void walk_tiles(int from, int to, bool careful, F fetch, S step, C copy) {
+  if (from >= to) return;
+  if (!careful) fetch(from, 0);
+  for (int n = from; n < to;) {
+    wait_tile();                               // this tile is there, and no wave reads the other stage any more
+    if (careful) {
+      fetch(n, 0);
+      wait_tile();
+      copy();
+      __syncthreads();
+    } else if (n + 1 < to) {
+      fetch(n + 1, 1);
+    }
+    step(Stage<0>{}, n);
+    ++n;
+    if (careful || n >= to) continue;
+    wait_tile();
+    if (n + 1 < to) fetch(n + 1, 0);
+    step(Stage<1>{}, n);
+    ++n;
+  }
+}
+__device__ __forceinline__ int share(int n, int part, int parts) { return (int)((int64_t)n * part / parts); }
 
 // ---- forward -----------------------------------------------------------------------------------------------------------------
 // The running maximum m (in scores) is raised only where one passes it by kPatience / c: what is summed then stays below 2^kPatience
 // times the sum that the true maximum would give, and few tiles rescale the accumulators.
-template <typename T, int NB, int NW, int OCC>
+template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
-  constexpr int ROWB = row_bytes<T, NB>(), KK = 2 * NB, BM = 32 * NW, STAGE = 2 * kTile * ROWB;
+  constexpr int ROWB = row_bytes<T, NB>(), BM = 32 * NW, TILE = kTile * ROWB, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
   Place p;
   if (!find_place<BM, true>(a, a.G, p)) return;
@@ -357,13 +437,14 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) q[kk] = load_row<T>(r, at, there, kk, lane, a.D);
   }
+  wait_own();
   TileLoad<ROWB, NW> kload, vload;
   kload.init(wave, lane, a.k.token, a.D * (int)sizeof(T));
   vload.init(wave, lane, a.v.token, a.D * (int)sizeof(T));
-  RowReader<T, ROWB> rows;
-  ColReader<T, ROWB> cols;
-  rows.init(lane);
-  cols.init(lane);
+  RowReader<T, ROWB, KK> rows;
+  ColReader<T, ROWB, NB> cols;
+  rows.init(lds_at(lds), lane);
+  cols.init(lds_at(lds) + TILE, lane);
 
   int lo, hi, wlo, whi;                        // keys that the workgroup's and the wave's rows see
   keys_seen(a, p, p.row0, min(p.row0 + BM, p.Lq) - 1, lo, hi);
@@ -372,105 +453,119 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
   const int c = i + p.Lk - p.Lq, mylo = max(0, c - a.left), myhi = min(p.Lk - 1, c + a.right);
   // keys that every row of the wave sees
   const int alllo = max(0, min(i0 + 32, p.Lq) - 1 + p.Lk - p.Lq - a.left), allhi = min(p.Lk - 1, i0 + p.Lk - p.Lq + a.right);
-  const int first = lo / kTile, last = hi / kTile;
-  const bool any = hi >= lo;
+  const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
+  const int from = tile0 + share(tiles, p.part, a.parts), to = tile0 + share(tiles, p.part + 1, a.parts);
 
   f32x16 acc[NB];
   float m, l;
-  auto walk = [&](bool careful) {
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) zero(acc[blk]);
-    m = -kInf; l = 0.0f;
-    if (!any) return;
-    auto fetch = [&](int t, int stage) {
-      unsigned char* s = lds + stage * STAGE;
-      kload.load(kbase + (int64_t)t * kTile * a.k.token, p.Lk - t * kTile, s, wave, lane);
-      vload.load(vbase + (int64_t)t * kTile * a.v.token, p.Lk - t * kTile, s + kTile * ROWB, wave, lane);
+  const float patience = (float)kPatience / a.c;
+  auto fetch = [&](int t, int stage) {
+    const uint32_t s = lds_at(lds) + stage * STAGE;
+    kload.load(kbase + (int64_t)t * kTile * a.k.token, p.Lk - t * kTile, s, wave, lane);
+    vload.load(vbase + (int64_t)t * kTile * a.v.token, p.Lk - t * kTile, s + TILE, wave, lane);
+  };
+  auto step = [&](auto stage, int t) {
+    constexpr int AT = decltype(stage)::value * STAGE;
+    const int j0 = t * kTile;
+    if (j0 > whi || j0 + kTile <= wlo) return;
+    f32x16 s[2];
+    Frag<T> buf[fragments_ahead<T>()];
+    // the keys' rows (block nb, k-step kk), then the values' columns (16 keys, block blk): the first of these are read under the
+    // last products of the scores and are there when the exponentials are
+    constexpr int NK = 2 * KK, NV = 4 * NB, ALL = NK + NV, P = fragments_ahead<T>();
+    auto fragment = [&](int n) {
+      return n < NK ? rows.read(AT + 32 * (n / KK) * ROWB, n % KK) : cols.read(AT + 16 * ((n - NK) / NB) * ROWB, (n - NK) % NB);
     };
-    if (!careful) fetch(first, first & 1);
-    for (int t = first; t <= last; ++t) {
-      wait_tile();                             // this tile is there, and no wave reads the other stage any more
-      if (careful) {
-        fetch(t, 0);
-        wait_tile();
-        copy_finite<T, kTile * ROWB, NW * 64>(lds + kTile * ROWB, lds + STAGE, tid);
-        __syncthreads();
-      } else if (t < last) {
-        fetch(t + 1, t + 1 & 1);
-      }
-      const int j0 = t * kTile;
-      if (j0 > whi || j0 + kTile <= wlo) continue;
-      const unsigned char* const kt = lds + (careful ? 0 : (t & 1) * STAGE);
-      const unsigned char* const vt = careful ? lds + STAGE : kt + kTile * ROWB;
-      f32x16 s[2];
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
-        zero(s[nb]);
+    for (int n = 0; n < P; ++n) if (n < ALL) buf[n] = fragment(n);
+    zero(s[0]);
+    zero(s[1]);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) mma(s[nb], rows.read(kt, 32 * nb, kk), q[kk]);
-      }
-      const bool border = j0 < alllo || j0 + kTile - 1 > allhi;
-      if (border) {
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = j0 + 32 * nb + 8 * (r >> 2) + 4 * half + (r & 3);
-            const bool see = j >= mylo && j <= myhi;
-            s[nb][r] = see ? s[nb][r] : -kInf;
-          }
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[nb][r]);
-      top = both_max(top);
-      const bool rise = top > m + (float)kPatience / a.c;        // (row by row: no row's rounding depends on another's values)
-      if (__any(rise)) {
-        const float up = rise ? top : m, f = rise ? __builtin_amdgcn_exp2f((m - up) * a.c) : 1.0f;
-        m = up; l *= f;
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[blk][r] *= f;
-      }
-      const float mc = m == -kInf ? 0.0f : m * a.c;
+    for (int n = 0; n < NK; ++n) {
+      mma(s[n / KK], buf[n % P], q[n % KK]);
+      if (n + P < ALL) buf[n % P] = fragment(n + P);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+    if (j0 < alllo || j0 + kTile - 1 > allhi) {
+      const int first = mylo - j0 - 4 * half, behind = myhi - j0 - 4 * half;
 #pragma unroll
       for (int nb = 0; nb < 2; ++nb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[nb][r] = __builtin_amdgcn_exp2f(fmaf(s[nb][r], a.c, -mc));
-          l += s[nb][r];
-        }
-#pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const Frag<T> pk = operand<T>(s[nb], kk);
-#pragma unroll
-          for (int blk = 0; blk < NB; ++blk) mma(acc[blk], cols.read(vt, 32 * nb + 16 * kk, blk, lane), pk);
+          const int j = 32 * nb + 8 * (r >> 2) + (r & 3);
+          s[nb][r] = j >= first && j <= behind ? s[nb][r] : -kInf;
         }
     }
+    float top = s[0][0];
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[nb][r]);
+    top = both_max(top);
+    const bool rise = top > m + patience;      // (row by row: no row's rounding depends on another's values)
+    if (__any(rise)) {
+      const float up = rise ? top : m, f = rise ? __builtin_amdgcn_exp2f((m - up) * a.c) : 1.0f;
+      m = up; l *= f;
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[blk][r] *= f;
+    }
+    const float mc = m == -kInf ? 0.0f : m * a.c;
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[nb][r] = __builtin_amdgcn_exp2f(fmaf(s[nb][r], a.c, -mc));
+        sum[r & 1] += s[nb][r];
+      }
+    l += sum[0] + sum[1];
+    Frag<T> pk;
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      if (n % NB == 0) pk = operand<T>(s[n / NB / 2], n / NB % 2);
+      mma(acc[n % NB], buf[(NK + n) % P], pk);
+      if (n + P < NV) buf[(NK + n) % P] = fragment(NK + n + P);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
   };
-  // a NaN may come from a value that a window hides (0 times what is not finite): once more then, with the tiles on a border taken apart
+  // a NaN may come from a value that a window hides (0 times what is not finite): once more then, with the values' finite copy
   bool careful = false;
   for (;;) {
-    walk(careful);
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) zero(acc[blk]);
+    m = -kInf; l = 0.0f;
+    walk_tiles(from, to, careful, fetch, step, [&] { copy_finite<T, TILE, NW * 64>(lds + TILE, lds + STAGE + TILE, tid); });
     if (careful || (a.left >= kFar && a.right >= kFar) || !__syncthreads_or(any_nan<NB>(acc))) break;
     careful = true;
+    cols.shift(STAGE);
   }
-  if (careful && there) spoil<T, NB>(acc, vbase, a.v.token, mylo, myhi, lane, a.D);
+  if (careful && there) spoil<T, NB>(acc, vbase, a.v.token, max(mylo, from * kTile), min(myhi, to * kTile - 1), lane, a.D);
   l = both_sum(l);
+  const int64_t at = stat_row(a, p, head) + i;
+  if (a.parts > 1) {
+    const int64_t row = p.part * a.rows + at;
+    store_rows<float, NB>((char*)(a.part + row * a.D), there, acc, 1.0f, lane, a.D);
+    if (there && half == 0) {
+      float* const ml = a.part + a.parts * a.rows * a.D + 2 * row;
+      ml[0] = m * a.c; ml[1] = l;
+    }
+    return;
+  }
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   store_rows<T, NB>(rows_of(a.o, p.b, p.q0 + i, head), there, acc, inv, lane, a.D);
-  if (there && half == 0) a.lse[stat_row(a, p, head) + i] = l > 0.0f || l != l ? (m * a.c + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
+  if (there && half == 0) a.lse[at] = l > 0.0f || l != l ? (m * a.c + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
 }
 
-// ---- gradient by the queries; D and lse / ln 2 for the pass over the keys ---------------------------------------------------
-template <typename T, int NB, int NW, int OCC>
+// ---- gradient by the queries; -D and lse / ln 2 for the pass over the keys --------------------------------------------------
+template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
-  constexpr int ROWB = row_bytes<T, NB>(), KK = 2 * NB, BM = 32 * NW, STAGE = 2 * kTile * ROWB;
+  constexpr int ROWB = row_bytes<T, NB>(), BM = 32 * NW, TILE = kTile * ROWB, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
   Place p;
   if (!find_place<BM, true>(a, a.G, p)) return;
@@ -500,15 +595,16 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
   const int64_t at = stat_row(a, p, head) + i;
   const float lse = there ? a.lse_in[at] : -kInf;
   const float l2 = lse == -kInf ? kInf : lse * kLog2e;            // (a row that sees nothing: no probability)
-  if (there && half == 0) { a.stats[at] = l2; a.stats[a.rows + at] = delta; }
+  if (there && half == 0 && p.part == 0) { a.stats[at] = l2; a.stats[a.rows + at] = -delta; }
+  wait_own();
 
   TileLoad<ROWB, NW> kload, vload;
   kload.init(wave, lane, a.k.token, a.D * (int)sizeof(T));
   vload.init(wave, lane, a.v.token, a.D * (int)sizeof(T));
-  RowReader<T, ROWB> rows;
-  ColReader<T, ROWB> cols;
-  rows.init(lane);
-  cols.init(lane);
+  RowReader<T, ROWB, KK> rows;
+  ColReader<T, ROWB, NB> cols;
+  rows.init(lds_at(lds), lane);
+  cols.init(lds_at(lds), lane);
 
   int lo, hi, wlo, whi;
   keys_seen(a, p, p.row0, min(p.row0 + BM, p.Lq) - 1, lo, hi);
@@ -516,80 +612,83 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
   if (i0 >= p.Lq) whi = -1;
   const int c = i + p.Lk - p.Lq, mylo = max(0, c - a.left), myhi = min(p.Lk - 1, c + a.right);
   const int alllo = max(0, min(i0 + 32, p.Lq) - 1 + p.Lk - p.Lq - a.left), allhi = min(p.Lk - 1, i0 + p.Lk - p.Lq + a.right);
-  const int first = lo / kTile, last = hi / kTile;
-  const bool any = hi >= lo;
+  const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
+  const int from = tile0 + share(tiles, p.part, a.parts), to = tile0 + share(tiles, p.part + 1, a.parts);
 
   f32x16 acc[NB];
-  auto walk = [&](bool careful) {
+  auto fetch = [&](int t, int stage) {
+    const uint32_t s = lds_at(lds) + stage * STAGE;
+    kload.load(kbase + (int64_t)t * kTile * a.k.token, p.Lk - t * kTile, s, wave, lane);
+    vload.load(vbase + (int64_t)t * kTile * a.v.token, p.Lk - t * kTile, s + TILE, wave, lane);
+  };
+  auto step = [&](auto stage, int t) {
+    constexpr int AT = decltype(stage)::value * STAGE;
+    const int j0 = t * kTile;
+    if (j0 > whi || j0 + kTile <= wlo) return;
+    const bool border = j0 < alllo || j0 + kTile - 1 > allhi;
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk) zero(acc[blk]);
-    if (!any) return;
-    auto fetch = [&](int t, int stage) {
-      unsigned char* s = lds + stage * STAGE;
-      kload.load(kbase + (int64_t)t * kTile * a.k.token, p.Lk - t * kTile, s, wave, lane);
-      vload.load(vbase + (int64_t)t * kTile * a.v.token, p.Lk - t * kTile, s + kTile * ROWB, wave, lane);
-    };
-    if (!careful) fetch(first, first & 1);
-    for (int t = first; t <= last; ++t) {
-      wait_tile();
-      if (careful) {
-        fetch(t, 0);
-        wait_tile();
-        copy_finite<T, kTile * ROWB, NW * 64>(lds, lds + STAGE, tid);
-        __syncthreads();
-      } else if (t < last) {
-        fetch(t + 1, t + 1 & 1);
+    for (int nb = 0; nb < 2; ++nb) {
+      f32x16 s, dp;
+      Frag<T> buf[fragments_ahead<T>()];
+      // rows of the keys, rows of the values, columns of the keys
+      constexpr int N1 = 2 * KK, N2 = 2 * NB, ALL = N1 + N2, P = fragments_ahead<T>();
+      auto fragment = [&](int n) {
+        return n < N1 ? rows.read(AT + (n < KK ? 0 : TILE) + 32 * nb * ROWB, n % KK) : cols.read(AT + (32 * nb + 16 * ((n - N1) / NB)) * ROWB, (n - N1) % NB);
+      };
+#pragma unroll
+      for (int n = 0; n < P; ++n) if (n < ALL) buf[n] = fragment(n);
+      zero(s);
+      zero(dp);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int n = 0; n < N1; ++n) {
+        if (n < KK) mma(s, buf[n % P], q[n]); else mma(dp, buf[n % P], g[n - KK]);
+        if (n + P < ALL) buf[n % P] = fragment(n + P);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const int j0 = t * kTile;
-      if (j0 > whi || j0 + kTile <= wlo) continue;
-      const unsigned char* const kt = lds + (careful ? 0 : (t & 1) * STAGE);
-      const unsigned char* const vt = kt + kTile * ROWB;
-      const unsigned char* const ct = careful ? lds + STAGE : kt;
-      const bool border = j0 < alllo || j0 + kTile - 1 > allhi;
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
-        f32x16 s, dp;
-        zero(s);
-        zero(dp);
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -l2)) * (dp[r] - delta);
+      if (border) {
+        const int first = mylo - j0 - 4 * half, behind = myhi - j0 - 4 * half;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) mma(s, rows.read(kt, 32 * nb, kk), q[kk]);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) mma(dp, rows.read(vt, 32 * nb, kk), g[kk]);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -l2)) * (dp[r] - delta);
-        if (border) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int j = j0 + 32 * nb + 8 * (r >> 2) + 4 * half + (r & 3);
-            const bool see = j >= mylo && j <= myhi;
-            s[r] = see ? s[r] : 0.0f;
-          }
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const Frag<T> ds = operand<T>(s, kk);
-#pragma unroll
-          for (int blk = 0; blk < NB; ++blk) mma(acc[blk], cols.read(ct, 32 * nb + 16 * kk, blk, lane), ds);
+        for (int r = 0; r < 16; ++r) {
+          const int j = 32 * nb + 8 * (r >> 2) + (r & 3);
+          s[r] = j >= first && j <= behind ? s[r] : 0.0f;
         }
       }
+      Frag<T> ds;
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int n = 0; n < N2; ++n) {
+        if (n % NB == 0) ds = operand<T>(s, n / NB);
+        mma(acc[n % NB], buf[(N1 + n) % P], ds);
+        if (n + P < N2) buf[(N1 + n) % P] = fragment(N1 + n + P);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
   bool careful = false;
   for (;;) {
-    walk(careful);
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) zero(acc[blk]);
+    walk_tiles(from, to, careful, fetch, step, [&] { copy_finite<T, TILE, NW * 64>(lds, lds + STAGE, tid); });
     if (careful || (a.left >= kFar && a.right >= kFar) || !__syncthreads_or(any_nan<NB>(acc))) break;
     careful = true;
+    cols.shift(STAGE);
   }
-  if (careful && there) spoil<T, NB>(acc, kbase, a.k.token, mylo, myhi, lane, a.D);
-  store_rows<T, NB>(rows_of(a.dq, p.b, p.q0 + i, head), there, acc, a.scale, lane, a.D);
+  if (careful && there) spoil<T, NB>(acc, kbase, a.k.token, max(mylo, from * kTile), min(myhi, to * kTile - 1), lane, a.D);
+  if (a.parts > 1) store_rows<float, NB>((char*)(a.part + (p.part * a.rows + at) * a.D), there, acc, a.scale, lane, a.D);
+  else store_rows<T, NB>(rows_of(a.dq, p.b, p.q0 + i, head), there, acc, a.scale, lane, a.D);
 }
 
 // ---- gradients by keys and values -------------------------------------------------------------------------------------------
-// A wave owns 32 keys, its lanes a key each, and walks over the queries of every head of its group: no sum leaves the workgroup, and the
-// order is always the same.
-template <typename T, int NB, int NW, int OCC>
+// A wave owns 32 keys, its lanes a key each, and walks over the queries of every head of its group: no sum leaves the workgroup (or the
+// parts, which are added in their order), and the order is always the same.
+template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
-  constexpr int ROWB = row_bytes<T, NB>(), KK = 2 * NB, BN = 32 * NW, TILE = kTile * ROWB, STAGE = 2 * TILE + 2 * kTile * 4;
+  constexpr int ROWB = row_bytes<T, NB>(), BN = 32 * NW, TILE = kTile * ROWB, STATS = 2 * TILE, STAGE = STATS + 2 * kTile * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE];
   Place p;
   if (!find_place<BN, false>(a, 1, p)) return;
@@ -608,13 +707,15 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
       v[kk] = load_row<T>(rv, (uint32_t)(row * a.v.token), there, kk, lane, a.D);
     }
   }
+  wait_own();
   TileLoad<ROWB, NW> qload, gload;
   qload.init(wave, lane, a.q.token, a.D * (int)sizeof(T));
   gload.init(wave, lane, a.d_o.token, a.D * (int)sizeof(T));
-  RowReader<T, ROWB> rows;
-  ColReader<T, ROWB> cols;
-  rows.init(lane);
-  cols.init(lane);
+  RowReader<T, ROWB, KK> rows;
+  ColReader<T, ROWB, NB> cols;
+  rows.init(lds_at(lds), lane);
+  cols.init(lds_at(lds), lane);
+  const uint32_t stats_at = lds_at(lds) + STATS + 16 * half;
 
   // query i sees key j from i = j - right - (Lk - Lq) to i = j + left - (Lk - Lq)
   const int ahead = p.Lk - p.Lq;
@@ -622,141 +723,278 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
   const int wlo = max(0, j0 - a.right - ahead), whi = j0 < p.Lk ? min(p.Lq - 1, min(j0 + 32, p.Lk) - 1 + a.left - ahead) : -1;
   const int mylo = max(0, j - a.right - ahead), myhi = min(p.Lq - 1, j + a.left - ahead);
   const int alllo = max(0, min(j0 + 32, p.Lk) - 1 - a.right - ahead), allhi = j0 + a.left - ahead;      // rows behind Lq add nothing anyway
-  const int first = lo / kTile, last = hi / kTile, tiles = hi >= lo ? last - first + 1 : 0;
+  const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
+  const int from = share(tiles * a.G, p.part, a.parts), to = share(tiles * a.G, p.part + 1, a.parts);      // of the tiles of all heads, one after the other
 
   f32x16 dk[NB], dv[NB];
-  auto walk = [&](bool careful) {
+  int fetched_head = 0, fetched_tile = 0, tile = 0;                    // the next ones
+  auto fetch = [&](int, int stage) {
+    const uint32_t s = lds_at(lds) + stage * STAGE;
+    const int head = p.hk * a.G + fetched_head, row = (tile0 + fetched_tile) * kTile, left = p.Lq - row;
+    qload.load(rows_of(a.q, p.b, p.q0 + row, head), left, s, wave, lane);
+    gload.load(rows_of(a.d_o, p.b, p.q0 + row, head), left, s + TILE, wave, lane);
+    if (wave == 0) {                                   // rows that are not there: lse 0 and D 0 beside do = 0
+      const float* st = a.stats + stat_row(a, p, head) + row;
+      const uint32_t off = lane < left ? lane * 4 : kOob;
+      load_to_lds<4>(descriptor((const char*)st), off, s + STATS);
+      load_to_lds<4>(descriptor((const char*)(st + a.rows)), off, s + STATS + kTile * 4);
+    }
+    if (++fetched_tile == tiles) { fetched_tile = 0; ++fetched_head; }
+  };
+  auto step = [&](auto stage, int) {
+    constexpr int AT = decltype(stage)::value * STAGE;
+    const int i0 = (tile0 + tile) * kTile;
+    if (++tile == tiles) tile = 0;
+    if (i0 > whi || i0 + kTile <= wlo) return;
+    const bool border = i0 < alllo || i0 + kTile - 1 > allhi;
 #pragma unroll
-    for (int blk = 0; blk < NB; ++blk) { zero(dk[blk]); zero(dv[blk]); }
-    const int steps = tiles * a.G;
-    if (steps == 0) return;
-    int ft = first, fg = 0;                              // the next tile to fetch
-    auto fetch = [&](int stage) {
-      unsigned char* s = lds + stage * STAGE;
-      const int head = p.hk * a.G + fg, row = ft * kTile, left = p.Lq - row;
-      qload.load(rows_of(a.q, p.b, p.q0 + row, head), left, s, wave, lane);
-      gload.load(rows_of(a.d_o, p.b, p.q0 + row, head), left, s + TILE, wave, lane);
-      if (wave == 0) {                                   // rows that are not there: lse 0 and D 0 beside do = 0
-        const float* st = a.stats + stat_row(a, p, head) + row;
-        const BufRsrc r0 = buffer_at((const char*)st), r1 = buffer_at((const char*)(st + a.rows));
-        const int off = lane < left ? lane * 4 : (int)kOob;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r0, (lds_void_ptr)(s + 2 * TILE), 4, off, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r1, (lds_void_ptr)(s + 2 * TILE + kTile * 4), 4, off, 0, 0, 0);
+    for (int nb = 0; nb < 2; ++nb) {
+      f32x16 s, dp;
+      Frag<T> buf[fragments_ahead<T>()];
+      // rows of the queries, rows of d_o, columns of d_o and of the queries
+      constexpr int N1 = 2 * KK, N2 = 4 * NB, ALL = N1 + N2, P = fragments_ahead<T>();
+      auto fragment = [&](int n) {
+        return n < N1 ? rows.read(AT + (n < KK ? 0 : TILE) + 32 * nb * ROWB, n % KK)
+                      : cols.read(AT + ((n - N1) % (2 * NB) < NB ? TILE : 0) + (32 * nb + 16 * ((n - N1) / (2 * NB))) * ROWB, (n - N1) % NB);
+      };
+#pragma unroll
+      for (int n = 0; n < P; ++n) if (n < ALL) buf[n] = fragment(n);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {                    // dP - D: the product starts from -D
+        const u32x4 d = lds_read<u32x4>(stats_at, AT + kTile * 4 + (32 * nb + 8 * b) * 4);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) dp[4 * b + x] = __uint_as_float(d[x]);
       }
-      if (++ft > last) { ft = first; ++fg; }
-    };
-    if (!careful) fetch(0);
-    int t = first;
-    for (int n = 0; n < steps; ++n, t = t == last ? first : t + 1) {
-      wait_tile();
-      if (careful) {
-        fetch(0);
-        wait_tile();
-        copy_finite<T, 2 * TILE, NW * 64>(lds, lds + STAGE, tid);
-        __syncthreads();
-      } else if (n + 1 < steps) {
-        fetch(n + 1 & 1);
+      zero(s);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int n = 0; n < N1; ++n) {
+        if (n < KK) mma(s, buf[n % P], k[n]); else mma(dp, buf[n % P], v[n - KK]);
+        if (n + P < ALL) buf[n % P] = fragment(n + P);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const int i0 = t * kTile;
-      if (i0 > whi || i0 + kTile <= wlo) continue;
-      const unsigned char* const qt = lds + (careful ? 0 : (n & 1) * STAGE);
-      const unsigned char* const gt = qt + TILE;
-      const unsigned char* const ct = careful ? lds + STAGE : qt;
-      const float* const st = reinterpret_cast<const float*>(qt + 2 * TILE);
-      const bool border = i0 < alllo || i0 + kTile - 1 > allhi;
+      __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
-        f32x16 s, dp;
-        zero(s);
-        zero(dp);
+      for (int b = 0; b < 4; ++b) {
+        const u32x4 l2 = lds_read<u32x4>(stats_at, AT + (32 * nb + 8 * b) * 4);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) mma(s, rows.read(qt, 32 * nb, kk), k[kk]);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) mma(dp, rows.read(gt, 32 * nb, kk), v[kk]);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const float4 l2 = *reinterpret_cast<const float4*>(st + 32 * nb + 8 * b + 4 * half);
-          const float4 de = *reinterpret_cast<const float4*>(st + kTile + 32 * nb + 8 * b + 4 * half);
-          const float l4[4] = {l2.x, l2.y, l2.z, l2.w}, d4[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int r = 4 * b + x;
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -l4[x]));
-            dp[r] = s[r] * (dp[r] - d4[x]);
-          }
-        }
-        if (border) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int i = i0 + 32 * nb + 8 * (r >> 2) + 4 * half + (r & 3);
-            const bool see = i >= mylo && i <= myhi;
-            s[r] = see ? s[r] : 0.0f;
-            dp[r] = see ? dp[r] : 0.0f;
-          }
-        }
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const Frag<T> pk = operand<T>(s, kk), ds = operand<T>(dp, kk);
-#pragma unroll
-          for (int blk = 0; blk < NB; ++blk) {
-            mma(dv[blk], cols.read(ct + TILE, 32 * nb + 16 * kk, blk, lane), pk);
-            mma(dk[blk], cols.read(ct, 32 * nb + 16 * kk, blk, lane), ds);
-          }
+        for (int x = 0; x < 4; ++x) {
+          const int r = 4 * b + x;
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -__uint_as_float(l2[x])));
+          dp[r] *= s[r];
         }
       }
+      if (border) {
+        const int first = mylo - i0 - 4 * half, behind = myhi - i0 - 4 * half;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = 32 * nb + 8 * (r >> 2) + (r & 3);
+          const bool see = i >= first && i <= behind;
+          s[r] = see ? s[r] : 0.0f;
+          dp[r] = see ? dp[r] : 0.0f;
+        }
+      }
+      Frag<T> pk, ds;
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int n = 0; n < N2; ++n) {
+        if (n % (2 * NB) == 0) { pk = operand<T>(s, n / (2 * NB)); ds = operand<T>(dp, n / (2 * NB)); }
+        if (n % (2 * NB) < NB) mma(dv[n % NB], buf[(N1 + n) % P], pk); else mma(dk[n % NB], buf[(N1 + n) % P], ds);
+        if (n + P < N2) buf[(N1 + n) % P] = fragment(N1 + n + P);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
   bool careful = false;
   for (;;) {
-    walk(careful);
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) { zero(dk[blk]); zero(dv[blk]); }
+    fetched_head = tiles > 0 ? from / tiles : 0;
+    tile = fetched_tile = from - fetched_head * tiles;
+    walk_tiles(from, to, careful, fetch, step, [&] { copy_finite<T, 2 * TILE, NW * 64>(lds, lds + STAGE, tid); });
     if (careful || (a.left >= kFar && a.right >= kFar) || !__syncthreads_or(any_nan<NB>(dk) || any_nan<NB>(dv))) break;
     careful = true;
+    cols.shift(STAGE);
   }
   if (careful && there)
     for (int g = 0; g < a.G; ++g) {
-      spoil<T, NB>(dk, rows_of(a.q, p.b, p.q0, p.hk * a.G + g), a.q.token, mylo, myhi, lane, a.D);
-      spoil<T, NB>(dv, rows_of(a.d_o, p.b, p.q0, p.hk * a.G + g), a.d_o.token, mylo, myhi, lane, a.D);
+      const int t0 = max(from - g * tiles, 0), t1 = min(to - g * tiles, tiles);        // of this head
+      const int r0 = max(mylo, (tile0 + t0) * kTile), r1 = min(myhi, (tile0 + t1) * kTile - 1);
+      spoil<T, NB>(dk, rows_of(a.q, p.b, p.q0, p.hk * a.G + g), a.q.token, r0, r1, lane, a.D);
+      spoil<T, NB>(dv, rows_of(a.d_o, p.b, p.q0, p.hk * a.G + g), a.d_o.token, r0, r1, lane, a.D);
     }
-  store_rows<T, NB>(rows_of(a.dk, p.b, p.k0 + j, p.hk), there, dk, a.scale, lane, a.D);
-  store_rows<T, NB>(rows_of(a.dv, p.b, p.k0 + j, p.hk), there, dv, 1.0f, lane, a.D);
+  if (a.parts > 1) {
+    const int64_t row = p.part * a.key_rows + key_row(a, p) + j;
+    store_rows<float, NB>((char*)(a.part + row * a.D), there, dk, a.scale, lane, a.D);
+    store_rows<float, NB>((char*)(a.part + (a.parts * a.key_rows + row) * a.D), there, dv, 1.0f, lane, a.D);
+  } else {
+    store_rows<T, NB>(rows_of(a.dk, p.b, p.k0 + j, p.hk), there, dk, a.scale, lane, a.D);
+    store_rows<T, NB>(rows_of(a.dv, p.b, p.k0 + j, p.hk), there, dv, 1.0f, lane, a.D);
+  }
+}
+
+// ---- parts into one result ---------------------------------------------------------------------------------------------------
+// Eight elements a thread, the parts in their order.  Forward: weighted by exp2(m c - the largest m c), over the weighted sum of the l.
+struct JoinArgs {
+  const float* part; const float* ml; HeadsArg out; float* lse;
+  const int32_t* off; int B, S, H, D, parts;
+  int64_t rows;
+};
+template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a) {
+  const int vectors = a.D / 8;
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x, row = n / vectors;
+  if (row >= a.rows) return;
+  const int d = (int)(n - row * vectors) * 8;
+  int64_t first = row / a.S;
+  const int i = (int)(row - first * a.S), b = a.off ? 0 : (int)(first / a.H), h = (int)(first - (int64_t)b * a.H);
+  if (a.off && (i < clampi(a.off[0], 0, a.S) || i >= clampi(a.off[a.B], 0, a.S))) return;      // in no sequence
+  float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, top = -kInf, l = 0.0f, factor = 1.0f;
+  if (a.ml) {
+    for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.ml[2 * (p * a.rows + row)]);
+  }
+  for (int p = 0; p < a.parts; ++p) {
+    const float* const src = a.part + (p * a.rows + row) * a.D + d;
+    float w = 1.0f;
+    if (a.ml) {
+      const float m = a.ml[2 * (p * a.rows + row)];
+      w = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+      l += w * a.ml[2 * (p * a.rows + row) + 1];
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float4 v = *reinterpret_cast<const float4*>(src + 4 * j);
+      x[4 * j] += w * v.x; x[4 * j + 1] += w * v.y; x[4 * j + 2] += w * v.z; x[4 * j + 3] += w * v.w;
+    }
+  }
+  if (a.ml) {
+    const bool some = l > 0.0f || l != l;
+    factor = some ? 1.0f / l : 0.0f;
+    if (d == 0) a.lse[row] = some ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
+  }
+  T* const out = reinterpret_cast<T*>(rows_of(a.out, b, i, h)) + d;
+  if constexpr (sizeof(T) == 2) {
+    u32x4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = f2bf_pack(x[2 * j] * factor, x[2 * j + 1] * factor);
+    *reinterpret_cast<u32x4*>(out) = v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) *reinterpret_cast<float4*>(out + 4 * j) = make_float4(x[4 * j] * factor, x[4 * j + 1] * factor, x[4 * j + 2] * factor, x[4 * j + 3] * factor);
+  }
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------------------
 enum { kForward, kGradQ, kGradKV };
+constexpr int kWavesOf = 4, kRows = 32 * kWavesOf, kUnits = 256, kMostParts = 32;
 
-// Tiles and items of a launch; false where it has too many.
-template <int BM, bool QUERIES> bool plan(AttnArgs& a, int per) {
-  const int S = QUERIES ? a.Sq : a.Sk;
-  const int64_t tiles = a.off_q ? (int64_t)S / BM + a.B : ((int64_t)S + BM - 1) / BM;
-  a.groups = a.off_q ? a.Hkv : a.B * a.Hkv;
+// Workgroups of a pass that a compute unit holds: two where 256 registers a lane are enough.
+template <typename T, int NB> constexpr int occupancy(int pass) {
+  return pass == kGradKV ? (sizeof(T) == 2 && NB <= 2 ? 2 : 1) : (sizeof(T) == 2 || NB <= 2 ? 2 : 1);
+}
+int occupancy_of(const dat_attention& s, int pass) {
+  const int nb = (s.D + 31) / 32;
+  return pass == kGradKV ? (s.dtype == DAT_BF16 && nb <= 2 ? 2 : 1) : (s.dtype == DAT_BF16 || nb <= 2 ? 2 : 1);
+}
+
+int64_t tiles_of(const AttnArgs& a, int pass) {
+  const int S = pass == kGradKV ? a.Sk : a.Sq;
+  return a.off_q ? (int64_t)S / kRows + a.B : ((int64_t)S + kRows - 1) / kRows;
+}
+
+// In how many parts a pass walks: where the tiles are too few for the compute units, or too unlike, several workgroups share the walk of each and a
+// launch adds up what they leave.  The estimate counts tiles of the walk: those that the busiest unit takes, three for each workgroup that it
+// starts, and for the launch that adds up eight and its traffic (a tile of the walk takes about as long as 4 MB; fp32: 20 MB).
+int parts_of(const dat_attention& s, const AttnArgs& a, int pass) {
+  const int64_t tiles = tiles_of(a, pass), groups = a.off_q ? a.Hkv : (int64_t)a.B * a.Hkv;
+  const int64_t items = tiles * groups * (pass == kGradKV ? 1 : a.G), slots = (int64_t)kUnits * occupancy_of(s, pass);
+  if (items == 0 || items > 8 * slots || tiles > 65536) return 1;
+  const int seqs = a.off_q ? (a.B > 0 ? a.B : 1) : 1;
+  const int64_t Lq = (a.Sq + seqs - 1) / seqs, Lk = (a.Sk + seqs - 1) / seqs;     // (packed: as if all were alike)
+  int64_t total = 0, most = 0;
+  const int64_t own = pass == kGradKV ? Lk : Lq;
+  for (int64_t r = 0; r < own; r += kRows) {
+    const int64_t end = (r + kRows < own ? r + kRows : own) - 1;
+    int64_t lo, hi;
+    if (pass == kGradKV) { lo = r - a.right - (Lk - Lq); hi = end + a.left - (Lk - Lq); lo = lo > 0 ? lo : 0; hi = hi < Lq - 1 ? hi : Lq - 1; }
+    else { lo = r + Lk - Lq - a.left; hi = end + Lk - Lq + a.right; lo = lo > 0 ? lo : 0; hi = hi < Lk - 1 ? hi : Lk - 1; }
+    const int64_t n = hi >= lo ? (hi / kTile - lo / kTile + 1) * (pass == kGradKV ? a.G : 1) : 0;
+    total += n;
+    most = n > most ? n : most;
+  }
+  total *= seqs * groups * (pass == kGradKV ? 1 : a.G);
+  const bool alike = a.left >= kFar && a.right >= kFar && !a.off_q;
+  const int64_t bytes = (pass == kGradKV ? 2 * a.key_rows : a.rows) * a.D * 4, unit = s.dtype == DAT_BF16 ? 4 << 20 : 20 << 20;
+  int best = 1;
+  double least = 0;
+  for (int p = 1; p <= kMostParts && (p == 1 || p <= most); ++p) {
+    const int64_t rounds = (items * p + slots - 1) / slots, longest = (most + p - 1) / p;
+    const double even = (double)total / slots;
+    double t = (alike ? (double)rounds * longest : even > longest ? even : longest) + 3.0 * rounds;
+    if (p > 1) t += 8.0 + 2.0 * p * bytes / unit;
+    if (p == 1 || t < least) { best = p; least = t; }
+  }
+  return best;
+}
+size_t part_bytes(const AttnArgs& a, int pass, int parts) {
+  if (parts <= 1) return 0;
+  return (size_t)parts * (pass == kGradKV ? 2 * a.key_rows * a.D : a.rows * (a.D + (pass == kForward ? 2 : 0))) * 4;
+}
+
+template <typename T, int NB, int KK> dat_status launch(int pass, AttnArgs a, hipStream_t st) {
+  constexpr int NW = kWavesOf;
+  const int64_t tiles = tiles_of(a, pass), groups = a.off_q ? a.Hkv : (int64_t)a.B * a.Hkv;
+  a.groups = (int)groups;
   a.rows_per_group = (int)tiles;
-  a.items = tiles * a.groups * per;
+  a.items = tiles * groups * (pass == kGradKV ? 1 : a.G) * a.parts;
   // a share of the work for each XCD, whose L2 then holds the keys of few heads; under a window the shares are only alike if each has
   // whole groups
   a.xcd = a.groups % 8 == 0 || (a.left >= kFar && a.right >= kFar);
-  return tiles <= INT32_MAX && a.items + 7 <= INT32_MAX;
-}
-
-template <typename T, int NB, int NW, int OCC> dat_status launch(int pass, AttnArgs a, hipStream_t st) {
-  constexpr int BM = 32 * NW;
-  if (!(pass == kGradKV ? plan<BM, false>(a, 1) : plan<BM, true>(a, a.G)) || !fits_launch(a.items + 7, NW * 64)) return DAT_ERR_SHAPE;
+  if (tiles > INT32_MAX || !fits_launch(a.items + 7, NW * 64)) return DAT_ERR_SHAPE;
   if (a.items == 0) return DAT_OK;
   const dim3 grid((unsigned)(a.xcd ? (a.items + 7) / 8 * 8 : a.items)), block(NW * 64);
-  if (pass == kForward) hipLaunchKernelGGL((attn_fwd_kernel<T, NB, NW, OCC>), grid, block, 0, st, a);
-  else if (pass == kGradQ) hipLaunchKernelGGL((attn_dq_kernel<T, NB, NW, OCC>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((attn_dkv_kernel<T, NB, NW, OCC>), grid, block, 0, st, a);
+  if (pass == kForward) hipLaunchKernelGGL((attn_fwd_kernel<T, NB, KK, NW, occupancy<T, NB>(kForward)>), grid, block, 0, st, a);
+  else if (pass == kGradQ) hipLaunchKernelGGL((attn_dq_kernel<T, NB, KK, NW, occupancy<T, NB>(kGradQ)>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((attn_dkv_kernel<T, NB, KK, NW, occupancy<T, NB>(kGradKV)>), grid, block, 0, st, a);
+  DAT_LAUNCH_CHECK();
+  return DAT_OK;
+}
+
+// Adds up the parts of a pass.
+template <typename T> dat_status join(const AttnArgs& a, const float* part, const float* ml, const HeadsArg& out, bool keys, hipStream_t st) {
+  const int64_t rows = keys ? a.key_rows : a.rows;
+  JoinArgs j{part, ml, out, a.lse, keys ? a.off_k : a.off_q, a.B, keys ? a.Sk : a.Sq, keys ? a.Hkv : a.H, a.D, a.parts, rows};
+  const int64_t blocks = (rows * (a.D / 8) + 255) / 256;
+  if (!fits_launch(blocks, 256)) return DAT_ERR_SHAPE;
+  hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, st, j);
   DAT_LAUNCH_CHECK();
   return DAT_OK;
 }
 
 template <typename T> dat_status launch_heads(int pass, const AttnArgs& a, hipStream_t st) {
-  switch ((a.D + 31) / 32) {
-    case 1: return launch<T, 1, 4, 2>(pass, a, st);
-    case 2: return launch<T, 2, 4, 2>(pass, a, st);
-    case 3: return launch<T, 3, 4, 1>(pass, a, st);
-    default: return launch<T, 4, 4, 1>(pass, a, st);
+  switch ((a.D + 15) / 16) {          // steps of 16 in the products over a head, blocks of 32 in its results
+    case 1: return launch<T, 1, 1>(pass, a, st);
+    case 2: return launch<T, 1, 2>(pass, a, st);
+    case 3: return launch<T, 2, 3>(pass, a, st);
+    case 4: return launch<T, 2, 4>(pass, a, st);
+    case 5: return launch<T, 3, 5>(pass, a, st);
+    case 6: return launch<T, 3, 6>(pass, a, st);
+    case 7: return launch<T, 4, 7>(pass, a, st);
+    default: return launch<T, 4, 8>(pass, a, st);
   }
 }
+template <typename T> dat_status run_pass(int pass, const AttnArgs& a, hipStream_t st) {
+  dat_status r = launch_heads<T>(pass, a, st);
+  if (r != DAT_OK || a.parts <= 1) return r;
+  if (pass == kForward) return join<T>(a, a.part, a.part + a.parts * a.rows * a.D, a.o, false, st);
+  if (pass == kGradQ) return join<T>(a, a.part, nullptr, a.dq, false, st);
+  r = join<T>(a, a.part, nullptr, a.dk, true, st);
+  return r != DAT_OK ? r : join<T>(a, a.part + a.parts * a.key_rows * a.D, nullptr, a.dv, true, st);
+}
+dat_status run_pass(int pass, dat_dtype dtype, const AttnArgs& a, hipStream_t st) {
+  return dtype == DAT_BF16 ? run_pass<bf16_t>(pass, a, st) : run_pass<float>(pass, a, st);
+}
+size_t stats_bytes(const AttnArgs& a) { return (size_t)(2 * a.rows * 4 + 15) / 16 * 16; }
 
 bool fill(const dat_attention* s, AttnArgs& a, dat_status& status) {
   status = DAT_ERR_ARG;
@@ -766,13 +1004,14 @@ bool fill(const dat_attention* s, AttnArgs& a, dat_status& status) {
   status = DAT_ERR_SHAPE;
   if (s->D % 8 || s->D > 128 || s->Sq >= kFar || s->Sk >= kFar) return false;
   const int64_t batches = s->offsets_q ? 1 : s->B;
-  if (batches * s->H * (int64_t)s->Sq >= (int64_t)1 << 40 || (int64_t)s->B * s->Hkv > INT32_MAX) return false;
+  if (batches * s->H * (int64_t)s->Sq >= (int64_t)1 << 40 || batches * s->Hkv * (int64_t)s->Sk >= (int64_t)1 << 40 || (int64_t)s->B * s->Hkv > INT32_MAX) return false;
   a.off_q = s->offsets_q; a.off_k = s->offsets_k;
   a.B = s->B; a.Sq = s->Sq; a.Sk = s->Sk; a.H = s->H; a.Hkv = s->Hkv; a.G = s->H / s->Hkv; a.D = s->D;
   a.left = s->left < 0 ? kFar : s->left < kFar ? s->left : kFar;
   a.right = s->right < 0 ? kFar : s->right < kFar ? s->right : kFar;
   a.scale = s->scale; a.c = s->scale * kLog2e;
   a.rows = batches * s->H * (int64_t)s->Sq;
+  a.key_rows = batches * s->Hkv * (int64_t)s->Sk;
   status = DAT_OK;
   return true;
 }
@@ -806,27 +1045,34 @@ dat_status take_all(std::initializer_list<Tensor> list, size_t width) {
 
 using namespace dat;
 
+extern "C" size_t dat_attention_workspace(int pass, const dat_attention* shape) {
+  AttnArgs a{};
+  dat_status st;
+  if (!fill(shape, a, st) || (pass != 0 && pass != 1)) return 0;
+  if (pass == 0) return part_bytes(a, kForward, parts_of(*shape, a, kForward));
+  // D and lse / ln 2, then the parts of one pass after those of the other
+  const size_t q = part_bytes(a, kGradQ, parts_of(*shape, a, kGradQ)), kv = part_bytes(a, kGradKV, parts_of(*shape, a, kGradKV));
+  return stats_bytes(a) + (q > kv ? q : kv);
+}
+
 extern "C" dat_status dat_attention_forward(const dat_attention* shape, const dat_heads* q, const dat_heads* k, const dat_heads* v,
-                                            const dat_heads* o, float* lse, void* stream) {
+                                            const dat_heads* o, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   AttnArgs a{};
   dat_status st;
   if (!fill(shape, a, st)) return st;
   const int64_t B = a.off_q ? (a.B > 0) : a.B;
   const HeadsShape sq{B, a.Sq, a.H, a.D}, sk{B, a.Sk, a.Hkv, a.D};
   const size_t width = shape->dtype == DAT_BF16 ? 2 : 4;
-  st = take_all(std::initializer_list<Tensor>{{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, true}}, width);
+  st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, true}}, width);
   if (st != DAT_OK) return st;
   if (B == 0 || a.Sq == 0) return DAT_OK;
   if (!lse || !aligned(lse, 4)) return DAT_ERR_ARG;
+  a.parts = parts_of(*shape, a, kForward);
+  const size_t need = part_bytes(a, kForward, a.parts);
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return DAT_ERR_ARG;
   a.lse = lse;
-  return width == 2 ? launch_heads<bf16_t>(kForward, a, (hipStream_t)stream) : launch_heads<float>(kForward, a, (hipStream_t)stream);
-}
-
-extern "C" size_t dat_attention_workspace(int pass, const dat_attention* shape) {
-  AttnArgs a{};
-  dat_status st;
-  if (!fill(shape, a, st) || pass != 1) return 0;
-  return (size_t)(2 * a.rows * 4 + 15) / 16 * 16;
+  a.part = (float*)workspace;
+  return run_pass(kForward, shape->dtype, a, (hipStream_t)stream);
 }
 
 extern "C" dat_status dat_attention_backward(const dat_attention* shape, const dat_heads* q, const dat_heads* k, const dat_heads* v,
@@ -838,17 +1084,22 @@ extern "C" dat_status dat_attention_backward(const dat_attention* shape, const d
   const int64_t B = a.off_q ? (a.B > 0) : a.B;
   const HeadsShape sq{B, a.Sq, a.H, a.D}, sk{B, a.Sk, a.Hkv, a.D};
   const size_t width = shape->dtype == DAT_BF16 ? 2 : 4;
-  st = take_all(std::initializer_list<Tensor>{{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, false}, {d_o, sq, &a.d_o, false},
-                                              {dq, sq, &a.dq, true}, {dk, sk, &a.dk, true}, {dv, sk, &a.dv, true}}, width);
+  st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, false}, {d_o, sq, &a.d_o, false},
+                 {dq, sq, &a.dq, true}, {dk, sk, &a.dk, true}, {dv, sk, &a.dv, true}}, width);
   if (st != DAT_OK) return st;
   if (B == 0) return DAT_OK;
+  if (a.Sq > 0 && (!lse || !aligned(lse, 4))) return DAT_ERR_ARG;
+  const size_t need = dat_attention_workspace(1, shape);
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return DAT_ERR_ARG;
+  a.lse_in = lse;
+  a.stats = (float*)workspace;
+  a.part = (float*)((char*)workspace + stats_bytes(a));
   if (a.Sq > 0) {
-    if (!lse || !aligned(lse, 4) || !workspace || !aligned(workspace, 16) || workspace_bytes < dat_attention_workspace(1, shape)) return DAT_ERR_ARG;
-    a.lse_in = lse;
-    a.stats = (float*)workspace;
-    st = width == 2 ? launch_heads<bf16_t>(kGradQ, a, (hipStream_t)stream) : launch_heads<float>(kGradQ, a, (hipStream_t)stream);
+    a.parts = parts_of(*shape, a, kGradQ);
+    st = run_pass(kGradQ, shape->dtype, a, (hipStream_t)stream);
     if (st != DAT_OK) return st;
   }
   if (a.Sk == 0) return DAT_OK;
-  return width == 2 ? launch_heads<bf16_t>(kGradKV, a, (hipStream_t)stream) : launch_heads<float>(kGradKV, a, (hipStream_t)stream);
+  a.parts = parts_of(*shape, a, kGradKV);
+  return run_pass(kGradKV, shape->dtype, a, (hipStream_t)stream);
 }

@@ -33,7 +33,7 @@ def attn(backward=False, lse=P, ws=P, size=1 << 40, stream=None, t=None, **kw):
         tensors[name] = heads(n, S, H, d["D"], **(t[1] if t and t[0] == name else {}))
     x = tensors
     if not backward:
-        return lib.dat_attention_forward(shape, x["q"], x["k"], x["v"], x["o"], lse, stream)
+        return lib.dat_attention_forward(shape, x["q"], x["k"], x["v"], x["o"], lse, ws, size, stream)
     return lib.dat_attention_backward(shape, x["q"], x["k"], x["v"], x["o"], lse, x["do"], x["dq"], x["dk"], x["dv"], ws, size, stream)
 
 
@@ -60,8 +60,8 @@ def test_attention_backward_refuses(status, kw):
 
 def test_attention_refuses_null_structs_and_has_nothing_to_do():
     h, s = heads(0, 10, 4, 16), b._Attention(**BASE)
-    assert lib.dat_attention_forward(None, h, h, h, h, P, None) == 1 and lib.dat_attention_forward(s, None, h, h, h, P, None) == 1
-    assert lib.dat_attention_forward(s, h, h, h, None, P, None) == 1
+    assert lib.dat_attention_forward(None, h, h, h, h, P, None, 0, None) == 1 and lib.dat_attention_forward(s, None, h, h, h, P, None, 0, None) == 1
+    assert lib.dat_attention_forward(s, h, h, h, None, P, None, 0, None) == 1
     assert lib.dat_attention_backward(s, h, h, h, h, P, h, h, h, None, P, 1 << 20, None) == 1
     assert attn(B=0) == 0 and attn(backward=True, B=0, lse=None, ws=None, size=0) == 0 and attn(Sq=0, lse=None) == 0
     assert attn(B=0, offsets_q=P, offsets_k=P) == 0 and attn(backward=True, Sq=0, Sk=0, ws=None, size=0) == 0
