@@ -41,7 +41,8 @@ struct AttnArgs {
   float scale, c;                                        // c = scale / ln 2
   int rows_per_group, groups, xcd;                       // tiles of a group of heads; groups; 1: a contiguous share of the work for each XCD
   int parts;                                             // workgroups that share the walk of a tile
-  int64_t items, rows, key_rows;                         // rows = B * H * Sq (H * Sq packed), key_rows = B * Hkv * Sk
+  int items;
+  int64_t rows, key_rows;                                // rows = B * H * Sq (H * Sq packed), key_rows = B * Hkv * Sk
   float* part;                                           // their results in fp32: [parts][rows][D], then [parts][rows][2] (forward: m c and l)
 };
 
@@ -61,23 +62,25 @@ __device__ __forceinline__ void sequence(const int32_t* off, int b, int T, int& 
 // handled apart).
 template <int BM, bool QUERIES>
 __device__ __forceinline__ bool find_place(const AttnArgs& a, int per, Place& p) {
-  int64_t item = blockIdx.x;
-  if (a.xcd) item = (int64_t)(blockIdx.x & 7) * ((a.items + 7) >> 3) + (blockIdx.x >> 3);
-  if (item >= a.items) return false;
-  const int t = (int)(item / (per * a.parts)), within = (int)(item - (int64_t)t * per * a.parts);
-  p.g = within / a.parts;
+  uint32_t item = blockIdx.x;
+  if (a.xcd) item = (blockIdx.x & 7) * (((uint32_t)a.items + 7) >> 3) + (blockIdx.x >> 3);
+  if (item >= (uint32_t)a.items) return false;
+  const int each = per * a.parts, t = (int)(item / (uint32_t)each), within = (int)item - t * each;
+  p.g = (uint32_t)within / (uint32_t)a.parts;
   p.part = within - p.g * a.parts;
-  const int group = t / a.rows_per_group;
+  const int group = (int)((uint32_t)t / (uint32_t)a.rows_per_group);
   int tile = a.rows_per_group - 1 - (t - group * a.rows_per_group);
   if (!QUERIES) tile = t - group * a.rows_per_group;      // early keys are seen by the most queries
   if (a.off_q) {
     p.hk = group;
     const int32_t* off = QUERIES ? a.off_q : a.off_k;
     const int T = QUERIES ? a.Sq : a.Sk;
-    int lo = 0, hi = a.B;
+    int lo = 0, hi = a.B;                                // the last sequence whose first slot is not behind the tile's: the lanes try 64 places at once
     while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (clampi(off[mid], 0, T) / BM + mid <= tile) lo = mid; else hi = mid;
+      const int stride = (hi - lo + 63) >> 6, at = lo + (int)(threadIdx.x & 63) * stride;
+      const uint64_t before = __ballot(at < hi && clampi(off[min(at, hi - 1)], 0, T) / BM + at <= tile);
+      lo += max(__popcll(before) - 1, 0) * stride;
+      hi = min(lo + stride, hi);
     }
     p.b = lo;
     sequence(a.off_q, p.b, a.Sq, p.q0, p.Lq);
@@ -86,7 +89,7 @@ __device__ __forceinline__ bool find_place(const AttnArgs& a, int per, Place& p)
     if (j < 0 || (int64_t)j * BM >= (QUERIES ? p.Lq : p.Lk)) return false;
     p.row0 = j * BM;
   } else {
-    p.b = group / a.Hkv;
+    p.b = (int)((uint32_t)group / (uint32_t)a.Hkv);
     p.hk = group - p.b * a.Hkv;
     p.row0 = tile * BM;
     p.q0 = p.k0 = 0; p.Lq = a.Sq; p.Lk = a.Sk;
@@ -165,25 +168,27 @@ template <int BYTES> __device__ __forceinline__ void load_to_lds(const u32x4& d,
 }
 
 // ---- LDS tiles ---------------------------------------------------------------------------------------------------------------
-// A tile holds kTile rows of a head as they are in memory, rows of 128, 256 or 512 bytes (what lies behind D is zero), their 16-byte
-// slots permuted: slot s of row r is at s ^ flip(r).  Row fragments (16 bytes of each of 32 rows) then spread over all banks, and so
-// do the transposing reads, whose half-waves take 64 bytes of each of four consecutive rows.
+// A tile holds kTile rows of a head as they are in memory (what lies between D and 32 NB is zero), their 16-byte slots permuted: slot s of row r
+// is at s ^ flip(r).  The 16 rows that a row fragment's read takes at once then lie in 16 different places of the 256 bytes that the banks
+// cover, and so do the 64 bytes of each of four consecutive rows that half a wave's transposing read takes.
 template <int ROWB> __device__ __forceinline__ int flip(int r) {
-  if (ROWB == 128) return (r & 1) | ((r >> 2 & 1) << 1) | ((r >> 1 & 1) << 2);
-  if (ROWB == 256) return ((r & 3) << 2) | (r >> 2 & 3);
-  return r & 7;
+  constexpr int apart = ROWB / 16 % 16;            // from row to row, in slots, around the banks
+  if (apart == 4 || apart == 12) return r >> 2 & 3;                                                   // every fourth row on the same place
+  if (apart == 8) return ROWB == 128 ? ((r >> 1 & 1) << 2) | ((r >> 2 & 1) << 1) | (r >> 3 & 1) : r >> 1 & 7;  // every other one
+  return ROWB == 256 ? ((r & 3) << 2) | (r >> 2 & 3) : r & 15;
 }
 
 // Loads of a tile straight into LDS: a wave's instruction fills 1 KB, the lane that fills slot p of row r fetches slot p ^ flip(r).
 template <int ROWB, int NW> struct TileLoad {
-  static constexpr int NS = ROWB / 16, N = kTile * NS / 64 / NW, RPI = 64 / NS;
+  static constexpr int NS = ROWB / 16, N = kTile * NS / 64 / NW;
+  static_assert(kTile * NS % (64 * NW) == 0, "whole instructions of every wave");
   uint32_t off[N];
-  __device__ __forceinline__ static int row(int i, int wave, int lane) { return (i * NW + wave) * RPI + lane / NS; }
+  __device__ __forceinline__ static int row(int i, int wave, int lane) { return (uint32_t)((i * NW + wave) * 64 + lane) / (uint32_t)NS; }
   __device__ __forceinline__ void init(int wave, int lane, int64_t stride, int row_bytes) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = row(i, wave, lane), slot = (lane % NS) ^ flip<ROWB>(r);
-      off[i] = slot * 16 < row_bytes ? (uint32_t)(r * stride + slot * 16) : kOob;
+      const int r = row(i, wave, lane), slot = ((i * NW + wave) * 64 + lane - r * NS) ^ flip<ROWB>(r);
+      off[i] = slot * 16 < row_bytes ? (uint32_t)r * (uint32_t)stride + slot * 16 : kOob;
     }
   }
   __device__ __forceinline__ void load(const char* base, int rows, uint32_t tile, int wave, int lane) const {
@@ -261,7 +266,10 @@ template <typename T, int ROWB, int NB> struct ColReader {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f.f[j] = lds_read<float>(at[j >> 2][j & 3] ^ (blk * 128), offset);
+      for (int j = 0; j < 8; ++j) {           // (rows of 384 bytes: the permutation stays within 128, and the rows do not begin at multiples of 256)
+        const uint32_t row = at[j >> 2][j & 3];
+        f.f[j] = lds_read<float>(ROWB == 384 ? row + blk * 128 : row ^ (blk * 128), offset);
+      }
     }
     return f;
   }
@@ -384,15 +392,13 @@ __device__ __forceinline__ void wait_tile() {
 }
 
 template <int N> struct Stage { static constexpr int value = N; };
-template <typename T, int NB> constexpr int row_bytes() { return (NB <= 2 ? 64 : 128) * (int)sizeof(T); }
+template <typename T, int NB> constexpr int row_bytes() { return 32 * NB * (int)sizeof(T); }
 
 // ---- the walk along a tile's other axis --------------------------------------------------------------------------------------
 // Two stages of LDS: while the waves compute on one, the other fills.  step(stage, n) computes tile n of the walk from a stage known at
 // compile time; fetch(n, stage) loads it.  Careful: every tile into the first stage, copy() makes the finite copy of it in the
 // second, and the columns are read from there.
 template <typename F, typename S, typename C> __device__ __forceinline__ void walk_tiles(int from, int to, bool careful, F fetch, S step, C copy) {
-  if (from >= to) return;
-  if (!careful) fetch(from, 0);
   for (int n = from; n < to;) {
     wait_tile();                               // this tile is there, and no wave reads the other stage any more
     if (careful) {
@@ -412,7 +418,7 @@ template <typename F, typename S, typename C> __device__ __forceinline__ void wa
     ++n;
   }
 }
-__device__ __forceinline__ int share(int n, int part, int parts) { return (int)((int64_t)n * part / parts); }
+__device__ __forceinline__ int share(int n, int part, int parts) { return parts == 1 ? n * part : (int)((int64_t)n * part / parts); }
 
 // ---- forward -----------------------------------------------------------------------------------------------------------------
 // The running maximum m (in scores) is raised only where one passes it by kPatience / c: what is summed then stays below 2^kPatience
@@ -430,14 +436,6 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
   const char* const kbase = rows_of(a.k, p.b, p.k0, p.hk);
   const char* const vbase = rows_of(a.v, p.b, p.k0, p.hk);
 
-  Frag<T> q[KK];
-  {
-    const BufRsrc r = buffer_at(rows_of(a.q, p.b, p.q0 + p.row0, head));
-    const uint32_t at = (uint32_t)((32 * wave + (lane & 31)) * a.q.token);
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[kk] = load_row<T>(r, at, there, kk, lane, a.D);
-  }
-  wait_own();
   TileLoad<ROWB, NW> kload, vload;
   kload.init(wave, lane, a.k.token, a.D * (int)sizeof(T));
   vload.init(wave, lane, a.v.token, a.D * (int)sizeof(T));
@@ -456,14 +454,24 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
   const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
   const int from = tile0 + share(tiles, p.part, a.parts), to = tile0 + share(tiles, p.part + 1, a.parts);
 
-  f32x16 acc[NB];
-  float m, l;
-  const float patience = (float)kPatience / a.c;
   auto fetch = [&](int t, int stage) {
     const uint32_t s = lds_at(lds) + stage * STAGE;
     kload.load(kbase + (int64_t)t * kTile * a.k.token, p.Lk - t * kTile, s, wave, lane);
     vload.load(vbase + (int64_t)t * kTile * a.v.token, p.Lk - t * kTile, s + TILE, wave, lane);
   };
+  if (from < to) fetch(from, 0);               // under way while the wave's own rows come
+  Frag<T> q[KK];
+  {
+    const BufRsrc r = buffer_at(rows_of(a.q, p.b, p.q0 + p.row0, head));
+    const uint32_t at = (uint32_t)(32 * wave + (lane & 31)) * (uint32_t)a.q.token;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = load_row<T>(r, at, there, kk, lane, a.D);
+  }
+  wait_own();
+
+  f32x16 acc[NB];
+  float m, l;
+  const float patience = (float)kPatience / a.c;
   auto step = [&](auto stage, int t) {
     constexpr int AT = decltype(stage)::value * STAGE;
     const int j0 = t * kTile;
@@ -480,14 +488,12 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
     for (int n = 0; n < P; ++n) if (n < ALL) buf[n] = fragment(n);
     zero(s[0]);
     zero(s[1]);
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int n = 0; n < NK; ++n) {
       mma(s[n / KK], buf[n % P], q[n % KK]);
       if (n + P < ALL) buf[n % P] = fragment(n + P);
       __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_s_setprio(0);
     if (j0 < alllo || j0 + kTile - 1 > allhi) {
       const int first = mylo - j0 - 4 * half, behind = myhi - j0 - 4 * half;
 #pragma unroll
@@ -524,7 +530,6 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
       }
     l += sum[0] + sum[1];
     Frag<T> pk;
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       if (n % NB == 0) pk = operand<T>(s[n / NB / 2], n / NB % 2);
@@ -532,7 +537,6 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
       if (n + P < NV) buf[(NK + n) % P] = fragment(NK + n + P);
       __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_s_setprio(0);
   };
   // a NaN may come from a value that a window hides (0 times what is not finite): once more then, with the values' finite copy
   bool careful = false;
@@ -576,28 +580,6 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
   const char* const kbase = rows_of(a.k, p.b, p.k0, p.hk);
   const char* const vbase = rows_of(a.v, p.b, p.k0, p.hk);
 
-  Frag<T> q[KK], g[KK];
-  float delta = 0.0f;
-  {
-    const BufRsrc rq = buffer_at(rows_of(a.q, p.b, p.q0 + p.row0, head)), rg = buffer_at(rows_of(a.d_o, p.b, p.q0 + p.row0, head)),
-                  ro = buffer_at(rows_of(a.o, p.b, p.q0 + p.row0, head));
-    const int row = 32 * wave + (lane & 31);
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      q[kk] = load_row<T>(rq, (uint32_t)(row * a.q.token), there, kk, lane, a.D);
-      g[kk] = load_row<T>(rg, (uint32_t)(row * a.d_o.token), there, kk, lane, a.D);
-      const Frag<T> o = load_row<T>(ro, (uint32_t)(row * a.o.token), there, kk, lane, a.D);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) delta = fmaf(element(g[kk], j), element(o, j), delta);
-    }
-  }
-  delta = both_sum(delta);
-  const int64_t at = stat_row(a, p, head) + i;
-  const float lse = there ? a.lse_in[at] : -kInf;
-  const float l2 = lse == -kInf ? kInf : lse * kLog2e;            // (a row that sees nothing: no probability)
-  if (there && half == 0 && p.part == 0) { a.stats[at] = l2; a.stats[a.rows + at] = -delta; }
-  wait_own();
-
   TileLoad<ROWB, NW> kload, vload;
   kload.init(wave, lane, a.k.token, a.D * (int)sizeof(T));
   vload.init(wave, lane, a.v.token, a.D * (int)sizeof(T));
@@ -615,12 +597,35 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
   const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
   const int from = tile0 + share(tiles, p.part, a.parts), to = tile0 + share(tiles, p.part + 1, a.parts);
 
-  f32x16 acc[NB];
   auto fetch = [&](int t, int stage) {
     const uint32_t s = lds_at(lds) + stage * STAGE;
     kload.load(kbase + (int64_t)t * kTile * a.k.token, p.Lk - t * kTile, s, wave, lane);
     vload.load(vbase + (int64_t)t * kTile * a.v.token, p.Lk - t * kTile, s + TILE, wave, lane);
   };
+  if (from < to) fetch(from, 0);
+  Frag<T> q[KK], g[KK];
+  float delta = 0.0f;
+  {
+    const BufRsrc rq = buffer_at(rows_of(a.q, p.b, p.q0 + p.row0, head)), rg = buffer_at(rows_of(a.d_o, p.b, p.q0 + p.row0, head)),
+                  ro = buffer_at(rows_of(a.o, p.b, p.q0 + p.row0, head));
+    const int row = 32 * wave + (lane & 31);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      q[kk] = load_row<T>(rq, (uint32_t)row * (uint32_t)a.q.token, there, kk, lane, a.D);
+      g[kk] = load_row<T>(rg, (uint32_t)row * (uint32_t)a.d_o.token, there, kk, lane, a.D);
+      const Frag<T> o = load_row<T>(ro, (uint32_t)row * (uint32_t)a.o.token, there, kk, lane, a.D);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = fmaf(element(g[kk], j), element(o, j), delta);
+    }
+  }
+  delta = both_sum(delta);
+  const int64_t at = stat_row(a, p, head) + i;
+  const float lse = there ? a.lse_in[at] : -kInf;
+  const float l2 = lse == -kInf ? kInf : lse * kLog2e;            // (a row that sees nothing: no probability)
+  if (there && half == 0 && p.part == 0) { a.stats[at] = l2; a.stats[a.rows + at] = -delta; }
+  wait_own();
+
+  f32x16 acc[NB];
   auto step = [&](auto stage, int t) {
     constexpr int AT = decltype(stage)::value * STAGE;
     const int j0 = t * kTile;
@@ -639,15 +644,13 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
       for (int n = 0; n < P; ++n) if (n < ALL) buf[n] = fragment(n);
       zero(s);
       zero(dp);
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
+  #pragma unroll
       for (int n = 0; n < N1; ++n) {
         if (n < KK) mma(s, buf[n % P], q[n]); else mma(dp, buf[n % P], g[n - KK]);
         if (n + P < ALL) buf[n % P] = fragment(n + P);
         __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_s_setprio(0);
-#pragma unroll
+  #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c, -l2)) * (dp[r] - delta);
       if (border) {
         const int first = mylo - j0 - 4 * half, behind = myhi - j0 - 4 * half;
@@ -658,16 +661,14 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
         }
       }
       Frag<T> ds;
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
+  #pragma unroll
       for (int n = 0; n < N2; ++n) {
         if (n % NB == 0) ds = operand<T>(s, n / NB);
         mma(acc[n % NB], buf[(N1 + n) % P], ds);
         if (n + P < N2) buf[(N1 + n) % P] = fragment(N1 + n + P);
         __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_s_setprio(0);
-    }
+      }
   };
   bool careful = false;
   for (;;) {
@@ -703,8 +704,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
     const int row = 32 * wave + (lane & 31);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      k[kk] = load_row<T>(rk, (uint32_t)(row * a.k.token), there, kk, lane, a.D);
-      v[kk] = load_row<T>(rv, (uint32_t)(row * a.v.token), there, kk, lane, a.D);
+      k[kk] = load_row<T>(rk, (uint32_t)row * (uint32_t)a.k.token, there, kk, lane, a.D);
+      v[kk] = load_row<T>(rv, (uint32_t)row * (uint32_t)a.v.token, there, kk, lane, a.D);
     }
   }
   wait_own();
@@ -726,8 +727,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
   const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
   const int from = share(tiles * a.G, p.part, a.parts), to = share(tiles * a.G, p.part + 1, a.parts);      // of the tiles of all heads, one after the other
 
-  f32x16 dk[NB], dv[NB];
-  int fetched_head = 0, fetched_tile = 0, tile = 0;                    // the next ones
+  const int from_head = tiles > 0 ? from / tiles : 0, from_tile = from - from_head * tiles;
+  int fetched_head = from_head, fetched_tile = from_tile, tile = from_tile;      // the next ones
   auto fetch = [&](int, int stage) {
     const uint32_t s = lds_at(lds) + stage * STAGE;
     const int head = p.hk * a.G + fetched_head, row = (tile0 + fetched_tile) * kTile, left = p.Lq - row;
@@ -741,6 +742,9 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
     }
     if (++fetched_tile == tiles) { fetched_tile = 0; ++fetched_head; }
   };
+  if (from < to) fetch(from, 0);
+
+  f32x16 dk[NB], dv[NB];
   auto step = [&](auto stage, int) {
     constexpr int AT = decltype(stage)::value * STAGE;
     const int i0 = (tile0 + tile) * kTile;
@@ -766,15 +770,13 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
         for (int x = 0; x < 4; ++x) dp[4 * b + x] = __uint_as_float(d[x]);
       }
       zero(s);
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
+  #pragma unroll
       for (int n = 0; n < N1; ++n) {
         if (n < KK) mma(s, buf[n % P], k[n]); else mma(dp, buf[n % P], v[n - KK]);
         if (n + P < ALL) buf[n % P] = fragment(n + P);
         __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_s_setprio(0);
-#pragma unroll
+  #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const u32x4 l2 = lds_read<u32x4>(stats_at, AT + (32 * nb + 8 * b) * 4);
 #pragma unroll
@@ -795,27 +797,25 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
         }
       }
       Frag<T> pk, ds;
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
+  #pragma unroll
       for (int n = 0; n < N2; ++n) {
         if (n % (2 * NB) == 0) { pk = operand<T>(s, n / (2 * NB)); ds = operand<T>(dp, n / (2 * NB)); }
         if (n % (2 * NB) < NB) mma(dv[n % NB], buf[(N1 + n) % P], pk); else mma(dk[n % NB], buf[(N1 + n) % P], ds);
         if (n + P < N2) buf[(N1 + n) % P] = fragment(N1 + n + P);
         __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_s_setprio(0);
-    }
+      }
   };
   bool careful = false;
   for (;;) {
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) { zero(dk[blk]); zero(dv[blk]); }
-    fetched_head = tiles > 0 ? from / tiles : 0;
-    tile = fetched_tile = from - fetched_head * tiles;
     walk_tiles(from, to, careful, fetch, step, [&] { copy_finite<T, 2 * TILE, NW * 64>(lds, lds + STAGE, tid); });
     if (careful || (a.left >= kFar && a.right >= kFar) || !__syncthreads_or(any_nan<NB>(dk) || any_nan<NB>(dv))) break;
     careful = true;
     cols.shift(STAGE);
+    fetched_head = from_head;
+    tile = fetched_tile = from_tile;
   }
   if (careful && there)
     for (int g = 0; g < a.G; ++g) {
@@ -837,7 +837,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
 // ---- parts into one result ---------------------------------------------------------------------------------------------------
 // Eight elements a thread, the parts in their order.  Forward: weighted by exp2(m c - the largest m c), over the weighted sum of the l.
 struct JoinArgs {
-  const float* part; const float* ml; HeadsArg out; float* lse;
+  const float* part; const float* ml; HeadsArg out, second; float* lse;      // second: of the parts behind these (dv behind dk)
   const int32_t* off; int B, S, H, D, parts;
   int64_t rows;
 };
@@ -849,12 +849,13 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(Jo
   int64_t first = row / a.S;
   const int i = (int)(row - first * a.S), b = a.off ? 0 : (int)(first / a.H), h = (int)(first - (int64_t)b * a.H);
   if (a.off && (i < clampi(a.off[0], 0, a.S) || i >= clampi(a.off[a.B], 0, a.S))) return;      // in no sequence
+  const float* const parts = a.part + (int64_t)blockIdx.y * a.parts * a.rows * a.D;
   float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, top = -kInf, l = 0.0f, factor = 1.0f;
   if (a.ml) {
     for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.ml[2 * (p * a.rows + row)]);
   }
   for (int p = 0; p < a.parts; ++p) {
-    const float* const src = a.part + (p * a.rows + row) * a.D + d;
+    const float* const src = parts + (p * a.rows + row) * a.D + d;
     float w = 1.0f;
     if (a.ml) {
       const float m = a.ml[2 * (p * a.rows + row)];
@@ -872,7 +873,7 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(Jo
     factor = some ? 1.0f / l : 0.0f;
     if (d == 0) a.lse[row] = some ? (top + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
   }
-  T* const out = reinterpret_cast<T*>(rows_of(a.out, b, i, h)) + d;
+  T* const out = reinterpret_cast<T*>(rows_of(blockIdx.y ? a.second : a.out, b, i, h)) + d;
   if constexpr (sizeof(T) == 2) {
     u32x4 v;
 #pragma unroll
@@ -890,7 +891,7 @@ constexpr int kWavesOf = 4, kRows = 32 * kWavesOf, kUnits = 256, kMostParts = 32
 
 // Workgroups of a pass that a compute unit holds: two where 256 registers a lane are enough.
 template <typename T, int NB> constexpr int occupancy(int pass) {
-  return pass == kGradKV ? (sizeof(T) == 2 && NB <= 2 ? 2 : 1) : (sizeof(T) == 2 || NB <= 2 ? 2 : 1);
+  return pass == kGradKV ? (sizeof(T) == 2 && NB <= 2 ? 2 : 1) : sizeof(T) == 2 && NB <= 2 ? 3 : (sizeof(T) == 2 || NB <= 2 ? 2 : 1);
 }
 int occupancy_of(const dat_attention& s, int pass) {
   const int nb = (s.D + 31) / 32;
@@ -903,8 +904,9 @@ int64_t tiles_of(const AttnArgs& a, int pass) {
 }
 
 // In how many parts a pass walks: where the tiles are too few for the compute units, or too unlike, several workgroups share the walk of each and a
-// launch adds up what they leave.  The estimate counts tiles of the walk: those that the busiest unit takes, three for each workgroup that it
-// starts, and for the launch that adds up eight and its traffic (a tile of the walk takes about as long as 4 MB; fp32: 20 MB).
+// launch adds up what they leave.  The estimate is in tiles of the walk (about 1 us in bf16, 8 in fp32): those that the busiest unit takes, the
+// start of a workgroup (3 us), and for the launch that adds up 7 us and its traffic at 4 TB/s.  Measured: 2 x 6001 tokens, 16 heads of
+// 128 on 4 key heads, causal: dk and dv 861 us in one part (376 unlike tiles on 256 units), 698 + 22 us in two.
 int parts_of(const dat_attention& s, const AttnArgs& a, int pass) {
   const int64_t tiles = tiles_of(a, pass), groups = a.off_q ? a.Hkv : (int64_t)a.B * a.Hkv;
   const int64_t items = tiles * groups * (pass == kGradKV ? 1 : a.G), slots = (int64_t)kUnits * occupancy_of(s, pass);
@@ -924,14 +926,14 @@ int parts_of(const dat_attention& s, const AttnArgs& a, int pass) {
   }
   total *= seqs * groups * (pass == kGradKV ? 1 : a.G);
   const bool alike = a.left >= kFar && a.right >= kFar && !a.off_q;
-  const int64_t bytes = (pass == kGradKV ? 2 * a.key_rows : a.rows) * a.D * 4, unit = s.dtype == DAT_BF16 ? 4 << 20 : 20 << 20;
+  const double us = s.dtype == DAT_BF16 ? 1.0 : 8.0, traffic = 2.0 * (pass == kGradKV ? 2 * a.key_rows : a.rows) * a.D * 4 / 4e6;
   int best = 1;
   double least = 0;
   for (int p = 1; p <= kMostParts && (p == 1 || p <= most); ++p) {
     const int64_t rounds = (items * p + slots - 1) / slots, longest = (most + p - 1) / p;
     const double even = (double)total / slots;
-    double t = (alike ? (double)rounds * longest : even > longest ? even : longest) + 3.0 * rounds;
-    if (p > 1) t += 8.0 + 2.0 * p * bytes / unit;
+    double t = us * (alike ? (double)rounds * longest : even > longest ? even : longest) + 3.0 * rounds;
+    if (p > 1) t += 7.0 + p * traffic;
     if (p == 1 || t < least) { best = p; least = t; }
   }
   return best;
@@ -946,13 +948,14 @@ template <typename T, int NB, int KK> dat_status launch(int pass, AttnArgs a, hi
   const int64_t tiles = tiles_of(a, pass), groups = a.off_q ? a.Hkv : (int64_t)a.B * a.Hkv;
   a.groups = (int)groups;
   a.rows_per_group = (int)tiles;
-  a.items = tiles * groups * (pass == kGradKV ? 1 : a.G) * a.parts;
+  const int64_t items = tiles * groups * (pass == kGradKV ? 1 : a.G) * a.parts;
+  a.items = (int)items;
   // a share of the work for each XCD, whose L2 then holds the keys of few heads; under a window the shares are only alike if each has
   // whole groups
   a.xcd = a.groups % 8 == 0 || (a.left >= kFar && a.right >= kFar);
-  if (tiles > INT32_MAX || !fits_launch(a.items + 7, NW * 64)) return DAT_ERR_SHAPE;
-  if (a.items == 0) return DAT_OK;
-  const dim3 grid((unsigned)(a.xcd ? (a.items + 7) / 8 * 8 : a.items)), block(NW * 64);
+  if (tiles > INT32_MAX || !fits_launch(items + 7, NW * 64)) return DAT_ERR_SHAPE;
+  if (items == 0) return DAT_OK;
+  const dim3 grid((unsigned)(a.xcd ? (items + 7) / 8 * 8 : items)), block(NW * 64);
   if (pass == kForward) hipLaunchKernelGGL((attn_fwd_kernel<T, NB, KK, NW, occupancy<T, NB>(kForward)>), grid, block, 0, st, a);
   else if (pass == kGradQ) hipLaunchKernelGGL((attn_dq_kernel<T, NB, KK, NW, occupancy<T, NB>(kGradQ)>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((attn_dkv_kernel<T, NB, KK, NW, occupancy<T, NB>(kGradKV)>), grid, block, 0, st, a);
@@ -961,12 +964,14 @@ template <typename T, int NB, int KK> dat_status launch(int pass, AttnArgs a, hi
 }
 
 // Adds up the parts of a pass.
-template <typename T> dat_status join(const AttnArgs& a, const float* part, const float* ml, const HeadsArg& out, bool keys, hipStream_t st) {
+template <typename T> dat_status join(int pass, const AttnArgs& a, hipStream_t st) {
+  const bool keys = pass == kGradKV;
   const int64_t rows = keys ? a.key_rows : a.rows;
-  JoinArgs j{part, ml, out, a.lse, keys ? a.off_k : a.off_q, a.B, keys ? a.Sk : a.Sq, keys ? a.Hkv : a.H, a.D, a.parts, rows};
+  JoinArgs j{a.part, pass == kForward ? a.part + a.parts * a.rows * a.D : nullptr, pass == kForward ? a.o : keys ? a.dk : a.dq, a.dv, a.lse, keys ? a.off_k : a.off_q, a.B,
+             keys ? a.Sk : a.Sq, keys ? a.Hkv : a.H, a.D, a.parts, rows};
   const int64_t blocks = (rows * (a.D / 8) + 255) / 256;
   if (!fits_launch(blocks, 256)) return DAT_ERR_SHAPE;
-  hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, st, j);
+  hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)blocks, keys ? 2 : 1), dim3(256), 0, st, j);
   DAT_LAUNCH_CHECK();
   return DAT_OK;
 }
@@ -984,12 +989,8 @@ template <typename T> dat_status launch_heads(int pass, const AttnArgs& a, hipSt
   }
 }
 template <typename T> dat_status run_pass(int pass, const AttnArgs& a, hipStream_t st) {
-  dat_status r = launch_heads<T>(pass, a, st);
-  if (r != DAT_OK || a.parts <= 1) return r;
-  if (pass == kForward) return join<T>(a, a.part, a.part + a.parts * a.rows * a.D, a.o, false, st);
-  if (pass == kGradQ) return join<T>(a, a.part, nullptr, a.dq, false, st);
-  r = join<T>(a, a.part, nullptr, a.dk, true, st);
-  return r != DAT_OK ? r : join<T>(a, a.part + a.parts * a.key_rows * a.D, nullptr, a.dv, true, st);
+  const dat_status r = launch_heads<T>(pass, a, st);
+  return r != DAT_OK || a.parts <= 1 ? r : join<T>(pass, a, st);
 }
 dat_status run_pass(int pass, dat_dtype dtype, const AttnArgs& a, hipStream_t st) {
   return dtype == DAT_BF16 ? run_pass<bf16_t>(pass, a, st) : run_pass<float>(pass, a, st);
