@@ -6,7 +6,8 @@
 //
 // Bound by HBM.  A lane holds two vectors of W elements of a head that hold W whole pairs (pairs of neighbours: vectors behind one another;
 // pairs of halves: one vector of each half), so nothing is exchanged but the sums of a head, among the L lanes (a power of two) that
-// share it.  A wave takes one token, or several where a token has few heads, and all its heads: the angles are made once for all of them.
+// share it.  A wave takes one token, or several where a token has few heads, and all its heads: the angles are made once for all of them,
+// each lane making some and the others taking them over.  Queries come first, then keys, so that a step of the wave has one scale.
 // An angle is a product in 64 bits (the exact one up to its last bit, at any position), reduced to quarter turns there; sine and
 // cosine of what is left are Taylor polynomials in fp32 (|x| <= pi/4, degrees 11 and 12: below 1e-9 off).
 #include "kernels.h"
@@ -20,16 +21,18 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kMaxParts = 1024;                  // workgroups of a backward pass: 4 a compute unit
+constexpr int kMaxParts = 512;                   // workgroups of a backward pass: 2 a compute unit
 
-struct Rows { char* data; int64_t batch, token, head; };       // strides in bytes
+struct Rows {                                    // strides in bytes
+  char* data; int64_t batch, token, head;
+};
 
 struct RotArgs {
   Rows q, k, yq, yk, dq, dk;                     // backward: yq and yk are the incoming gradients
   const float* gamma_q; const float* gamma_k;
   const int32_t* positions; const float* frequencies;
   float* parts;                                  // backward: [workgroups][2][D]
-  int T, S, H, heads, D, axes, pairs, units, turned;   // heads of q and k together; vectors a lane; of them with pairs that turn
+  int T, S, H, Hkv, D, axes, pairs, units, turned;     // vectors a lane; of them with pairs that turn
   int c1, c2, c3;                                // first pairs of the axes 1, 2 and 3
   int lanes, head_groups, token_groups;          // L; heads and tokens that a wave takes at once
   float eps, inv_d;
@@ -99,9 +102,9 @@ template <int W, bool HALVES> struct Lane {
   bool there;
   float c[W], s[W];
   __device__ __forceinline__ void init(const RotArgs& a, int lane) {
-    const int u = lane & (a.lanes - 1), g = lane / a.lanes;
-    group = g % a.head_groups;
-    token = g / a.head_groups;
+    const int u = lane & (a.lanes - 1), g = (uint32_t)lane / (uint32_t)a.lanes;
+    group = g & (a.head_groups - 1);
+    token = (uint32_t)g / (uint32_t)a.head_groups;
     there = u < a.units;
     if (HALVES) {                                // behind the turned pairs: what is left, in two halves as well
       const int rest = u - a.turned, half = (a.D - 2 * a.pairs) / 2;
@@ -114,17 +117,33 @@ template <int W, bool HALVES> struct Lane {
 #pragma unroll
     for (int j = 0; j < W; ++j) { c[j] = 1.0f; s[j] = 0.0f; }     // (lanes without elements hold zeros, which have to stay zeros)
   }
-  __device__ __forceinline__ void angles(const RotArgs& a, int lane, int64_t t) {
-    const int u = lane & (a.lanes - 1);
+  // Of the W pairs that SHARE lanes (heads of one token) have in common, this lane makes every SHARE-th; the rest comes from the others.
+  template <int SHARE> __device__ __forceinline__ void make(const RotArgs& a, int lane, int64_t t, bool live) {
+    const int u = lane & (a.lanes - 1), mine = group & (SHARE - 1);
+    float cc[W / SHARE], ss[W / SHARE];
+    const float* frequencies = a.frequencies;
+    asm volatile("" : "+s"(frequencies));        // read again for each token: kept over the backward pass's loop they cost more registers than it has
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      const int p = W * u + j;
-      c[j] = 1.0f; s[j] = 0.0f;
-      if (p < a.pairs) {
+    for (int i = 0; i < W / SHARE; ++i) {
+      const int p = W * u + mine + SHARE * i;
+      cc[i] = 1.0f; ss[i] = 0.0f;
+      if (live && p < a.pairs) {
         const int axis = (p >= a.c1) + (p >= a.c2) + (p >= a.c3);
-        turn(a.positions[t * a.axes + axis], a.frequencies[p], c[j], s[j]);
+        turn(a.positions[t * a.axes + axis], frequencies[p], cc[i], ss[i]);
       }
     }
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      const int from = 4 * (lane + (j % SHARE - mine) * a.lanes);
+      c[j] = SHARE == 1 ? cc[j / SHARE] : __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(cc[j / SHARE])));
+      s[j] = SHARE == 1 ? ss[j / SHARE] : __int_as_float(__builtin_amdgcn_ds_bpermute(from, __float_as_int(ss[j / SHARE])));
+    }
+  }
+  __device__ __forceinline__ void angles(const RotArgs& a, int lane, int64_t t, bool live) {
+    if (a.head_groups >= W) make<W>(a, lane, t, live);
+    else if (a.head_groups >= 4) make<W < 4 ? W : 4>(a, lane, t, live);
+    else if (a.head_groups >= 2) make<2>(a, lane, t, live);
+    else make<1>(a, lane, t, live);
   }
   // pair j of the two vectors
   __device__ __forceinline__ static float& one(float (&x)[2][W], int j) { return HALVES ? x[0][j] : x[(2 * j) / W][(2 * j) % W]; }
@@ -158,73 +177,88 @@ template <int W> __device__ __forceinline__ void rms(const RotArgs& a, const flo
     again = head_sum(again, a.lanes);
     ss = f != 1.0f ? again : ss;
   }
-  rs = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps * f * f));
+  rs = __builtin_amdgcn_rsqf(fmaf(ss, a.inv_d, a.eps * f * f));
 }
 
-__device__ __forceinline__ int64_t token_offset(const Rows& r, int b, int s) { return (int64_t)b * r.batch + (int64_t)s * r.token; }
+// Heads of one token: where they are, and how many.
+struct HeadRow { char* p; int64_t stride; int n; };
+__device__ __forceinline__ HeadRow heads_at(const Rows& r, int b, int s, int n) { return HeadRow{r.data + (int64_t)b * r.batch + (int64_t)s * r.token, r.head, n}; }
+
+// U steps of heads from h0 on: a lane's two vectors of each.
+template <typename T, int W, bool HALVES, int U>
+__device__ __forceinline__ void load_heads(const RotArgs& a, const Lane<W, HALVES>& me, const HeadRow& x, bool live, int h0, typename Vec<T, W>::type (&raw)[U][2]) {
+  typedef typename Vec<T, W>::type V;
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int head = h0 + i * a.head_groups + me.group;
+    __builtin_memset(raw[i], 0, sizeof(raw[i]));
+    if (live && head < x.n) {
+      const T* const p = reinterpret_cast<const T*>(x.p + head * x.stride);
+      raw[i][0] = *reinterpret_cast<const V*>(p + me.first);
+      raw[i][1] = *reinterpret_cast<const V*>(p + me.second);
+    }
+  }
+}
+template <typename T, int W, bool HALVES>
+__device__ __forceinline__ void store_head(const Lane<W, HALVES>& me, const HeadRow& y, int head, const float (&v)[2][W]) {
+  typedef typename Vec<T, W>::type V;
+  T* const p = reinterpret_cast<T*>(y.p + head * y.stride);
+  *reinterpret_cast<V*>(p + me.first) = pack<T, W>(v[0]);
+  *reinterpret_cast<V*>(p + me.second) = pack<T, W>(v[1]);
+}
 
 template <typename T, int W, bool HALVES>
 __global__ __launch_bounds__(kThreads) void rotary_forward_kernel(RotArgs a) {
   typedef typename Vec<T, W>::type V;
-  constexpr int U = 4;                           // heads in flight
+  constexpr int U = 4;                           // steps in flight
   const int lane = threadIdx.x & 63, wave = (int)(threadIdx.x >> 6);
   Lane<W, HALVES> me;
   me.init(a, lane);
   const int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * a.token_groups + me.token;
   const bool live = t < a.T && me.there;
-  const int b = live ? (int)t / a.S : 0, s = live ? (int)t - b * a.S : 0;
-  if (live) me.angles(a, lane, t);
-  float gq[2][W], gk[2][W];
-  if (a.norm) {
-    load_gamma<W>(a.gamma_q, me.there, me.first, me.second, gq);
-    load_gamma<W>(a.gamma_k, me.there, me.first, me.second, gk);
-  }
-  const char* const xq = a.q.data + token_offset(a.q, b, s); const char* const xk = a.k.data + token_offset(a.k, b, s);
-  char* const yq = a.yq.data + token_offset(a.yq, b, s); char* const yk = a.yk.data + token_offset(a.yk, b, s);
-  for (int h0 = 0; h0 < a.heads; h0 += U * a.head_groups) {
-    V raw[U][2];
+  const int b = live && a.S < a.T ? (int)((uint32_t)t / (uint32_t)a.S) : 0, s = live ? (int)t - b * a.S : 0;
+  V raw[U][2];
+  // loaded: the first U steps are there already
+  auto run = [&](const HeadRow& x, const HeadRow& y, const float* gamma, bool loaded) {
+    float g[2][W];
+    if (a.norm) load_gamma<W>(gamma, me.there, me.first, me.second, g);
+    for (int h0 = 0; h0 < x.n; h0 += U * a.head_groups) {
+      if (!loaded || h0 > 0) load_heads<T, W, HALVES, U>(a, me, x, live, h0, raw);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int head = h0 + i * a.head_groups + me.group;
-      __builtin_memset(raw[i], 0, sizeof(raw[i]));
-      if (live && head < a.heads) {
-        const T* const p = reinterpret_cast<const T*>(head < a.H ? xq + head * a.q.head : xk + (head - a.H) * a.k.head);
-        raw[i][0] = *reinterpret_cast<const V*>(p + me.first);
-        raw[i][1] = *reinterpret_cast<const V*>(p + me.second);
+      for (int i = 0; i < U; ++i) {
+        if (h0 + i * a.head_groups >= x.n) break;
+        const int head = h0 + i * a.head_groups + me.group;
+        float v[2][W], w[2][W];
+        unpack<T, W>(raw[i][0], v[0]);
+        unpack<T, W>(raw[i][1], v[1]);
+        if (a.norm) {
+          float f, rs;
+          rms<W>(a, v, f, rs);
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[k][j] = v[k][j] * f * rs * g[k][j];
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          const float p = Lane<W, HALVES>::one(v, j), q = Lane<W, HALVES>::two(v, j);
+          Lane<W, HALVES>::one(w, j) = fmaf(p, me.c[j], -(q * me.s[j]));
+          Lane<W, HALVES>::two(w, j) = fmaf(p, me.s[j], q * me.c[j]);
+        }
+        if (live && head < x.n) store_head<T, W, HALVES>(me, y, head, w);
       }
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int head = h0 + i * a.head_groups + me.group;
-      float x[2][W], y[2][W];
-      unpack<T, W>(raw[i][0], x[0]);
-      unpack<T, W>(raw[i][1], x[1]);
-      if (a.norm) {
-        float f, rs;
-        rms<W>(a, x, f, rs);
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-          for (int j = 0; j < W; ++j) x[v][j] = x[v][j] * f * rs * (head < a.H ? gq[v][j] : gk[v][j]);
-      }
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const float p = Lane<W, HALVES>::one(x, j), q = Lane<W, HALVES>::two(x, j);
-        Lane<W, HALVES>::one(y, j) = fmaf(p, me.c[j], -(q * me.s[j]));
-        Lane<W, HALVES>::two(y, j) = fmaf(p, me.s[j], q * me.c[j]);
-      }
-      if (live && head < a.heads) {
-        T* const p = reinterpret_cast<T*>(head < a.H ? yq + head * a.yq.head : yk + (head - a.H) * a.yk.head);
-        *reinterpret_cast<V*>(p + me.first) = pack<T, W>(y[0]);
-        *reinterpret_cast<V*>(p + me.second) = pack<T, W>(y[1]);
-      }
-    }
-  }
+  };
+  const HeadRow q = heads_at(a.q, b, s, a.H);
+  load_heads<T, W, HALVES, U>(a, me, q, live, 0, raw);           // on their way while the angles are made
+  me.angles(a, lane, t, live);
+  run(q, heads_at(a.yq, b, s, a.H), a.gamma_q, true);
+  run(heads_at(a.k, b, s, a.Hkv), heads_at(a.yk, b, s, a.Hkv), a.gamma_k, false);
 }
 
 // Waves go on to further tokens, so that few partial sums of dgamma are left: one for each workgroup, added up by a launch of its own.
 template <typename T, int W, bool HALVES>
-__global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void rotary_backward_kernel(RotArgs a) {
   typedef typename Vec<T, W>::type V;
   constexpr int U = 2;
   __shared__ float sums[2 * W][kThreads];
@@ -240,38 +274,20 @@ __global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotArgs a) {
   for (int v = 0; v < 2; ++v)
 #pragma unroll
     for (int j = 0; j < W; ++j) dgq[v][j] = dgk[v][j] = 0.0f;
-  const int64_t step = (int64_t)gridDim.x * kWaves * a.token_groups;
-  for (int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * a.token_groups; t0 < a.T; t0 += step) {
-    const int64_t t = t0 + me.token;
-    const bool live = t < a.T && me.there;
-    const int b = live ? (int)t / a.S : 0, s = live ? (int)t - b * a.S : 0;
-    if (live) me.angles(a, lane, t);
-    for (int h0 = 0; h0 < a.heads; h0 += U * a.head_groups) {
-      V raw[U][2], grad[U][2];
+  V raw[U][2], grad[U][2];
+  auto load = [&](const HeadRow& x, const HeadRow& dy, bool live, int h0) {
+    load_heads<T, W, HALVES, U>(a, me, dy, live, h0, grad);
+    if (a.norm) load_heads<T, W, HALVES, U>(a, me, x, live, h0, raw);
+  };
+  auto run = [&](const HeadRow& x, const HeadRow& dy, const HeadRow& dx, const float (&gamma)[2][W], float (&dgamma)[2][W], bool live, bool loaded) {
+    for (int h0 = 0; h0 < dy.n; h0 += U * a.head_groups) {
+      if (!loaded || h0 > 0) load(x, dy, live, h0);
 #pragma unroll
       for (int i = 0; i < U; ++i) {
+        if (h0 + i * a.head_groups >= dy.n) break;
         const int head = h0 + i * a.head_groups + me.group;
-        __builtin_memset(raw[i], 0, sizeof(raw[i]));
-        __builtin_memset(grad[i], 0, sizeof(grad[i]));
-        if (live && head < a.heads) {
-          const bool is_q = head < a.H;
-          const T* const g = reinterpret_cast<const T*>(is_q ? a.yq.data + token_offset(a.yq, b, s) + head * a.yq.head
-                                                             : a.yk.data + token_offset(a.yk, b, s) + (head - a.H) * a.yk.head);
-          grad[i][0] = *reinterpret_cast<const V*>(g + me.first);
-          grad[i][1] = *reinterpret_cast<const V*>(g + me.second);
-          if (a.norm) {
-            const T* const p = reinterpret_cast<const T*>(is_q ? a.q.data + token_offset(a.q, b, s) + head * a.q.head
-                                                               : a.k.data + token_offset(a.k, b, s) + (head - a.H) * a.k.head);
-            raw[i][0] = *reinterpret_cast<const V*>(p + me.first);
-            raw[i][1] = *reinterpret_cast<const V*>(p + me.second);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int head = h0 + i * a.head_groups + me.group;
-        const bool is_q = head < a.H;
-        float x[2][W], y[2][W], dn[2][W];
+        const bool counts = live && head < dy.n;
+        float v[2][W], y[2][W], dn[2][W];
         unpack<T, W>(grad[i][0], y[0]);
         unpack<T, W>(grad[i][1], y[1]);
 #pragma unroll
@@ -281,36 +297,40 @@ __global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotArgs a) {
           Lane<W, HALVES>::two(dn, j) = fmaf(q, me.c[j], -(p * me.s[j]));
         }
         if (a.norm) {
-          unpack<T, W>(raw[i][0], x[0]);
-          unpack<T, W>(raw[i][1], x[1]);
+          unpack<T, W>(raw[i][0], v[0]);
+          unpack<T, W>(raw[i][1], v[1]);
           float f, rs, dot = 0.0f;
-          rms<W>(a, x, f, rs);
-          const bool counts = live && head < a.heads;             // (a head that is not there may have an infinite 1 / sqrt(eps))
+          rms<W>(a, v, f, rs);
+          if (!counts) rs = 0.0f;                // (a head that is not there may have an infinite 1 / sqrt(eps))
 #pragma unroll
-          for (int v = 0; v < 2; ++v)
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int j = 0; j < W; ++j) {
-              const float xhat = x[v][j] * f * rs, d = counts ? dn[v][j] * xhat : 0.0f;
-              x[v][j] = xhat;
-              dgq[v][j] += is_q ? d : 0.0f;
-              dgk[v][j] += is_q ? 0.0f : d;
-              dn[v][j] *= is_q ? gq[v][j] : gk[v][j];
-              dot = fmaf(dn[v][j], xhat, dot);
+              v[k][j] = v[k][j] * f * rs;        // xhat
+              dgamma[k][j] = fmaf(dn[k][j], v[k][j], dgamma[k][j]);
+              dn[k][j] *= gamma[k][j];
+              dot = fmaf(dn[k][j], v[k][j], dot);
             }
           dot = head_sum(dot, a.lanes) * a.inv_d;
 #pragma unroll
-          for (int v = 0; v < 2; ++v)
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int j = 0; j < W; ++j) dn[v][j] = fmaf(-x[v][j], dot, dn[v][j]) * rs * f;
+            for (int j = 0; j < W; ++j) dn[k][j] = fmaf(-v[k][j], dot, dn[k][j]) * rs * f;
         }
-        if (live && head < a.heads) {
-          T* const p = reinterpret_cast<T*>(is_q ? a.dq.data + token_offset(a.dq, b, s) + head * a.dq.head
-                                                 : a.dk.data + token_offset(a.dk, b, s) + (head - a.H) * a.dk.head);
-          *reinterpret_cast<V*>(p + me.first) = pack<T, W>(dn[0]);
-          *reinterpret_cast<V*>(p + me.second) = pack<T, W>(dn[1]);
-        }
+        if (counts) store_head<T, W, HALVES>(me, dx, head, dn);
       }
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * kWaves * a.token_groups;
+  for (int64_t t0 = ((int64_t)blockIdx.x * kWaves + wave) * a.token_groups; t0 < a.T; t0 += step) {
+    const int64_t t = t0 + me.token;
+    const bool live = t < a.T && me.there;
+    const int b = live && a.S < a.T ? (int)((uint32_t)t / (uint32_t)a.S) : 0, s = live ? (int)t - b * a.S : 0;
+    const HeadRow q = heads_at(a.q, b, s, a.H), dyq = heads_at(a.yq, b, s, a.H);
+    load(q, dyq, live, 0);
+    me.angles(a, lane, t, live);
+    run(q, dyq, heads_at(a.dq, b, s, a.H), gq, dgq, live, true);
+    run(heads_at(a.k, b, s, a.Hkv), heads_at(a.yk, b, s, a.Hkv), heads_at(a.dk, b, s, a.Hkv), gk, dgk, live, false);
   }
   if (!a.norm) return;
   // element e of a head: the lanes that hold it, of all waves, one after the other
@@ -341,18 +361,22 @@ __global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotArgs a) {
   }
 }
 
-// dgamma[e] = sum over the workgroups' parts in a fixed order: 16 elements a workgroup, 16 threads an element.
-__global__ __launch_bounds__(kThreads) void rotary_dgamma_kernel(const float* __restrict__ parts, int n, int D, float* __restrict__ dgq, float* __restrict__ dgk) {
-  __shared__ float part[16][17];
+// dgamma[e] = sum over the workgroups' parts in a fixed order: 16 elements a workgroup, 64 threads an element (16 ones: 18 us for 1024 parts of
+// 128; the parts come one after the other).
+__global__ __launch_bounds__(1024) void rotary_dgamma_kernel(const float* __restrict__ parts, int n, int D, float* __restrict__ dgq, float* __restrict__ dgk) {
+  __shared__ float part[64][17];
   const int e = threadIdx.x & 15, row = threadIdx.x >> 4, col = blockIdx.x * 16 + e;
   float total = 0.0f;
-  if (col < 2 * D) for (int i = row; i < n; i += 16) total += parts[(int64_t)i * 2 * D + col];
+  if (col < 2 * D) {
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 64; ++i) total += row + 64 * i < n ? parts[(int64_t)(row + 64 * i) * 2 * D + col] : 0.0f;
+  }
   part[row][e] = total;
   __syncthreads();
   if (threadIdx.x < 16 && col < 2 * D) {
     total = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) total += part[r][e];
+    for (int r = 0; r < 64; ++r) total += part[r][e];
     float* const out = col < D ? dgq : dgk;
     if (out) out[col < D ? col : col - D] = total;
   }
@@ -378,7 +402,7 @@ bool fill(const dat_rotary* s, RotArgs& a, dat_status& status) {
   status = DAT_ERR_SHAPE;
   if (s->D % 8 || s->D > 256 || (s->layout == DAT_ROTARY_HALVES && pairs % 2)) return false;
   if ((int64_t)s->B * s->S > 1 << 30 || s->H + (int64_t)s->Hkv > 1 << 20) return false;
-  a.T = s->B * s->S; a.S = s->S; a.H = s->H; a.heads = s->H + s->Hkv; a.D = s->D; a.axes = s->axes; a.pairs = (int)pairs;
+  a.T = s->B * s->S; a.S = s->S; a.H = s->H; a.Hkv = s->Hkv; a.D = s->D; a.axes = s->axes; a.pairs = (int)pairs;
   a.c1 = s->axes > 1 ? s->sections[0] : INT32_MAX;
   a.c2 = s->axes > 2 ? a.c1 + s->sections[1] : INT32_MAX;
   a.c3 = s->axes > 3 ? a.c2 + s->sections[2] : INT32_MAX;
@@ -401,8 +425,11 @@ void arrange(const dat_rotary& s, RotArgs& a) {
   const int w = vector_of(s, a.pairs);
   a.units = a.D / (2 * w); a.turned = a.pairs / w;
   a.lanes = power_of_two(a.units);
-  const int groups = 64 / a.lanes, heads = power_of_two(a.heads);
-  a.head_groups = heads < groups ? heads : groups;
+  // heads of a token that a wave takes at once: as many as leave at most an eighth of the steps' places empty
+  const int groups = 64 / a.lanes;
+  auto places = [&](int n) { return ((int64_t)a.H + n - 1) / n * n + ((int64_t)a.Hkv + n - 1) / n * n; };
+  a.head_groups = groups;
+  while (a.head_groups > 1 && 8 * places(a.head_groups) > 9 * ((int64_t)a.H + a.Hkv)) a.head_groups /= 2;
   a.token_groups = groups / a.head_groups;
 }
 
@@ -521,7 +548,7 @@ extern "C" dat_status dat_norm_rotary_backward(const dat_rotary* shape, const da
     parts = blocks_of(a) < kMaxParts ? blocks_of(a) : kMaxParts;
   }
   if (sums) {
-    hipLaunchKernelGGL(rotary_dgamma_kernel, dim3((2 * a.D + 15) / 16), dim3(kThreads), 0, (hipStream_t)stream, a.parts, parts, a.D, dgamma_q, dgamma_k);
+    hipLaunchKernelGGL(rotary_dgamma_kernel, dim3((2 * a.D + 15) / 16), dim3(1024), 0, (hipStream_t)stream, a.parts, parts, a.D, dgamma_q, dgamma_k);
     DAT_LAUNCH_CHECK();
   }
   return DAT_OK;
