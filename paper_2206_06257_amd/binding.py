@@ -658,12 +658,6 @@ def group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, act=ACT_NONE, dx
     return dx, dgamma, dbeta
 
 
-def _heads(t):
-    """Strides of [B, S, H, D] or [T, H, D]; a dimension of one has any."""
-    st = t.stride()
-    return _Heads(t.data_ptr(), st[0] if t.dim() == 4 else 0, st[-3], st[-2])
-
-
 def _want_heads(name, t, dtype, shape, optional=False):
     """Checks a tensor of heads: any strides but one between the elements of a head."""
     if t is None and optional:
@@ -673,29 +667,48 @@ def _want_heads(name, t, dtype, shape, optional=False):
         raise ValueError("%s: the elements of a head have to lie beside one another, strides are %s" % (name, tuple(t.stride())))
 
 
-def _attention(q, k, v, scale, window, offsets_q, offsets_k):
-    """The checks that both directions share -> (shape, batched)."""
-    _want("q", q, _FLOATS, contiguous=False)
+def _heads(name, t, dtype, shape, optional=False):
+    """Address and strides of [B, S, H, D] or [T, H, D] (a dimension of one has any), checked; None for an optional tensor that is not there."""
+    if t is None:
+        if not optional:
+            raise ValueError("%s: needed here" % name)
+        return None
+    st = t.stride()
+    if t.dtype != dtype or t.shape != shape or st[-1] != 1:
+        _want_heads(name, t, dtype, shape)
+    return _Heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+
+
+# (a call's sizes without offsets, and what the library says it needs: built once for each set of them)
+@functools.lru_cache(maxsize=1024)
+def _attention_shape(*sizes):
+    shape = _Attention(*sizes)
+    return shape, (int(_lib.dat_attention_workspace(0, shape)), int(_lib.dat_attention_workspace(1, shape)))
+
+
+def _attention(q, k, scale, window, offsets_q, offsets_k):
+    """The checks of sizes that both directions share -> (shape, workspaces, batched)."""
+    if q.dtype not in _FLOATS:
+        _want("q", q, _FLOATS, contiguous=False)
     batched = offsets_q is None
     if batched != (offsets_k is None):
         raise ValueError("offsets_q and offsets_k: both or neither")
-    if q.dim() != (4 if batched else 3):
-        raise ValueError("q: expected %s, got %s" % ("[B, S, H, D]" if batched else "[T, H, D]", tuple(q.shape)))
-    if k.dim() != q.dim() or k.shape[-1] != q.shape[-1] or (batched and k.shape[0] != q.shape[0]):
-        raise ValueError("k: %s does not go with q %s" % (tuple(k.shape), tuple(q.shape)))
-    _want_heads("q", q, q.dtype, q.shape)
-    _want_heads("k", k, q.dtype, k.shape)
-    _want_heads("v", v, q.dtype, k.shape)
-    if not batched:
-        _want("offsets_q", offsets_q, (torch.int32,), contiguous=True)
-        _want("offsets_k", offsets_k, (torch.int32,), offsets_q.shape)
-        if offsets_q.dim() != 1 or offsets_q.numel() < 1:
-            raise ValueError("offsets_q: expected [B + 1], got %s" % (tuple(offsets_q.shape),))
+    qs, ks = q.shape, k.shape
+    if len(qs) != (4 if batched else 3):
+        raise ValueError("q: expected %s, got %s" % ("[B, S, H, D]" if batched else "[T, H, D]", tuple(qs)))
+    if len(ks) != len(qs) or ks[-1] != qs[-1] or (batched and ks[0] != qs[0]):
+        raise ValueError("k: %s does not go with q %s" % (tuple(ks), tuple(qs)))
     left, right = window
-    D = q.shape[-1]
-    B = q.shape[0] if batched else offsets_q.numel() - 1
-    return _Attention(_code(q), B, q.shape[-3], k.shape[-3], q.shape[-2], k.shape[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale, left, right,
-                      _at(offsets_q), _at(offsets_k)), batched
+    D = qs[-1]
+    sizes = (_code(q), qs[0] if batched else offsets_q.numel() - 1, qs[-3], ks[-3], qs[-2], ks[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale, left, right)
+    if batched:
+        return _attention_shape(*sizes) + (True,)
+    _want("offsets_q", offsets_q, (torch.int32,), contiguous=True)
+    _want("offsets_k", offsets_k, (torch.int32,), offsets_q.shape)
+    if offsets_q.dim() != 1 or offsets_q.numel() < 1:
+        raise ValueError("offsets_q: expected [B + 1], got %s" % (tuple(offsets_q.shape),))
+    shape = _Attention(*sizes, _at(offsets_q), _at(offsets_k))
+    return shape, (int(_lib.dat_attention_workspace(0, shape)), int(_lib.dat_attention_workspace(1, shape))), False
 
 
 def _lse_shape(q, batched):
@@ -706,30 +719,33 @@ def attention_forward(q, k, v, scale=None, window=(-1, -1), offsets_q=None, offs
     """q [B, Sq, H, D], k and v [B, Sk, Hkv, D], or packed sequences [T, H, D] with int32 offsets [B + 1]; fp32 or bf16, any strides
     between tokens and heads -> (o like q, lse fp32 [B, H, Sq] or [H, T]).  window = (left, right): keys that a query sees beside its own
     place, -1 for all of them, (-1, 0) is causal; scale: 1 / sqrt(D) for None.  See dat_attention_forward."""
-    shape, batched = _attention(q, k, v, scale, window, offsets_q, offsets_k)
-    _want_heads("o", o, q.dtype, q.shape, optional=True)
+    shape, need, batched = _attention(q, k, scale, window, offsets_q, offsets_k)
+    dtype, qs, ks = q.dtype, q.shape, k.shape
+    hq, hk, hv, ho = _heads("q", q, dtype, qs), _heads("k", k, dtype, ks), _heads("v", v, dtype, ks), _heads("o", o, dtype, qs, optional=True)
     with _On(stream, q, k, v, o, offsets_q, offsets_k) as st:
         if o is None:
-            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(_lse_shape(q, batched), device=q.device)
-        size = int(_lib.dat_attention_workspace(0, shape))
-        ws = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
-        _check(_lib.dat_attention_forward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), _at(ws), size, st), "dat_attention_forward")
+            o = q.new_empty(qs)
+            ho = _heads("o", o, dtype, qs)
+        lse = q.new_empty(_lse_shape(q, batched), dtype=torch.float32)
+        ws = torch.empty(need[0], dtype=torch.uint8, device=q.device) if need[0] else None
+        _check(_lib.dat_attention_forward(shape, hq, hk, hv, ho, lse.data_ptr(), _at(ws), need[0], st), "dat_attention_forward")
     return o, lse
 
 
 def attention_backward(q, k, v, o, lse, do, scale=None, window=(-1, -1), offsets_q=None, offsets_k=None, dq=None, dk=None, dv=None, stream=None):
     """Gradients of attention_forward's o from its o and lse and the incoming gradient do -> (dq, dk, dv)."""
-    shape, batched = _attention(q, k, v, scale, window, offsets_q, offsets_k)
-    for name, t, like in (("o", o, q), ("do", do, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
-        _want_heads(name, t, q.dtype, like.shape, optional=name in ("dq", "dk", "dv"))
+    shape, need, batched = _attention(q, k, scale, window, offsets_q, offsets_k)
+    dtype, qs, ks = q.dtype, q.shape, k.shape
+    given = [_heads(name, t, dtype, like) for name, t, like in (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs))]
+    hdo = _heads("do", do, dtype, qs)
     _want("lse", lse, (torch.float32,), torch.Size(_lse_shape(q, batched)))
+    for name, t, like in (("dq", dq, qs), ("dk", dk, ks), ("dv", dv, ks)):
+        _heads(name, t, dtype, like, optional=True)
     with _On(stream, q, k, v, o, lse, do, dq, dk, dv, offsets_q, offsets_k) as st:
-        dq, dk, dv = (torch.empty(like.shape, dtype=q.dtype, device=q.device) if t is None else t for t, like in ((dq, q), (dk, k), (dv, k)))
-        size = int(_lib.dat_attention_workspace(1, shape))
-        ws = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
-        _check(_lib.dat_attention_backward(shape, _heads(q), _heads(k), _heads(v), _heads(o), _at(lse), _heads(do), _heads(dq), _heads(dk), _heads(dv),
-                                           _at(ws), size, st), "dat_attention_backward")
+        dq, dk, dv = (q.new_empty(like) if t is None else t for t, like in ((dq, qs), (dk, ks), (dv, ks)))
+        ws = torch.empty(need[1], dtype=torch.uint8, device=q.device) if need[1] else None
+        _check(_lib.dat_attention_backward(shape, *given, lse.data_ptr(), hdo, _heads("dq", dq, dtype, qs), _heads("dk", dk, dtype, ks), _heads("dv", dv, dtype, ks),
+                                           _at(ws), need[1], st), "dat_attention_backward")
     return dq, dk, dv
 
 
@@ -738,50 +754,51 @@ def rotary_frequencies(sections, base=10000.0, device="cuda"):
     return torch.cat([base ** (-torch.arange(n, dtype=torch.float64) / n) for n in sections]).float().to(device) if sections else torch.empty(0, device=device)
 
 
-def _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm, like=None):
-    """The checks that both directions share -> shape.  q, or (where it is not given) the gradient `like`, has the sizes."""
-    first, second = (q, k) if like is None else like
+@functools.lru_cache(maxsize=1024)
+def _rotary_shape(dtype, B, S, H, Hkv, D, sections, layout, norm, eps):
+    shape = _Rotary(dtype, B, S, H, Hkv, D, len(sections), (C.c_int32 * 4)(*sections), layout, norm, eps)
+    return shape, int(_lib.dat_norm_rotary_workspace(1, shape))
+
+
+def _rotary(first, second, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm):
+    """The checks of sizes that both directions share, by the tensors that have to be there (queries', keys') -> (shape, workspace, one of them)."""
     one = second if first is None else first
     if one is None:
         raise ValueError("q or k: one of them is needed")
-    _want("q" if first is not None else "k", one, _FLOATS, contiguous=False)
-    if one.dim() not in (3, 4):
-        raise ValueError("q: expected [B, S, H, D] or [T, H, D], got %s" % (tuple(one.shape),))
-    D, lead = one.shape[-1], tuple(one.shape[:-2])
-    if second is not None and (second.dim() != one.dim() or tuple(second.shape[:-2]) != lead or second.shape[-1] != D):
-        raise ValueError("k: %s does not go with q %s" % (tuple(second.shape), tuple(one.shape)))
-    for name, t in (("q", first), ("k", second)):
-        _want_heads(name, t, one.dtype, None, optional=True)
+    if one.dtype not in _FLOATS:
+        _want("q" if first is not None else "k", one, _FLOATS, contiguous=False)
+    size = one.shape
+    if len(size) not in (3, 4):
+        raise ValueError("q: expected [B, S, H, D] or [T, H, D], got %s" % (tuple(size),))
+    D, lead = size[-1], tuple(size[:-2])
+    if second is not None and second is not one and (len(second.shape) != len(size) or tuple(second.shape[:-2]) != lead or second.shape[-1] != D):
+        raise ValueError("k: %s does not go with q %s" % (tuple(second.shape), tuple(size)))
     for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
         _want(name, t, (torch.float32,), (D,), optional=True)
-    sections = list(sections)
+    sections = tuple(sections)
     if len(sections) > 4:
         raise ValueError("sections: at most 4 axes, got %r" % (sections,))
     pairs = sum(sections)
     _want("positions", positions, (torch.int32,), lead + (len(sections),), optional=pairs == 0)
     _want("frequencies", frequencies, (torch.float32,), (pairs,), optional=pairs == 0)
     B, S = lead if len(lead) == 2 else (1, lead[0])
-    return _Rotary(_code(one), B, S, 0 if first is None else first.shape[-2], 0 if second is None else second.shape[-2], D, len(sections),
-                   (C.c_int32 * 4)(*sections), layout, int(bool(norm)), eps)
-
-
-def _heads_or_none(t):
-    return None if t is None else _heads(t)
+    return _rotary_shape(_code(one), B, S, 0 if first is None else first.shape[-2], 0 if second is None else second.shape[-2], D, sections, layout, int(bool(norm)), eps) + (one,)
 
 
 def norm_rotary_forward(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout=ROTARY_HALVES, eps=1e-6, norm=True, yq=None, yk=None, stream=None):
     """Norm of every head of q [B, S, H, D] and k [B, S, Hkv, D] (or [T, H, D]; fp32 or bf16, any strides between tokens and heads; either may be
     None), its scale (fp32 [D] or None) and the rotation by positions int32 [.., axes]: sections[a] pairs go by axis a, with one
     frequency (fp32, radians a step) each -> (yq, yk).  yq may be q, yk may be k.  See dat_norm_rotary_forward."""
-    shape = _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm)
-    first = k if q is None else q
+    shape, _, first = _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm)
+    dtype = first.dtype
+    given = [None if t is None else _heads(name, t, dtype, t.shape) for name, t in (("q", q), ("k", k))]
     for name, t, like in (("yq", yq, q), ("yk", yk, k)):
         if like is not None:
-            _want_heads(name, t, first.dtype, like.shape, optional=True)
+            _heads(name, t, dtype, like.shape, optional=True)
     with _On(stream, first, k, gamma_q, gamma_k, positions, frequencies, yq, yk) as st:
-        yq, yk = (None if like is None else torch.empty(like.shape, dtype=like.dtype, device=like.device) if t is None else t for t, like in ((yq, q), (yk, k)))
-        _check(_lib.dat_norm_rotary_forward(shape, _heads_or_none(q), _heads_or_none(k), _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies),
-                                            _heads_or_none(yq), _heads_or_none(yk), st), "dat_norm_rotary_forward")
+        yq, yk = (None if like is None else like.new_empty(like.shape) if t is None else t for t, like in ((yq, q), (yk, k)))
+        out = [None if t is None else _heads("y", t, dtype, t.shape) for t in (yq, yk)]
+        _check(_lib.dat_norm_rotary_forward(shape, *given, _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies), *out, st), "dat_norm_rotary_forward")
     return yq, yk
 
 
@@ -789,23 +806,22 @@ def norm_rotary_backward(q, k, gamma_q, gamma_k, positions, frequencies, section
                          dgamma_q=None, dgamma_k=None, stream=None):
     """Gradients of norm_rotary_forward for the incoming gradients dyq and dyk -> (dq, dk, dgamma_q, dgamma_k); the last two are None where there is
     no such scale.  dq may be q or dyq, dk may be k or dyk.  Without the norm q and k are not needed."""
-    shape = _rotary(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm, like=(dyq, dyk))
-    first = dyk if dyq is None else dyq
-    for name, t, like, needed in (("q", q, dyq, norm), ("k", k, dyk, norm), ("dq", dq, dyq, False), ("dk", dk, dyk, False)):
+    shape, size, first = _rotary(dyq, dyk, gamma_q, gamma_k, positions, frequencies, sections, layout, eps, norm)
+    dtype, D = first.dtype, first.shape[-1]
+    given = [None if t is None else _heads(name, t, dtype, t.shape) for name, t in (("dyq", dyq), ("dyk", dyk))]
+    x = [None if like is None else _heads(name, t, dtype, like.shape, optional=not norm) for name, t, like in (("q", q, dyq), ("k", k, dyk))]
+    for name, t, like in (("dq", dq, dyq), ("dk", dk, dyk)):
         if like is not None:
-            _want_heads(name, t, first.dtype, like.shape, optional=not needed)
-    D = first.shape[-1]
+            _heads(name, t, dtype, like.shape, optional=True)
     for name, t in (("dgamma_q", dgamma_q), ("dgamma_k", dgamma_k)):
         _want(name, t, (torch.float32,), (D,), optional=True)
     with _On(stream, first, dyk, q, k, gamma_q, gamma_k, positions, frequencies, dq, dk, dgamma_q, dgamma_k) as st:
-        device = first.device
-        dq, dk = (None if like is None else torch.empty(like.shape, dtype=like.dtype, device=device) if t is None else t for t, like in ((dq, dyq), (dk, dyk)))
-        dgamma_q, dgamma_k = (torch.empty(D, device=device) if t is None and norm and gamma is not None and like is not None else t
+        dq, dk = (None if like is None else like.new_empty(like.shape) if t is None else t for t, like in ((dq, dyq), (dk, dyk)))
+        dgamma_q, dgamma_k = (torch.empty(D, device=first.device) if t is None and norm and gamma is not None and like is not None else t
                               for t, gamma, like in ((dgamma_q, gamma_q, dyq), (dgamma_k, gamma_k, dyk)))
-        size = int(_lib.dat_norm_rotary_workspace(1, shape))
-        ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-        _check(_lib.dat_norm_rotary_backward(shape, _heads_or_none(q), _heads_or_none(k), _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies),
-                                             _heads_or_none(dyq), _heads_or_none(dyk), _heads_or_none(dq), _heads_or_none(dk), _at(dgamma_q), _at(dgamma_k),
+        out = [None if t is None else _heads("dx", t, dtype, t.shape) for t in (dq, dk)]
+        ws = torch.empty(size, dtype=torch.uint8, device=first.device) if size else None
+        _check(_lib.dat_norm_rotary_backward(shape, *x, _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies), *given, *out, _at(dgamma_q), _at(dgamma_k),
                                              _at(ws), size, st), "dat_norm_rotary_backward")
     return dq, dk, dgamma_q, dgamma_k
 
