@@ -193,11 +193,12 @@ template <int ROWB, int NW> struct TileLoad {
   }
   __device__ __forceinline__ void load(const char* base, int rows, uint32_t tile, int wave, int lane) const {
     const u32x4 r = descriptor(base);
+    if (rows >= kTile) {                       // (a branch of its own: no comparisons for whole tiles)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      uint32_t at = off[i];
-      if (rows < kTile) at = row(i, wave, lane) < rows ? at : kOob;
-      load_to_lds<16>(r, at, tile + (i * NW + wave) * 1024);
+      for (int i = 0; i < N; ++i) load_to_lds<16>(r, off[i], tile + (i * NW + wave) * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) load_to_lds<16>(r, row(i, wave, lane) < rows ? off[i] : kOob, tile + (i * NW + wave) * 1024);
     }
   }
 };
@@ -889,13 +890,10 @@ template <typename T> __global__ __launch_bounds__(256) void attn_join_kernel(Jo
 enum { kForward, kGradQ, kGradKV };
 constexpr int kWavesOf = 4, kRows = 32 * kWavesOf, kUnits = 256, kMostParts = 32;
 
-// Workgroups of a pass that a compute unit holds: two where 256 registers a lane are enough.
-template <typename T, int NB> constexpr int occupancy(int pass) {
-  return pass == kGradKV ? (sizeof(T) == 2 && NB <= 2 ? 2 : 1) : sizeof(T) == 2 && NB <= 2 ? 3 : (sizeof(T) == 2 || NB <= 2 ? 2 : 1);
-}
-int occupancy_of(const dat_attention& s, int pass) {
-  const int nb = (s.D + 31) / 32;
-  return pass == kGradKV ? (s.dtype == DAT_BF16 && nb <= 2 ? 2 : 1) : (s.dtype == DAT_BF16 || nb <= 2 ? 2 : 1);
+// Workgroups of a pass that a compute unit holds at least (one wave of each on every SIMD): what their registers leave room for without spilling
+// in the loops.  Three where 168 a lane are enough (bf16 heads of up to 64, forward and dq), two with 256, one with 512.
+constexpr int occupancy(bool half_width, int nb, int pass) {
+  return pass == kGradKV ? (half_width && nb <= 2 ? 2 : 1) : half_width && nb <= 2 ? 3 : half_width || nb <= 2 ? 2 : 1;
 }
 
 int64_t tiles_of(const AttnArgs& a, int pass) {
@@ -909,7 +907,7 @@ int64_t tiles_of(const AttnArgs& a, int pass) {
 // 128 on 4 key heads, causal: dk and dv 861 us in one part (376 unlike tiles on 256 units), 698 + 22 us in two.
 int parts_of(const dat_attention& s, const AttnArgs& a, int pass) {
   const int64_t tiles = tiles_of(a, pass), groups = a.off_q ? a.Hkv : (int64_t)a.B * a.Hkv;
-  const int64_t items = tiles * groups * (pass == kGradKV ? 1 : a.G), slots = (int64_t)kUnits * occupancy_of(s, pass);
+  const int64_t items = tiles * groups * (pass == kGradKV ? 1 : a.G), slots = (int64_t)kUnits * occupancy(s.dtype == DAT_BF16, (s.D + 31) / 32, pass);
   if (items == 0 || items > 8 * slots || tiles > 65536) return 1;
   const int seqs = a.off_q ? (a.B > 0 ? a.B : 1) : 1;
   const int64_t Lq = (a.Sq + seqs - 1) / seqs, Lk = (a.Sk + seqs - 1) / seqs;     // (packed: as if all were alike)
@@ -956,9 +954,9 @@ template <typename T, int NB, int KK> dat_status launch(int pass, AttnArgs a, hi
   if (tiles > INT32_MAX || !fits_launch(items + 7, NW * 64)) return DAT_ERR_SHAPE;
   if (items == 0) return DAT_OK;
   const dim3 grid((unsigned)(a.xcd ? (items + 7) / 8 * 8 : items)), block(NW * 64);
-  if (pass == kForward) hipLaunchKernelGGL((attn_fwd_kernel<T, NB, KK, NW, occupancy<T, NB>(kForward)>), grid, block, 0, st, a);
-  else if (pass == kGradQ) hipLaunchKernelGGL((attn_dq_kernel<T, NB, KK, NW, occupancy<T, NB>(kGradQ)>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((attn_dkv_kernel<T, NB, KK, NW, occupancy<T, NB>(kGradKV)>), grid, block, 0, st, a);
+  if (pass == kForward) hipLaunchKernelGGL((attn_fwd_kernel<T, NB, KK, NW, occupancy(sizeof(T) == 2, NB, kForward)>), grid, block, 0, st, a);
+  else if (pass == kGradQ) hipLaunchKernelGGL((attn_dq_kernel<T, NB, KK, NW, occupancy(sizeof(T) == 2, NB, kGradQ)>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((attn_dkv_kernel<T, NB, KK, NW, occupancy(sizeof(T) == 2, NB, kGradKV)>), grid, block, 0, st, a);
   DAT_LAUNCH_CHECK();
   return DAT_OK;
 }
@@ -1006,6 +1004,7 @@ bool fill(const dat_attention* s, AttnArgs& a, dat_status& status) {
   if (s->D % 8 || s->D > 128 || s->Sq >= kFar || s->Sk >= kFar) return false;
   const int64_t batches = s->offsets_q ? 1 : s->B;
   if (batches * s->H * (int64_t)s->Sq >= (int64_t)1 << 40 || batches * s->Hkv * (int64_t)s->Sk >= (int64_t)1 << 40 || (int64_t)s->B * s->Hkv > INT32_MAX) return false;
+  if (((int64_t)s->Sq / kTile + 1) * (s->H / s->Hkv) > INT32_MAX) return false;       // tiles of a key head's queries are counted in 32 bits
   a.off_q = s->offsets_q; a.off_k = s->offsets_k;
   a.B = s->B; a.Sq = s->Sq; a.Sk = s->Sk; a.H = s->H; a.Hkv = s->Hkv; a.G = s->H / s->Hkv; a.D = s->D;
   a.left = s->left < 0 ? kFar : s->left < kFar ? s->left : kFar;

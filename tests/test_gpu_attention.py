@@ -10,6 +10,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2206_06257_amd import binding
 from tests import plain_transformer as pt
 
 pytestmark = pytest.mark.gpu
@@ -109,6 +110,53 @@ def test_attention(dat, shape, dtype, window):
     check(dat, *batch(10, *shape, dtype), window=window)
 
 
+def shared(q, k, window, offsets_q=None, offsets_k=None):
+    """Whether workgroups share walks: forward, and in one of the backward passes (the workspace is for their parts, behind 8 bytes a row there)."""
+    forward, backward = binding._attention(q, k, None, window, offsets_q, offsets_k)[1]
+    return forward > 0, backward > (8 * (q.numel() // q.shape[-1]) + 15) // 16 * 16
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", range(8, 129, 8))
+def test_heads_of_every_size(dat, D, dtype):
+    check(dat, *batch(15, 1, 70, 150, 2, 1, D, dtype), window=(90, 20))
+
+
+# few queries over many keys (a walk over keys shared by up to 32 workgroups), few keys under many queries, few tiles of both
+SHARED = [(1, 1, 9000, 2, 1, 64), (1, 5, 4100, 4, 2, 72), (2, 5, 3001, 2, 1, 8), (1, 130, 1500, 2, 1, 40), (1, 1500, 130, 4, 1, 128), (1, 700, 700, 2, 1, 96)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [(-1, -1), (-1, 0), (1000, 3)])
+@pytest.mark.parametrize("shape", SHARED)
+def test_walks_shared_by_workgroups(dat, shape, window, dtype):
+    q, k, v, do = batch(16, *shape, dtype)
+    assert any(shared(q, k, window))
+    check(dat, q, k, v, do, window=window)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [(-1, -1), (-1, 0), (200, 9)])
+@pytest.mark.parametrize("lengths", [([0, 1, 700, 0, 129, 5], [4, 1, 700, 0, 300, 600]), ([3, 1], [3000, 2500]), ([0, 2000, 129], [4, 1500, 900])])
+def test_packed_walks_shared_by_workgroups(dat, lengths, window, dtype):
+    """Tokens around the sequences are neither read nor written by the launch that adds up either."""
+    H, Hkv, D, before, behind = 2, 1, 72, 5, 9
+    oq, ok = (torch.tensor(np.cumsum([before] + n), dtype=torch.int32, device="cuda") for n in lengths)
+    Tq, Tk = int(oq[-1]) + behind, int(ok[-1]) + behind
+    q, k, v, do = randn(1, Tq, H, D).to(dtype), randn(2, Tk, Hkv, D).to(dtype), randn(3, Tk, Hkv, D).to(dtype), randn(4, Tq, H, D).to(dtype)
+    if dtype == F32 or (window != (200, 9) and len(lengths[0]) < 6):          # (short walks in bf16 are not shared)
+        assert any(shared(q, k, window, oq, ok))
+    for t in (q, k, v, do):
+        t[:before], t[t.shape[0] - behind:] = math.nan, math.inf
+    o, dq, dk, dv = (torch.full_like(t, 7.0) for t in (q, q, k, v))
+    _, lse = dat.attention_forward(q, k, v, window=window, offsets_q=oq, offsets_k=ok, o=o)
+    check_forward(q, k, v, D ** -0.5, window, oq, ok, o, lse)
+    dat.attention_backward(q, k, v, o, lse, do, window=window, offsets_q=oq, offsets_k=ok, dq=dq, dk=dk, dv=dv)
+    check_backward(q, k, v, o, lse, do, D ** -0.5, window, oq, ok, (dq, dk, dv))
+    for t in (o, dq, dk, dv):
+        assert bool((t[:before] == 7.0).all()) and bool((t[t.shape[0] - behind:] == 7.0).all())
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("window", [(-1, -1), (-1, 0), (40, 9)])
 def test_packed_sequences(dat, dtype, window):
@@ -181,8 +229,20 @@ def test_strides(dat, dtype):
 @pytest.mark.parametrize("window", [(-1, 0), (20, 3)])
 def test_hidden_values_may_be_anything(dat, dtype, bad, window):
     """What is not finite reaches the rows that see it and no other."""
-    S, H, D, at = 150, 2, 40, 97
+    hidden_values(dat, 150, 97, dtype, bad, window)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("window", [(-1, 0), (300, 3)])
+def test_hidden_values_where_walks_are_shared(dat, dtype, bad, window):
+    hidden_values(dat, 700, 401, dtype, bad, window, walks=True)
+
+
+def hidden_values(dat, S, at, dtype, bad, window, walks=False):
+    H, D = 2, 40
     q, k, v, do = batch(40, 1, S, S, H, 1, D, dtype)
+    assert any(shared(q, k, window)) or not walks
     o, lse = dat.attention_forward(q, k, v, window=window)
     grads = dat.attention_backward(q, k, v, o, lse, do, window=window)
     sees = torch.from_numpy(pt.seen(S, S, window)).cuda()
@@ -294,9 +354,10 @@ def test_beyond_32_bit_offsets(dat):
     assert_near(host(o), host(o1), 2 * half(BF16) * np.abs(host(v[:, -400:])).max(), "o")
 
 
-def test_streams_and_graphs(dat):
+@pytest.mark.parametrize("S", [150, 700])
+def test_streams_and_graphs(dat, S):
     """On a stream of the caller's; captured, replayed several times with new inputs and eager calls between, against the eager results."""
-    q, k, v, do = batch(100, 2, 150, 150, 4, 2, 64, BF16)
+    q, k, v, do = batch(100, 2, S, S, 4, 2, 64, BF16)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     o, lse = dat.attention_forward(q, k, v, window=(-1, 0), stream=side)
