@@ -347,14 +347,15 @@ dat_status dat_group_norm_backward(const void* x, const void* dy, const float* g
  *              share the key head.  P is made again from q, k and lse; sums in a fixed order (the same bits on every call).
  * Sums, statistics and S, P, dP, dS in fp32; bf16 rounds P and dS to bf16 where they enter a product, and the outputs once.  What a row
  * does not see does not enter it, whatever it holds; where it sees a value that is not finite, elements of its result may be NaN where
- * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row NaN).
+ * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row
+ * NaN), and so do v times 256 keys (o is divided by its probabilities' sum at the end).
  * Outputs overlap neither inputs nor each other (parts of one tensor between each other are fine).  workspace: device, 16-byte aligned,
  * dat_attention_workspace(pass, shape) bytes (pass 0 forward, 1 backward; may be 0, then NULL is allowed); nothing in it outlives the
  * call.  Asynchronous on `stream`, no allocation.
  * DAT_ERR_ARG: null or misaligned pointers, negative sizes, H no multiple of Hkv, outputs that overlap (above) or whose strides lay
  * elements on one another, scale not positive and finite, a window side below -1, one of the offsets without the other, a workspace that
  * is too small; DAT_ERR_SHAPE: D above 128 or no multiple of 8, a length from 2^30 on, token strides from 2^23 bytes on, more tiles
- * of 128 rows than a launch takes. */
+ * of 128 rows than a launch takes, 2^31 tiles of 64 queries or more on a key head. */
 typedef struct { void* data; int64_t batch, token, head; } dat_heads;
 typedef struct {
   dat_dtype dtype;

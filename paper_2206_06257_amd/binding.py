@@ -700,6 +700,10 @@ def _attention(q, k, scale, window, offsets_q, offsets_k):
         raise ValueError("k: %s does not go with q %s" % (tuple(ks), tuple(qs)))
     left, right = window
     D = qs[-1]
+    if not (-1 <= left < 1 << 31 and -1 <= right < 1 << 31):
+        raise ValueError("window: sides are -1 (no limit) or keys below 2^31, got %r" % (window,))
+    if max(qs) >= 1 << 31 or max(ks) >= 1 << 31:
+        raise ValueError("q %s and k %s: sizes have to be below 2^31" % (tuple(qs), tuple(ks)))
     sizes = (_code(q), qs[0] if batched else offsets_q.numel() - 1, qs[-3], ks[-3], qs[-2], ks[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale, left, right)
     if batched:
         return _attention_shape(*sizes) + (True,)
@@ -771,6 +775,8 @@ def _rotary(first, second, gamma_q, gamma_k, positions, frequencies, sections, l
     if len(size) not in (3, 4):
         raise ValueError("q: expected [B, S, H, D] or [T, H, D], got %s" % (tuple(size),))
     D, lead = size[-1], tuple(size[:-2])
+    if max(size) >= 1 << 31 or (second is not None and max(second.shape) >= 1 << 31):
+        raise ValueError("q or k: sizes have to be below 2^31")
     if second is not None and second is not one and (len(second.shape) != len(size) or tuple(second.shape[:-2]) != lead or second.shape[-1] != D):
         raise ValueError("k: %s does not go with q %s" % (tuple(second.shape), tuple(size)))
     for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
@@ -827,10 +833,10 @@ def norm_rotary_backward(q, k, gamma_q, gamma_k, positions, frequencies, section
 
 
 class GradientTable:
-    """Gradient tensors (fp32 or bf16, contiguous, on one GPU, none on another) as clip_gradients takes them; keeps them alive."""
+    """Gradient tensors (fp32 or bf16, contiguous, on one GPU, none on another) as clip_gradients takes them; keeps the memory alive that they have now."""
 
     def __init__(self, tensors):
-        self.tensors = tensors = list(tensors)
+        self.tensors = tensors = [t.detach() if isinstance(t, torch.Tensor) else t for t in tensors]
         if not tensors:
             raise ValueError("a table needs a tensor at least")
         for n, t in enumerate(tensors):

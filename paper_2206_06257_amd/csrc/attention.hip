@@ -724,7 +724,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
   const int lo = max(0, p.row0 - a.right - ahead), hi = min(p.Lq - 1, min(p.row0 + BN, p.Lk) - 1 + a.left - ahead);
   const int wlo = max(0, j0 - a.right - ahead), whi = j0 < p.Lk ? min(p.Lq - 1, min(j0 + 32, p.Lk) - 1 + a.left - ahead) : -1;
   const int mylo = max(0, j - a.right - ahead), myhi = min(p.Lq - 1, j + a.left - ahead);
-  const int alllo = max(0, min(j0 + 32, p.Lk) - 1 - a.right - ahead), allhi = j0 + a.left - ahead;      // rows behind Lq add nothing anyway
+  const int alllo = max(0, min(j0 + 32, p.Lk) - 1 - a.right - ahead), allhi = min(p.Lq - 1, j0 + a.left - ahead);
   const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
   const int from = share(tiles * a.G, p.part, a.parts), to = share(tiles * a.G, p.part + 1, a.parts);      // of the tiles of all heads, one after the other
 
@@ -735,7 +735,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
     const int head = p.hk * a.G + fetched_head, row = (tile0 + fetched_tile) * kTile, left = p.Lq - row;
     qload.load(rows_of(a.q, p.b, p.q0 + row, head), left, s, wave, lane);
     gload.load(rows_of(a.d_o, p.b, p.q0 + row, head), left, s + TILE, wave, lane);
-    if (wave == 0) {                                   // rows that are not there: lse 0 and D 0 beside do = 0
+    if (wave == 0) {                                   // (zeros for rows that are not there)
       const float* st = a.stats + stat_row(a, p, head) + row;
       const uint32_t off = lane < left ? lane * 4 : kOob;
       load_to_lds<4>(descriptor((const char*)st), off, s + STATS);

@@ -279,6 +279,24 @@ def hidden_values(dat, S, at, dtype, bad, window, walks=False):
     assert torch.equal(dq[0, i], grads[0][0, i])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("S", [33, 64, 150])
+def test_scores_of_minus_infinity(dat, dtype, S):
+    """A key that holds -inf under positive queries has no probability: its gradients are 0, all the others are those without it."""
+    q, k, v, do = batch(55, 1, S, S, 2, 1, 40, dtype)
+    q, at = q.abs() + 0.01, S - 2
+    k[0, at, 0, 3] = -math.inf
+    keep = torch.arange(S, device="cuda") != at
+    o, lse = dat.attention_forward(q, k, v)
+    check_forward(q, k[:, keep], v[:, keep], 40 ** -0.5, (-1, -1), None, None, o, lse)
+    _, dk, dv = dat.attention_backward(q, k, v, o, lse, do)
+    want, tol = pt.attention_backward(host(q)[0], host(k[:, keep])[0], host(v[:, keep])[0], host(o)[0], host(lse)[0], host(do)[0], 40 ** -0.5, (-1, -1),
+                                      half(dtype) if dtype == BF16 else 0.0)
+    for n, g in ((1, dk), (2, dv)):
+        assert bool((g[0, at] == 0).all())
+        assert_near(host(g[:, keep])[0], want[n], tol[n] * 1.01 + (half(dtype) + 4 * U) * np.abs(want[n]) * 1.01, "dk" if n == 1 else "dv")
+
+
 def test_rows_that_see_nothing(dat):
     """More queries than keys under a causal window: the first rows have no key; what their gradients hold enters nothing."""
     q, k, v, do = batch(50, 2, 150, 70, 2, 1, 64, BF16)

@@ -245,6 +245,15 @@ def test_clip_is_repeatable_and_beyond_32_bits(dat):
     assert_near(host(big[-5:]), host(tail) / 2, (half(BF16) + 4 * U) * np.abs(host(tail)), "tail")
 
 
+def test_gradient_table_keeps_its_memory(dat):
+    """A tensor that is given other memory afterwards: the table works on what it was made for."""
+    g = torch.full((1000,), 3.0, device="cuda")
+    old, table = g.detach(), dat.gradient_table([g])
+    g.data = torch.ones(1000, device="cuda")
+    assert abs(float(dat.clip_gradients(table, 1.0)) - math.sqrt(9000.0)) < 1e-4
+    assert bool((g == 1).all()) and bool((old == old[0]).all()) and abs(float(old[0]) - 1 / math.sqrt(1000.0)) < 1e-8
+
+
 def test_gradient_table_refuses(dat):
     g = randn(1, 100)
     for bad in ([], [g.cpu()], [g.half()], [g[::2]], [g, g], [g[:50], g[40:]], [g, None]):

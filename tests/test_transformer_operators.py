@@ -101,11 +101,23 @@ def test_attention_binding_refuses():
                  lambda: b.attention_forward(q, k[..., :8], k[..., :8]), lambda: b.attention_forward(q.transpose(2, 3).contiguous().transpose(2, 3), k, k),
                  lambda: b.attention_forward(q, k, k, offsets_q=off), lambda: b.attention_forward(q, k, k, offsets_q=off, offsets_k=off),
                  lambda: b.attention_forward(q[0], k[0], k[0], offsets_q=off.long(), offsets_k=off), lambda: b.attention_forward(q[0], k[0], k[0], offsets_q=off, offsets_k=off[:2]),
-                 lambda: b.attention_forward(q, k, k, o=q[:, :4]), lambda: b.attention_forward(q, k, None), lambda: b.attention_forward(q, k, k, window=(1,)),
+                 lambda: b.attention_forward(q, k, k, o=q[:, :4]), lambda: b.attention_forward(q, k, None), lambda: b.attention_forward(q, k, k, window=(1,)), lambda: b.attention_forward(q, k, k, window=((1 << 32) + 5, 0)),
+                 lambda: b.attention_forward(q, k, k, window=(-1, -2)), lambda: b.attention_forward(q[:1].expand(1 << 31, *q.shape[1:]), k[:1].expand(1 << 31, *k.shape[1:]), k),
                  lambda: b.attention_backward(q, k, k, q, lse[:1], q), lambda: b.attention_backward(q, k, k, q, lse, k), lambda: b.attention_backward(q, k, k, q, lse, q, dk=q),
                  lambda: b.attention_backward(q, k, k, q, lse, q)):
         with pytest.raises((ValueError, AttributeError)):
             call()
+
+
+def test_attention_binding_refuses_sizes_beyond_its_types():
+    q, k = torch.zeros(2, 5, 4, 16), torch.zeros(2, 7, 2, 16)
+    for window in (((1 << 32) + 5, 0), (-1, 1 << 31), (-2, 0)):
+        with pytest.raises(ValueError, match="window"):
+            b.attention_forward(q, k, k, window=window)
+    with pytest.raises(ValueError, match="below 2"):
+        b.attention_forward(*(t[:1].expand((1 << 32) + 1, *t.shape[1:]) for t in (q, k, k)))
+    with pytest.raises(ValueError, match="below 2"):
+        b.norm_rotary_forward(q[:1].expand((1 << 32) + 1, *q.shape[1:]), None, None, None, None, None, [])
 
 
 @pytest.mark.parametrize("window", [(-1, -1), (-1, 0), (2, 1)])
