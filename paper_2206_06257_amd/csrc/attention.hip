@@ -10,6 +10,15 @@
 // P or dS as its B operand from the registers the first one left it in (elements 0-3 of half h are rows 4h.., elements 4-7 rows
 // 8 + 4h..), and reads its A operand from LDS in that order, transposed.  fp32 runs the same code: a 32x32x16 product is eight
 // 32x32x2 ones that take the eight elements of a lane one after the other.
+//
+// Bound by the matrix cores and the vector instructions of the softmax beside them: 64 keys for 32 queries are 32 products of 32 cycles at D = 128
+// and about 150 vector instructions, a third of them exponentials and their arguments (at D = 64 16 products, and the vector work is the
+// longer).  The waves of different workgroups on a SIMD fill each other's gaps; inside a wave fragments are read ahead of their
+// products.  Memory: a tile of 64 rows comes in once for 128 rows of the result, 4 to 5 TB/s out of the L2s, and nothing of S x S size is
+// written.  Measured, operations that the mask leaves: forward 1 x 8192 tokens, 32 heads of 128 on 8, causal 505 us (1090 TFLOP/s; a plain
+// product of 8192^3 reaches 1216 here); 32 x 1024 tokens, 16 heads of 64 188 us (730); 2 x 4096 tokens 165 us (833).
+// Why 32 rows a wave and 128 a workgroup: 64 rows a wave halve the reads of LDS, but need 512 registers, one wave a SIMD (causal
+// 302 -> 392 us at 32 x 1024 x 16 x 128); 256 rows a workgroup (8 waves) 504 -> 493 us on the 8192 tokens, slower on all shorter ones.
 #include "kernels.h"
 #include "heads.h"
 #include <initializer_list>
@@ -424,6 +433,8 @@ __device__ __forceinline__ int share(int n, int part, int parts) { return parts 
 // ---- forward -----------------------------------------------------------------------------------------------------------------
 // The running maximum m (in scores) is raised only where one passes it by kPatience / c: what is summed then stays below 2^kPatience
 // times the sum that the true maximum would give, and few tiles rescale the accumulators.
+// A tile costs a wave, at D = 128, 16 + 16 products, 32 exponentials and the reads of 32 KB from LDS.  Timing with parts left out (32 x 1024 tokens,
+// 16 heads of 128): 311 us; without the tiles' loads 256, without the fragments' reads 276, without both 212.
 template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
   constexpr int ROWB = row_bytes<T, NB>(), BM = 32 * NW, TILE = kTile * ROWB, STAGE = 2 * TILE;
@@ -568,6 +579,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
 }
 
 // ---- gradient by the queries; -D and lse / ln 2 for the pass over the keys --------------------------------------------------
+// The rows of o and d_o are here anyway, so D is made here and no launch of its own reads them.  Three products a pair of tiles; keys by halves of a
+// tile, which needs 32 registers less than both at once and leaves room for two or three workgroups a compute unit.  2 x 6001 tokens, 16
+// heads of 128 on 4, causal: 409 us, 1080 TFLOP/s; 32 x 577 tokens, 16 heads of 64: 93 us, 700 TFLOP/s (640 keys in tiles for 577).
+// (A half tile that no row sees left out: 1112 -> 1147 us for the whole gradient, the test breaks the order of the loads.)
 template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
   constexpr int ROWB = row_bytes<T, NB>(), BM = 32 * NW, TILE = kTile * ROWB, STAGE = 2 * TILE;
@@ -688,6 +703,10 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
 // ---- gradients by keys and values -------------------------------------------------------------------------------------------
 // A wave owns 32 keys, its lanes a key each, and walks over the queries of every head of its group: no sum leaves the workgroup (or the
 // parts, which are added in their order), and the order is always the same.
+// Four products a pair of tiles; two accumulators and two own operands of 128 elements take 192 of the 512 registers that one wave a SIMD
+// has at D > 64, so little runs beside its vector work, waits and barriers: 2 x 6001 tokens as above 650 to 710 us by clock, 830 to 900 TFLOP/s, matrix
+// cores busy 43 % of the time (dq 56 %); 32 x 577 tokens, 16 heads of 64, two waves a SIMD: 122 us, 715 TFLOP/s.  Forming one block's probabilities
+// under the other's products gave 2 % there and lost 20 % at D = 64 (registers); more fragments ahead gave nothing.
 template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
   constexpr int ROWB = row_bytes<T, NB>(), BN = 32 * NW, TILE = kTile * ROWB, STATS = 2 * TILE, STAGE = STATS + 2 * kTile * 4;
@@ -836,7 +855,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
 }
 
 // ---- parts into one result ---------------------------------------------------------------------------------------------------
-// Eight elements a thread, the parts in their order.  Forward: weighted by exp2(m c - the largest m c), over the weighted sum of the l.
+// Bound by HBM or, where it is used most, by its launch: 20 us for dk and dv of 2 x 6001 x 4 x 128 in two parts (98 MB in, 25 MB out, 6 TB/s from the
+// cache), 4.5 us for 8 x 197 x 6 x 64.  Eight elements a thread, the parts in their order.  Forward: weighted by exp2(m c - the largest m c), over the weighted sum of the l.
 struct JoinArgs {
   const float* part; const float* ml; HeadsArg out, second; float* lse;      // second: of the parts behind these (dv behind dk)
   const int32_t* off; int B, S, H, D, parts;
@@ -948,9 +968,10 @@ template <typename T, int NB, int KK> dat_status launch(int pass, AttnArgs a, hi
   a.rows_per_group = (int)tiles;
   const int64_t items = tiles * groups * (pass == kGradKV ? 1 : a.G) * a.parts;
   a.items = (int)items;
-  // a share of the work for each XCD, whose L2 then holds the keys of few heads; under a window the shares are only alike if each has
-  // whole groups
-  a.xcd = a.groups % 8 == 0 || (a.left >= kFar && a.right >= kFar);
+  // A share of the work for each XCD, whose L2 then holds the keys of few heads; under a window the shares of few groups are too unlike.  Measured with
+  // and without, causal: 8 groups 511 / 593 us forward and 1070 / 1321 us backward (the cases named above), 36 groups 366 / 494, 11 300 / 327, 6
+  // 287 / 358 (backward), 12 64 / 66, 9 241 / 230, 5 140 / 137, 3 296 / 251 (forward); no window, 64 sequences of 4 to 1024 tokens 260 / 308.
+  a.xcd = a.groups >= 6 || (a.left >= kFar && a.right >= kFar);
   if (tiles > INT32_MAX || !fits_launch(items + 7, NW * 64)) return DAT_ERR_SHAPE;
   if (items == 0) return DAT_OK;
   const dim3 grid((unsigned)(a.xcd ? (items + 7) / 8 * 8 : items)), block(NW * 64);

@@ -10,6 +10,9 @@
 // each lane making some and the others taking them over.  Queries come first, then keys, so that a step of the wave has one scale.
 // An angle is a product in 64 bits (the exact one up to its last bit, at any position), reduced to quarter turns there; sine and
 // cosine of what is left are Taylor polynomials in fp32 (|x| <= pi/4, degrees 11 and 12: below 1e-9 off).
+// Measured: forward 65536 tokens of 16 + 4 heads of 128, bf16, three axes, 137 us: 672 MB at 4.9 TB/s (a copy reaches 5.14); backward 18464 tokens of
+// 16 + 16 heads of 64, bf16, 50 us: 227 MB at 4.5 TB/s, and 4 us for the sums of dgamma; 10007 tokens of 6 + 6 heads of 80, fp32, 29 us and 4.
+// (With every lane making all its angles, and no heads on their way meanwhile: 217 and 96 us for the first two calls.)
 #include "kernels.h"
 #include "heads.h"
 #include <initializer_list>
@@ -426,6 +429,8 @@ void arrange(const dat_rotary& s, RotArgs& a) {
   a.units = a.D / (2 * w); a.turned = a.pairs / w;
   a.lanes = power_of_two(a.units);
   // heads of a token that a wave takes at once: as many as leave at most an eighth of the steps' places empty
+  // (16 + 4 heads of 128, forward: 4 at once 142 us, 8, a sixth of the places empty, 175, one 138; 16 + 16 of 64, backward: 8 at once 59 us, one 77; 6 + 6 of
+  // 80, backward, fp32: 2 at once 38 us, 4 37, one 41)
   const int groups = 64 / a.lanes;
   auto places = [&](int n) { return ((int64_t)a.H + n - 1) / n * n + ((int64_t)a.Hkv + n - 1) / n * n; };
   a.head_groups = groups;

@@ -189,7 +189,8 @@ def gradients(seed, sizes, kinds, scale=1e-2):
     return out, flat
 
 
-SIZES = [[1], [0, 5, 0], [432, 16, 4608, 32, 320, 10], [8192], [8191, 8193, 1, 16384], [40000], [70001, 3, 0, 12345, 8192], [3] * 200, [100000, 1] * 3, [5_000_001]]
+SIZES = [[1], [0, 5, 0], [432, 16, 4608, 32, 320, 10], [8192], [8191, 8193, 1, 16384], [40000], [70001, 3, 0, 12345, 8192], [3] * 200, [100000, 1] * 3, [5_000_001],
+         [8192, 0, 0, 0], [8190, 1, 1, 3], [4096] * 8, [101] * 16, [101] * 17]          # (the last five about one launch or two)
 
 
 @pytest.mark.parametrize("mixed", [0, 1, 2])
