@@ -679,11 +679,22 @@ def _heads(name, t, dtype, shape, optional=False):
     return _Heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
 
 
-# (a call's sizes without offsets, and what the library says it needs: built once for each set of them)
-@functools.lru_cache(maxsize=1024)
-def _attention_shape(*sizes):
+def _like(t):
+    """An output of a tensor's size and type, without its strides."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _attention_sizes(*sizes):
+    """A call's sizes, checked, and what the library says it needs."""
+    if max(sizes[1:7]) >= 1 << 31:
+        raise ValueError("q or k: sizes have to be below 2^31")
+    if not all(-1 <= side < 1 << 31 for side in sizes[8:10]):
+        raise ValueError("window: sides are -1 (no limit) or keys below 2^31, got %r" % (sizes[8:10],))
     shape = _Attention(*sizes)
     return shape, (int(_lib.dat_attention_workspace(0, shape)), int(_lib.dat_attention_workspace(1, shape)))
+
+
+_attention_shape = functools.lru_cache(maxsize=1024)(_attention_sizes)       # (without offsets: built once for each set of them)
 
 
 def _attention(q, k, scale, window, offsets_q, offsets_k):
@@ -700,10 +711,6 @@ def _attention(q, k, scale, window, offsets_q, offsets_k):
         raise ValueError("k: %s does not go with q %s" % (tuple(ks), tuple(qs)))
     left, right = window
     D = qs[-1]
-    if not (-1 <= left < 1 << 31 and -1 <= right < 1 << 31):
-        raise ValueError("window: sides are -1 (no limit) or keys below 2^31, got %r" % (window,))
-    if max(qs) >= 1 << 31 or max(ks) >= 1 << 31:
-        raise ValueError("q %s and k %s: sizes have to be below 2^31" % (tuple(qs), tuple(ks)))
     sizes = (_code(q), qs[0] if batched else offsets_q.numel() - 1, qs[-3], ks[-3], qs[-2], ks[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale, left, right)
     if batched:
         return _attention_shape(*sizes) + (True,)
@@ -711,8 +718,7 @@ def _attention(q, k, scale, window, offsets_q, offsets_k):
     _want("offsets_k", offsets_k, (torch.int32,), offsets_q.shape)
     if offsets_q.dim() != 1 or offsets_q.numel() < 1:
         raise ValueError("offsets_q: expected [B + 1], got %s" % (tuple(offsets_q.shape),))
-    shape = _Attention(*sizes, _at(offsets_q), _at(offsets_k))
-    return shape, (int(_lib.dat_attention_workspace(0, shape)), int(_lib.dat_attention_workspace(1, shape))), False
+    return _attention_sizes(*sizes, _at(offsets_q), _at(offsets_k)) + (False,)
 
 
 def _lse_shape(q, batched):
@@ -728,9 +734,9 @@ def attention_forward(q, k, v, scale=None, window=(-1, -1), offsets_q=None, offs
     hq, hk, hv, ho = _heads("q", q, dtype, qs), _heads("k", k, dtype, ks), _heads("v", v, dtype, ks), _heads("o", o, dtype, qs, optional=True)
     with _On(stream, q, k, v, o, offsets_q, offsets_k) as st:
         if o is None:
-            o = q.new_empty(qs)
+            o = _like(q)
             ho = _heads("o", o, dtype, qs)
-        lse = q.new_empty(_lse_shape(q, batched), dtype=torch.float32)
+        lse = torch.empty(*_lse_shape(q, batched), dtype=torch.float32, device=q.device)
         ws = torch.empty(need[0], dtype=torch.uint8, device=q.device) if need[0] else None
         _check(_lib.dat_attention_forward(shape, hq, hk, hv, ho, lse.data_ptr(), _at(ws), need[0], st), "dat_attention_forward")
     return o, lse
@@ -746,7 +752,7 @@ def attention_backward(q, k, v, o, lse, do, scale=None, window=(-1, -1), offsets
     for name, t, like in (("dq", dq, qs), ("dk", dk, ks), ("dv", dv, ks)):
         _heads(name, t, dtype, like, optional=True)
     with _On(stream, q, k, v, o, lse, do, dq, dk, dv, offsets_q, offsets_k) as st:
-        dq, dk, dv = (q.new_empty(like) if t is None else t for t, like in ((dq, qs), (dk, ks), (dv, ks)))
+        dq, dk, dv = (_like(x) if t is None else t for t, x in ((dq, q), (dk, k), (dv, k)))
         ws = torch.empty(need[1], dtype=torch.uint8, device=q.device) if need[1] else None
         _check(_lib.dat_attention_backward(shape, *given, lse.data_ptr(), hdo, _heads("dq", dq, dtype, qs), _heads("dk", dk, dtype, ks), _heads("dv", dv, dtype, ks),
                                            _at(ws), need[1], st), "dat_attention_backward")
@@ -760,6 +766,8 @@ def rotary_frequencies(sections, base=10000.0, device="cuda"):
 
 @functools.lru_cache(maxsize=1024)
 def _rotary_shape(dtype, B, S, H, Hkv, D, sections, layout, norm, eps):
+    if max(B, S, H, Hkv, D) >= 1 << 31:
+        raise ValueError("q or k: sizes have to be below 2^31")
     shape = _Rotary(dtype, B, S, H, Hkv, D, len(sections), (C.c_int32 * 4)(*sections), layout, norm, eps)
     return shape, int(_lib.dat_norm_rotary_workspace(1, shape))
 
@@ -775,8 +783,6 @@ def _rotary(first, second, gamma_q, gamma_k, positions, frequencies, sections, l
     if len(size) not in (3, 4):
         raise ValueError("q: expected [B, S, H, D] or [T, H, D], got %s" % (tuple(size),))
     D, lead = size[-1], tuple(size[:-2])
-    if max(size) >= 1 << 31 or (second is not None and max(second.shape) >= 1 << 31):
-        raise ValueError("q or k: sizes have to be below 2^31")
     if second is not None and second is not one and (len(second.shape) != len(size) or tuple(second.shape[:-2]) != lead or second.shape[-1] != D):
         raise ValueError("k: %s does not go with q %s" % (tuple(second.shape), tuple(size)))
     for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
@@ -802,7 +808,7 @@ def norm_rotary_forward(q, k, gamma_q, gamma_k, positions, frequencies, sections
         if like is not None:
             _heads(name, t, dtype, like.shape, optional=True)
     with _On(stream, first, k, gamma_q, gamma_k, positions, frequencies, yq, yk) as st:
-        yq, yk = (None if like is None else like.new_empty(like.shape) if t is None else t for t, like in ((yq, q), (yk, k)))
+        yq, yk = (None if like is None else _like(like) if t is None else t for t, like in ((yq, q), (yk, k)))
         out = [None if t is None else _heads("y", t, dtype, t.shape) for t in (yq, yk)]
         _check(_lib.dat_norm_rotary_forward(shape, *given, _at(gamma_q), _at(gamma_k), _at(positions), _at(frequencies), *out, st), "dat_norm_rotary_forward")
     return yq, yk
@@ -822,7 +828,7 @@ def norm_rotary_backward(q, k, gamma_q, gamma_k, positions, frequencies, section
     for name, t in (("dgamma_q", dgamma_q), ("dgamma_k", dgamma_k)):
         _want(name, t, (torch.float32,), (D,), optional=True)
     with _On(stream, first, dyk, q, k, gamma_q, gamma_k, positions, frequencies, dq, dk, dgamma_q, dgamma_k) as st:
-        dq, dk = (None if like is None else like.new_empty(like.shape) if t is None else t for t, like in ((dq, dyq), (dk, dyk)))
+        dq, dk = (None if like is None else _like(like) if t is None else t for t, like in ((dq, dyq), (dk, dyk)))
         dgamma_q, dgamma_k = (torch.empty(D, device=first.device) if t is None and norm and gamma is not None and like is not None else t
                               for t, gamma, like in ((dgamma_q, gamma_q, dyq), (dgamma_k, gamma_k, dyk)))
         out = [None if t is None else _heads("dx", t, dtype, t.shape) for t in (dq, dk)]

@@ -15,7 +15,7 @@
 // and about 150 vector instructions, a third of them exponentials and their arguments (at D = 64 16 products, and the vector work is the
 // longer).  The waves of different workgroups on a SIMD fill each other's gaps; inside a wave fragments are read ahead of their
 // products.  Memory: a tile of 64 rows comes in once for 128 rows of the result, 4 to 5 TB/s out of the L2s, and nothing of S x S size is
-// written.  Measured, operations that the mask leaves: forward 1 x 8192 tokens, 32 heads of 128 on 8, causal 505 us (1090 TFLOP/s; a plain
+// written.  Measured, operations that the mask leaves: forward 1 x 8192 tokens, 32 heads of 128 on 8, causal 497 us (1107 TFLOP/s; a plain
 // product of 8192^3 reaches 1216 here); 32 x 1024 tokens, 16 heads of 64 188 us (730); 2 x 4096 tokens 165 us (833).
 // Why 32 rows a wave and 128 a workgroup: 64 rows a wave halve the reads of LDS, but need 512 registers, one wave a SIMD (causal
 // 302 -> 392 us at 32 x 1024 x 16 x 128); 256 rows a workgroup (8 waves) 504 -> 493 us on the 8192 tokens, slower on all shorter ones.

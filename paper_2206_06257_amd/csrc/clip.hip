@@ -6,7 +6,7 @@
 // that costs nothing.  Bound by HBM: one read and, where c < 1, one more read and a write.  Tensors are cut into blocks of kBlock elements; block j
 // of tensor t has the slot off[t] / kBlock + t + j (strictly increasing in (t, j)), and a workgroup takes a range of slots, in the
 // second pass from its end, which is what the last-level cache still holds.
-// Measured: 236 M elements, bf16 matrices and fp32 vectors (472 MB), 292 us where they are scaled: 85 to 104 us for the sum (4.5 to 5.6 TB/s, part of it
+// Measured: 236 M elements, bf16 matrices and fp32 vectors (472 MB), 292 us where they are scaled: 91 to 106 us for the sum (4.5 to 5.2 TB/s, part of it
 // from the cache), 154 us for the scaling (945 MB at 6.1 TB/s).
 #include "kernels.h"
 #include "tensor_table.h"
@@ -147,7 +147,7 @@ template <int PASS> __global__ __launch_bounds__(PASS == 2 ? kAloneThreads : kTh
   constexpr int THREADS = PASS == 2 ? kAloneThreads : kThreads, LANES = PASS == 2 ? 64 : kThreads, STEP = THREADS / LANES;
   __shared__ double s[THREADS / 64];
   const int at = threadIdx.x % LANES;
-  const int start = min((int)blockIdx.x * a.per, a.slots), last = min(start + a.per, a.slots), first = start + (int)threadIdx.x / LANES;
+  const int start = min((int)blockIdx.x * a.per, a.slots), last = min(start + a.per, a.slots), first = PASS == 2 ? start + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) : start;
   double sum = 0.0;
   if (PASS != 1) {
     each_block(a, first, last, STEP, false, [&](const Block& b) { if (b.half) squares_of<Vec2, true, LANES>(b, at, sum); else squares_of<Vec4, false, LANES>(b, at, sum); });
