@@ -343,8 +343,9 @@ dat_status dat_group_norm_backward(const void* x, const void* dy, const float* g
  * limit on that side; left = -1, right = 0 is causal.
  *   forward:   S = scale q k^T over what a row sees, lse = log sum_j exp S_j, P = exp(S - lse), o = P v; a row that sees nothing has o = 0,
  *              lse = -inf.  lse: device fp32 [B][H][Sq] ([H][Sq] packed).
- *   backward:  D = sum_d d_o o, dP = d_o v^T, dS = P (dP - D); dq = scale dS k, dk = scale dS^T q and dv = P^T d_o, over all heads that
- *              share the key head.  P is made again from q, k and lse; sums in a fixed order (the same bits on every call).
+ *   backward (o and lse: the forward call's for the same shape):  D = sum_d d_o o, dP = d_o v^T, dS = P (dP - D); dq = scale dS k,
+ *              dk = scale dS^T q and dv = P^T d_o, over all heads that share the key head.  P is made again from q, k and lse; sums in a
+ *              fixed order (the same bits on every call).  A query that sees one key has dq = 0, and where no query sees more dk = 0.
  * Sums, statistics and S, P, dP, dS in fp32; bf16 rounds P and dS to bf16 where they enter a product, and the outputs once.  What a row
  * does not see does not enter it, whatever it holds; where it sees a value that is not finite, elements of its result may be NaN where
  * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row

@@ -399,6 +399,7 @@ __device__ __forceinline__ void wait_own() {
 __device__ __forceinline__ void wait_tile() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");               // (the barrier alone does not hold reads of LDS back)
 }
 
 template <int N> struct Stage { static constexpr int value = N; };
@@ -696,8 +697,9 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
     cols.shift(STAGE);
   }
   if (careful && there) spoil<T, NB>(acc, kbase, a.k.token, max(mylo, from * kTile), min(myhi, to * kTile - 1), lane, a.D);
-  if (a.parts > 1) store_rows<float, NB>((char*)(a.part + (p.part * a.rows + at) * a.D), there, acc, a.scale, lane, a.D);
-  else store_rows<T, NB>(rows_of(a.dq, p.b, p.q0 + i, head), there, acc, a.scale, lane, a.D);
+  const float factor = mylo == myhi ? 0.0f : a.scale;             // the softmax of one score has no gradient, and what rounding leaves of dP - D is none
+  if (a.parts > 1) store_rows<float, NB>((char*)(a.part + (p.part * a.rows + at) * a.D), there, acc, factor, lane, a.D);
+  else store_rows<T, NB>(rows_of(a.dq, p.b, p.q0 + i, head), there, acc, factor, lane, a.D);
 }
 
 // ---- gradients by keys and values -------------------------------------------------------------------------------------------
@@ -844,12 +846,13 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
       spoil<T, NB>(dk, rows_of(a.q, p.b, p.q0, p.hk * a.G + g), a.q.token, r0, r1, lane, a.D);
       spoil<T, NB>(dv, rows_of(a.d_o, p.b, p.q0, p.hk * a.G + g), a.d_o.token, r0, r1, lane, a.D);
     }
+  const float factor = p.Lk == 1 || (a.left | a.right) == 0 ? 0.0f : a.scale;       // (no query sees more than one key)
   if (a.parts > 1) {
     const int64_t row = p.part * a.key_rows + key_row(a, p) + j;
-    store_rows<float, NB>((char*)(a.part + row * a.D), there, dk, a.scale, lane, a.D);
+    store_rows<float, NB>((char*)(a.part + row * a.D), there, dk, factor, lane, a.D);
     store_rows<float, NB>((char*)(a.part + (a.parts * a.key_rows + row) * a.D), there, dv, 1.0f, lane, a.D);
   } else {
-    store_rows<T, NB>(rows_of(a.dk, p.b, p.k0 + j, p.hk), there, dk, a.scale, lane, a.D);
+    store_rows<T, NB>(rows_of(a.dk, p.b, p.k0 + j, p.hk), there, dk, factor, lane, a.D);
     store_rows<T, NB>(rows_of(a.dv, p.b, p.k0 + j, p.hk), there, dv, 1.0f, lane, a.D);
   }
 }

@@ -297,6 +297,21 @@ def test_scores_of_minus_infinity(dat, dtype, S):
         assert_near(host(g[:, keep])[0], want[n], tol[n] * 1.01 + (half(dtype) + 4 * U) * np.abs(want[n]) * 1.01, "dk" if n == 1 else "dv")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_key_has_no_gradient_by_its_score(dat, dtype):
+    """The softmax of a single score is 1: dq, and dk where no query sees more, are 0 and not what rounding leaves; dv is the sum of d_o."""
+    for Sq, Sk, window in ((1, 1, (-1, -1)), (300, 1, (-1, -1)), (5, 1, (-1, 0)), (200, 200, (0, 0)), (70, 200, (0, 0)), (700, 700, (0, 0))):
+        q, k, v, do = batch(57, 2, Sq, Sk, 4, 2, 72, dtype)
+        _, _, (dq, dk, _) = check(dat, q, k, v, do, window=window)
+        assert bool((dq == 0).all()) and bool((dk == 0).all()), (Sq, Sk, window)
+    q, k, v, do = batch(58, 2, 200, 200, 4, 2, 72, dtype)
+    _, _, (dq, dk, _) = check(dat, q, k, v, do, window=(-1, 0))
+    assert bool((dq[:, 0] == 0).all()) and bool((dq[:, 1] != 0).any()) and bool((dk != 0).any())
+    do[0, 1, 0, 0] = math.nan                                      # (a NaN stays one)
+    dq = dat.attention_backward(q, k, v, *dat.attention_forward(q, k, v, window=(0, 0)), do, window=(0, 0))[0]
+    assert bool(torch.isnan(dq[0, 1, 0]).all()) and bool((dq[0, 2:] == 0).all())
+
+
 def test_rows_that_see_nothing(dat):
     """More queries than keys under a causal window: the first rows have no key; what their gradients hold enters nothing."""
     q, k, v, do = batch(50, 2, 150, 70, 2, 1, 64, BF16)
