@@ -34,7 +34,7 @@ typedef short v4s16 __attribute__((ext_vector_type(4)));
 typedef __amdgpu_buffer_rsrc_t BufRsrc;
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr float kInf = __builtin_inff();
+constexpr float kInf = __builtin_inff(), kLargest = 0x1.fffffep127f;
 constexpr int kFar = 1 << 30;                    // lengths stay below it: a window side without a limit
 constexpr uint32_t kOob = 0xfffffff0u;           // an offset behind every descriptor's range: the load delivers zeros
 constexpr int kTile = 64;                        // rows of an LDS tile
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
 
   f32x16 acc[NB];
   float m, l;
-  const float patience = (float)kPatience / a.c;
+  const float patience = fminf((float)kPatience / a.c, kLargest);   // finite: m rises from -inf at any scale
   auto step = [&](auto stage, int t) {
     constexpr int AT = decltype(stage)::value * STAGE;
     const int j0 = t * kTile;

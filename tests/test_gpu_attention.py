@@ -410,3 +410,15 @@ def test_streams_and_graphs(dat, S):
         grads = dat.attention_backward(q, k, v, o, lse, do, window=(-1, 0))
         torch.cuda.synchronize()
         assert torch.equal(o, co) and torch.equal(lse, cl) and all(torch.equal(a, b) for a, b in zip(grads, cg))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [1.7e-38, 1.5e-38, 1e-40, 1e-44])
+@pytest.mark.parametrize("shape", [(2, 70, 150, 4, 2, 64), (1, 5, 4100, 4, 2, 72)])
+def test_the_smallest_scales(dat, shape, scale, dtype):
+    """Scores that all but vanish: the probabilities are alike, and lse is the logarithm of the keys' number, in one walk and in shared ones."""
+    q, k, v, do = batch(62, *shape, dtype)
+    assert shape[1] > 5 or any(shared(q, k, (-1, -1)))
+    for window in ((-1, -1), (-1, 0), (40, 3)):
+        o, lse, grads = check(dat, q, k, v, do, window=window, scale=scale)
+        assert bool(torch.isfinite(lse).all()) and bool((grads[2] != 0).any())
