@@ -345,7 +345,8 @@ dat_status dat_group_norm_backward(const void* x, const void* dy, const float* g
  *              lse = -inf.  lse: device fp32 [B][H][Sq] ([H][Sq] packed).
  *   backward (o and lse: the forward call's for the same shape):  D = sum_d d_o o, dP = d_o v^T, dS = P (dP - D); dq = scale dS k,
  *              dk = scale dS^T q and dv = P^T d_o, over all heads that share the key head.  P is made again from q, k and lse; sums in a
- *              fixed order (the same bits on every call).  A query that sees one key has dq = 0, and where no query sees more dk = 0.
+ *              fixed order (the same bits on every call).  A query that sees one key has dq = 0 and adds
+ *              nothing to dk.
  * Sums, statistics and S, P, dP, dS in fp32; bf16 rounds P and dS to bf16 where they enter a product, and the outputs once.  What a row
  * does not see does not enter it, whatever it holds; where it sees a value that is not finite, elements of its result may be NaN where
  * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row

@@ -745,7 +745,9 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
   const int lo = max(0, p.row0 - a.right - ahead), hi = min(p.Lq - 1, min(p.row0 + BN, p.Lk) - 1 + a.left - ahead);
   const int wlo = max(0, j0 - a.right - ahead), whi = j0 < p.Lk ? min(p.Lq - 1, min(j0 + 32, p.Lk) - 1 + a.left - ahead) : -1;
   const int mylo = max(0, j - a.right - ahead), myhi = min(p.Lq - 1, j + a.left - ahead);
-  const int alllo = max(0, min(j0 + 32, p.Lk) - 1 - a.right - ahead), allhi = min(p.Lq - 1, j0 + a.left - ahead);
+  // Rows between these see every key of the wave and no row that sees one key alone is among them: query -right - ahead sees key 0 alone and no
+  // other key of that wave; where left = 0 the last query sees the last key alone, which may be its wave's only one.
+  const int alllo = max(0, min(j0 + 32, p.Lk) - 1 - a.right - ahead), allhi = min(p.Lq - 1 - (a.left == 0), j0 + a.left - ahead);
   const int tile0 = lo / kTile, tiles = hi >= lo ? hi / kTile - tile0 + 1 : 0;
   const int from = share(tiles * a.G, p.part, a.parts), to = share(tiles * a.G, p.part + 1, a.parts);      // of the tiles of all heads, one after the other
 
@@ -809,13 +811,17 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
         }
       }
       if (border) {
-        const int first = mylo - i0 - 4 * half, behind = myhi - i0 - 4 * half;
+        int at = lane;
+        if constexpr (NB > 2) asm volatile("" : "+v"(at));     // (made again for each border: kept over the loop this costs registers that D > 96 does not have)
+        const int key = j0 + (at & 31), base = i0 + 4 * (at >> 5);
+        const int first = max(0, key - a.right - ahead) - base, behind = min(p.Lq - 1, key + a.left - ahead) - base;
+        const int alone = max(key == 0 ? -a.right - ahead : key == p.Lk - 1 && a.left == 0 ? p.Lq - 1 : -1, -1) - base;     // the query that sees no other key
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int i = 32 * nb + 8 * (r >> 2) + (r & 3);
           const bool see = i >= first && i <= behind;
           s[r] = see ? s[r] : 0.0f;
-          dp[r] = see ? dp[r] : 0.0f;
+          dp[r] = see ? i == alone ? 0.0f * dp[r] : dp[r] : 0.0f;      // (one score has no gradient; a NaN stays one)
         }
       }
       Frag<T> pk, ds;
@@ -846,7 +852,7 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
       spoil<T, NB>(dk, rows_of(a.q, p.b, p.q0, p.hk * a.G + g), a.q.token, r0, r1, lane, a.D);
       spoil<T, NB>(dv, rows_of(a.d_o, p.b, p.q0, p.hk * a.G + g), a.d_o.token, r0, r1, lane, a.D);
     }
-  const float factor = p.Lk == 1 || (a.left | a.right) == 0 ? 0.0f : a.scale;       // (no query sees more than one key)
+  const float factor = p.Lk == 1 || (a.left | a.right) == 0 ? 0.0f : a.scale;       // (no query sees more than one key; single ones among others: at the border, above)
   if (a.parts > 1) {
     const int64_t row = p.part * a.key_rows + key_row(a, p) + j;
     store_rows<float, NB>((char*)(a.part + row * a.D), there, dk, factor, lane, a.D);

@@ -422,3 +422,26 @@ def test_the_smallest_scales(dat, shape, scale, dtype):
     for window in ((-1, -1), (-1, 0), (40, 3)):
         o, lse, grads = check(dat, q, k, v, do, window=window, scale=scale)
         assert bool(torch.isfinite(lse).all()) and bool((grads[2] != 0).any())
+
+
+# queries that see one key at a window's ends: key 0 (a limit on the right) or the last one (0 on the left), alone in its wave among them
+ALONE = [(1, 70, (0, -1)), (1, 70, (0, 3)), (200, 200, (-1, 0)), (150, 70, (-1, 0)), (150, 70, (16, 5)), (97, 97, (0, -1)), (64, 97, (0, -1)), (64, 97, (0, 40)),
+         (128, 33, (0, 12)), (130, 65, (0, 64)), (700, 700, (-1, 0)), (640, 641, (0, -1))]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("Sq,Sk,window", ALONE)
+def test_a_query_of_one_key_adds_nothing_to_dk(dat, Sq, Sk, window, dtype):
+    """Gradients that enter only at queries of one key: dk is exactly 0, dv is not; a NaN among them stays one in dk of their key alone."""
+    q, k, v, do = batch(59, 2, Sq, Sk, 4, 2, 72, dtype)
+    see = torch.from_numpy(pt.seen(Sq, Sk, window)).cuda()
+    alone = see.sum(1) == 1
+    assert bool(alone.any()) and bool((see.sum(1) > 1).any() or Sq == 1)
+    check(dat, q, k, v, do, window=window)
+    do[:, ~alone] = 0
+    o, lse, (dq, dk, dv) = check(dat, q, k, v, do, window=window)
+    assert bool((dk == 0).all()) and bool((dq == 0).all()) and bool((dv != 0).any())
+    do[0, alone, 1, 3] = math.nan
+    _, dk, dv = dat.attention_backward(q, k, v, o, lse, do, window=window)
+    key = see[alone].any(0)
+    assert bool(torch.isnan(dk[0, key, 0]).all()) and bool((dk[0, ~key] == 0).all()) and bool((dk[1] == 0).all()) and bool((dk[:, :, 1] == 0).all())
