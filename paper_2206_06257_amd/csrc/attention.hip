@@ -1050,7 +1050,7 @@ bool fill(const dat_attention* s, AttnArgs& a, dat_status& status) {
 dat_status take(const dat_heads* t, const HeadsShape& s, size_t width, bool output, HeadsArg& out) {
   if (!t) return DAT_ERR_ARG;
   if (s.batch * s.tokens * s.heads == 0) { out = HeadsArg{(char*)t->data, 0, 0, 0}; return DAT_OK; }
-  if (!heads_vectors(*t, s, width) || (output && !heads_dims(*t, s).apart)) return DAT_ERR_ARG;
+  if (!heads_vectors(*t, s, width) || (output && !heads_apart(*t, s))) return DAT_ERR_ARG;
   const int64_t w = (int64_t)width, token = s.tokens > 1 ? t->token * w : 0;
   if (token >= (int64_t)1 << 23) return DAT_ERR_SHAPE;             // the offsets in a tile of up to 256 rows are 31 bits
   out = HeadsArg{(char*)t->data, s.batch > 1 ? t->batch * w : 0, token, s.heads > 1 ? t->head * w : 0};

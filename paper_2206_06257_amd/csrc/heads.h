@@ -6,59 +6,68 @@ namespace dat {
 
 struct HeadsShape { int64_t batch, tokens, heads, D; };
 
-// The dimensions of a tensor from the widest stride to the narrowest; false where some of its elements lie on one another (or may).
-struct HeadsDims { int64_t stride[3], count[3], inner[3]; bool apart; };   // inner: elements from the first to behind the last of what lies inside
-inline HeadsDims heads_dims(const dat_heads& t, const HeadsShape& s) {
-  HeadsDims d;
-  const int64_t stride[3] = {t.batch, t.token, t.head}, count[3] = {s.batch, s.tokens, s.heads};
-  int order[3] = {0, 1, 2};
-  auto wider = [&](int a, int b) { return (count[a] > 1 ? stride[a] : 0) > (count[b] > 1 ? stride[b] : 0); };
+// Whether a tensor's elements are apart: each dimension's stride reaches over what lies inside it, from the widest stride to the narrowest.
+inline bool heads_apart(const dat_heads& t, const HeadsShape& s) {
+  int64_t stride[3] = {t.batch, t.token, t.head}, count[3] = {s.batch, s.tokens, s.heads};
+  for (int i = 0; i < 3; ++i) if (count[i] <= 1) stride[i] = 0;
   for (int i = 0; i < 3; ++i)
-    for (int j = i + 1; j < 3; ++j) if (wider(order[j], order[i])) { const int x = order[i]; order[i] = order[j]; order[j] = x; }
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[j] > stride[i]) { const int64_t x = stride[i], n = count[i]; stride[i] = stride[j]; count[i] = count[j]; stride[j] = x; count[j] = n; }
   int64_t inner = s.D;
-  d.apart = true;
   for (int i = 2; i >= 0; --i) {
-    d.count[i] = count[order[i]];
-    d.stride[i] = d.count[i] > 1 ? stride[order[i]] : 0;
-    d.inner[i] = inner;
-    if (d.count[i] > 1 && d.stride[i] < inner) d.apart = false;
-    if (d.count[i] > 1) inner += d.stride[i] * (d.count[i] - 1);
+    if (count[i] <= 1) continue;
+    if (stride[i] < inner) return false;
+    inner += stride[i] * (count[i] - 1);
   }
-  return d;
+  return true;
 }
 inline int64_t heads_extent(const dat_heads& t, const HeadsShape& s) {
-  const HeadsDims d = heads_dims(t, s);
-  return d.inner[0] + (d.count[0] > 1 ? d.stride[0] * (d.count[0] - 1) : 0);
+  const int64_t stride[3] = {t.batch, t.token, t.head}, count[3] = {s.batch, s.tokens, s.heads};
+  int64_t extent = s.D;
+  for (int i = 0; i < 3; ++i) if (count[i] > 1) extent += stride[i] * (count[i] - 1);
+  return extent;
 }
 
-// Whether elements of two tensors with the same strides, the second (b) `delta` elements behind the first (a), are the same one.
-inline bool nested_overlap(int64_t delta, const HeadsDims& a, const HeadsDims& b, int level, int64_t D) {
-  if (level == 3) return delta < D && -delta < D;
-  const int64_t s = a.stride[level] ? a.stride[level] : b.stride[level];     // a's index less b's: above -b's count, below a's
-  if (a.count[level] <= 1 && b.count[level] <= 1) return nested_overlap(delta, a, b, level + 1, D);
-  int64_t i = delta / s;
-  if (delta < 0 && i * s != delta) --i;                 // floor
+// A dimension (batch, token or head) of two tensors that step through it alike; a dimension of one has no stride.
+struct SharedDim { int64_t stride, a, b; };             // and how many the first has of it, and the second
+
+// Whether elements of two tensors, the second `delta` elements behind the first, are the same one; dimensions from the widest stride to the
+// narrowest, each reaching over what lies inside it in either tensor.
+inline bool nested_overlap(int64_t delta, const SharedDim* d, int left, int64_t D) {
+  if (left == 0) return delta < D && -delta < D;
+  if (d->a <= 1 && d->b <= 1) return nested_overlap(delta, d + 1, left - 1, D);
+  int64_t i = delta / d->stride;                        // the first's index less the second's: above -b, below a
+  if (delta < 0 && i * d->stride != delta) --i;         // floor
   for (int64_t k = i; k <= i + 1; ++k)
-    if (k < a.count[level] && -k < b.count[level] && nested_overlap(delta - k * s, a, b, level + 1, D)) return true;
+    if (k < d->a && -k < d->b && nested_overlap(delta - k * d->stride, d + 1, left - 1, D)) return true;
   return false;
 }
 
-// Whether two tensors share an element: exact where their strides agree (parts of one tensor), by their extents elsewhere.
+// Whether two tensors share an element: exact where they step through each dimension alike (parts of one tensor), by their extents elsewhere.
 inline bool heads_overlap(const dat_heads& x, const HeadsShape& sx, const dat_heads& y, const HeadsShape& sy, size_t width) {
   if (sx.batch * sx.tokens * sx.heads == 0 || sy.batch * sy.tokens * sy.heads == 0) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(x.data), b = reinterpret_cast<uintptr_t>(y.data);
   const uintptr_t ea = a + (uintptr_t)heads_extent(x, sx) * width, eb = b + (uintptr_t)heads_extent(y, sy) * width;
   if (ea <= b || eb <= a) return false;
-  const HeadsDims dx = heads_dims(x, sx), dy = heads_dims(y, sy);
-  const int64_t gap = (int64_t)(b - a);
-  bool same = dx.apart && dy.apart && gap % (int64_t)width == 0;
-  for (int i = 0; i < 3; ++i) same = same && (dx.count[i] <= 1 || dy.count[i] <= 1 || dx.stride[i] == dy.stride[i]);
-  for (int i = 0; i < 3; ++i)                           // a level's stride has to reach over what lies inside in either tensor
-    if (dx.count[i] > 1 || dy.count[i] > 1) {
-      const int64_t s = dx.stride[i] ? dx.stride[i] : dy.stride[i];
-      same = same && s >= dx.inner[i] && s >= dy.inner[i];
-    }
-  return same ? nested_overlap(gap / (int64_t)width, dx, dy, 0, sx.D) : true;
+  const int64_t gap = (int64_t)(b - a), xs[3] = {x.batch, x.token, x.head}, ys[3] = {y.batch, y.token, y.head};
+  const int64_t xn[3] = {sx.batch, sx.tokens, sx.heads}, yn[3] = {sy.batch, sy.tokens, sy.heads};
+  SharedDim dims[3];
+  bool alike = gap % (int64_t)width == 0;
+  for (int i = 0; i < 3; ++i) {                         // dimension by dimension, then sorted by what both step by: a tensor's own order may differ
+    dims[i] = SharedDim{xn[i] > 1 ? xs[i] : yn[i] > 1 ? ys[i] : 0, xn[i], yn[i]};
+    alike = alike && (xn[i] <= 1 || yn[i] <= 1 || xs[i] == ys[i]);
+  }
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j) if (dims[j].stride > dims[i].stride) { const SharedDim d = dims[i]; dims[i] = dims[j]; dims[j] = d; }
+  int64_t inner_a = sx.D, inner_b = sy.D;               // elements from the first to behind the last of what lies inside
+  for (int i = 2; i >= 0; --i) {
+    const SharedDim& d = dims[i];
+    if (d.a <= 1 && d.b <= 1) continue;
+    alike = alike && d.stride >= inner_a && d.stride >= inner_b;
+    inner_a += d.stride * (d.a - 1);
+    inner_b += d.stride * (d.b - 1);
+  }
+  return alike ? nested_overlap(gap / (int64_t)width, dims, 3, sx.D) : true;
 }
 
 // Alignment of 16-byte vectors; strides at least 0 (that of a dimension of one is not looked at).

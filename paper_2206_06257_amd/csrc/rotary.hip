@@ -466,7 +466,7 @@ struct Tensor { const dat_heads* t; HeadsShape s; Rows* to; bool output; };
 
 dat_status take(const Tensor& x, size_t width) {
   if (x.s.batch * x.s.tokens * x.s.heads == 0) { *x.to = Rows{nullptr, 0, 0, 0}; return DAT_OK; }
-  if (!x.t || !heads_vectors(*x.t, x.s, width) || (x.output && !heads_dims(*x.t, x.s).apart)) return DAT_ERR_ARG;
+  if (!x.t || !heads_vectors(*x.t, x.s, width) || (x.output && !heads_apart(*x.t, x.s))) return DAT_ERR_ARG;
   const int64_t w = (int64_t)width;
   *x.to = Rows{(char*)x.t->data, x.s.batch > 1 ? x.t->batch * w : 0, x.s.tokens > 1 ? x.t->token * w : 0, x.s.heads > 1 ? x.t->head * w : 0};
   return DAT_OK;

@@ -234,3 +234,63 @@ def test_clip_gradients_binding_refuses():
 def test_plain_clip():
     norm, out, c = pt.clip([np.array([3.0]), np.array([0.0, 4.0])], 2.5)
     assert norm == 5.0 and c == 0.5 and out[1][1] == 2.0 and pt.clip([np.array([3.0])], 3.0)[2] == 1.0
+
+
+# Calls that are refused for their launch (DAT_ERR_SHAPE), which is looked at behind the overlaps (DAT_ERR_ARG): nothing is launched.
+def places_in(layout, S, W, D):
+    """Strides of parts of one tensor [B, S, W, D], or [B, W, S, D] with heads before tokens, and the bytes from head to head."""
+    kw = dict(batch=W * S * D, token=W * D, head=D) if layout == "tokens" else dict(batch=W * S * D, token=D, head=S * D)
+    return kw, 4 * kw["head"]
+
+
+PARTS = [(S, B, H, Hkv, layout) for B, H, Hkv in ((1 << 22, 1 << 10, 1), (1 << 22, 1 << 10, 2), (1 << 24, 1, 1), (1 << 23, 2, 1), (1, 1 << 24, 1), (1, 1 << 24, 1 << 23))
+         for S in (1, 2) for layout in ("tokens", "heads") if not (layout == "tokens" and S > 1 and B == 1)]       # (token strides stay below 2^23 bytes)
+
+
+@pytest.mark.parametrize("S,B,H,Hkv,layout", PARTS)
+def test_attention_tells_parts_of_one_tensor_apart(S, B, H, Hkv, layout):
+    D, W = 16, H + 2 * Hkv
+    kw, step = places_in(layout, S, W, D)
+    part = lambda first: b._Heads(data=P + first * step, **kw)  # noqa: E731
+    h, hk = [b._Heads(data=P + (n + 1) * FAR, **kw) for n in range(3)], [b._Heads(data=P + (n + 20) * FAR, **kw) for n in range(2)]
+
+    def call(dq, dk, dv):
+        return lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], hk[0], hk[1], h[1], P, h[2], dq, dk, dv, P, 1 << 62, None)
+    assert call(part(0), part(H), part(H + Hkv)) == 2 and call(part(2 * Hkv), part(0), part(Hkv)) == 2 and call(part(Hkv), part(0), part(H + Hkv)) == 2
+    for dq, dk, dv in ((0, H - 1, H + Hkv), (0, H, H + Hkv - 1), (1, H, H + Hkv), (0, 0, H), (0, H, H)):
+        assert call(part(dq), part(dk), part(dv)) == 1, (dq, dk, dv)
+    # parts of it as inputs beside outputs in the others
+    assert lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], part(H), part(H + Hkv), part(0), P, P, 1 << 62, None) == 2
+    assert lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], part(H - 1), part(H + Hkv), part(0), P, P, 1 << 62, None) == 1
+
+
+def test_attention_tells_parts_along_tokens_and_batches_apart():
+    """dk and dv behind dq's tokens, with heads before tokens; other strides: by their extents."""
+    B, H, Hkv, S, Sk, D = 1 << 22, 1 << 10, 2, 2, 3, 16
+    T = S + 2 * Sk
+    kw = dict(batch=H * T * D, token=D, head=T * D)
+    h, hk = [b._Heads(data=P + (n + 1) * 4 * FAR, **kw) for n in range(3)], [b._Heads(data=P + (n + 10) * 4 * FAR, **kw) for n in range(2)]
+    part = lambda first, **other: b._Heads(data=P + first * D * 4, **dict(kw, **other))  # noqa: E731
+
+    def call(dq, dk, dv):
+        return lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=Sk, H=H, Hkv=Hkv)), h[0], hk[0], hk[1], h[1], P, h[2], dq, dk, dv, P, 1 << 62, None)
+    assert call(part(0), part(S), part(S + Sk)) == 2
+    assert call(part(0), part(S - 1), part(S + Sk)) == 1 and call(part(0), part(S), part(S + Sk - 1)) == 1
+    assert call(part(0), part(S), part(S + Sk, token=2 * D)) == 1          # (a stride unlike dq's, within its extent)
+
+
+@pytest.mark.parametrize("layout", ["tokens", "heads"])
+@pytest.mark.parametrize("H,Hkv", [(4, 1), (4, 2), (1, 4), (1, 1)])
+@pytest.mark.parametrize("B,S", [(2, 1 << 27), (1 << 27, 2), (1, 1 << 28), (1 << 28, 1)])
+def test_norm_rotary_tells_parts_of_one_tensor_apart(B, S, H, Hkv, layout):
+    D = 256
+    kw, step = places_in(layout, S, H + Hkv, D)
+    part = lambda first: b._Heads(data=P + first * step, **kw)  # noqa: E731
+    d = dict(ROT, B=B, S=S, H=H, Hkv=Hkv, D=D, sections=(2, 2, 0, 0))
+    shape = b._Rotary(d["dtype"], B, S, H, Hkv, D, d["axes"], (b.C.c_int32 * 4)(*d["sections"]), 0, 1, 1e-6)
+    q, k, far = part(0), part(H), [b._Heads(data=P + (n + 1) * 16 * FAR, **kw) for n in range(4)]
+    forward = lambda yq, yk: lib.dat_norm_rotary_forward(shape, q, k, P, P, P, P, yq, yk, None)  # noqa: E731
+    assert forward(q, k) == 2 and forward(q, far[0]) == 2 and forward(far[0], k) == 2 and forward(far[0], far[1]) == 2
+    assert forward(k, far[0]) == 1 and forward(far[0], q) == 1 and forward(far[0], far[0]) == 1
+    assert lib.dat_norm_rotary_backward(shape, far[0], far[1], P, P, P, P, far[2], far[3], q, k, P, P + 4096, P, 1 << 62, None) == 2
+    assert lib.dat_norm_rotary_backward(shape, far[0], far[1], P, P, P, P, far[2], far[3], k, k, P, P + 4096, P, 1 << 62, None) == 1
