@@ -839,7 +839,9 @@ def norm_rotary_backward(q, k, gamma_q, gamma_k, positions, frequencies, section
 
 
 class GradientTable:
-    """Gradient tensors (fp32 or bf16, contiguous, on one GPU, none on another) as clip_gradients takes them; keeps the memory alive that they have now."""
+    """Gradient tensors (fp32 or bf16, contiguous, on one GPU, none on another) as clip_gradients takes them; keeps the memory alive that they have now.
+    The table may be dropped while a call is under way, on any stream (the gradients themselves are the caller's, as any call's tensors), but has
+    to live as long as a captured graph of such a call."""
 
     def __init__(self, tensors):
         self.tensors = tensors = [t.detach() if isinstance(t, torch.Tensor) else t for t in tensors]
@@ -858,6 +860,7 @@ class GradientTable:
         self.pointers = torch.tensor([t.data_ptr() for t in tensors], dtype=torch.int64, device=device)
         self.types = torch.tensor([_code(t) for t in tensors], dtype=torch.uint8, device=device)
         self.offsets = torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), dtype=torch.int64, device=device)
+        self.stream = torch.cuda.current_stream(device).cuda_stream        # (what the three belong to)
 
 
 def gradient_table(tensors):
@@ -870,6 +873,9 @@ def clip_gradients(table, largest, norm=None, stream=None):
     largest = inf: the norm alone.  See dat_clip_gradients."""
     _want("norm", norm, (torch.float32,), (1,), optional=True)
     with _On(stream, table.pointers, norm) as st:
+        if st != table.stream:                     # (the addresses decide where the call writes: not to be handed out again before)
+            for t in (table.pointers, table.types, table.offsets):
+                t.record_stream(torch.cuda.current_stream(t.device))
         if norm is None:
             norm = torch.empty(1, device=table.pointers.device)
         size = int(_lib.dat_clip_gradients_workspace(len(table.tensors), table.total))

@@ -255,6 +255,29 @@ def test_gradient_table_keeps_its_memory(dat):
     assert bool((g == 1).all()) and bool((old == old[0]).all()) and abs(float(old[0]) - 1 / math.sqrt(1000.0)) < 1e-8
 
 
+def test_gradient_table_dropped_while_another_stream_uses_it(dat):
+    """A table made for one call on a side stream: its memory is not handed out again before that stream has passed the call."""
+    g, x = randn(1, 1000), randn(2, 8192, 8192)
+    before, side = g.clone(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(10):                       # several milliseconds each
+            x @ x
+    table = dat.gradient_table([g[:500], g[500:]])
+    sizes = [t.numel() * t.element_size() for t in (table.pointers, table.types, table.offsets)]
+    places = {t.data_ptr() for t in (table.pointers, table.types, table.offsets)}
+    norm = dat.clip_gradients(table, 1.0, stream=side)
+    del table
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    assert not side.query(), "the side stream has to be busy here"
+    assert not places & {t.data_ptr() for t in others}
+    torch.cuda.synchronize()
+    want = math.sqrt(float(before.double().square().sum()))
+    assert abs(float(norm) - want) < 1e-6 * want
+    assert_near(host(g), host(before) / want, 4 * U * np.abs(host(before)) / want, "g")
+
+
 def test_gradient_table_refuses(dat):
     g = randn(1, 100)
     for bad in ([], [g.cpu()], [g.half()], [g[::2]], [g, g], [g[:50], g[40:]], [g, None]):

@@ -231,6 +231,42 @@ def test_clip_gradients_binding_refuses():
             b.gradient_table(bad)
 
 
+class Place:
+    """A device tensor as clip_gradients looks at it, which notes the streams that it is recorded for."""
+
+    def __init__(self):
+        self.device, self.streams = torch.device("cpu"), []
+
+    def data_ptr(self):
+        return P
+
+    def record_stream(self, stream):
+        self.streams.append(stream)
+
+
+@pytest.mark.parametrize("made,used", [(7, 7), (7, 9), (0, 5), (5, 0)])
+def test_gradient_table_is_recorded_for_the_stream_it_is_used_on(monkeypatch, made, used):
+    """The table's memory goes back to the stream that it was made on, so every other one that reads it has to be known."""
+    table = b.GradientTable.__new__(b.GradientTable)
+    table.tensors, table.total, table.stream = [None], 100, made
+    table.pointers, table.types, table.offsets = places = Place(), Place(), Place()
+
+    class On:
+        def __init__(self, *args):
+            pass
+
+        def __enter__(self):
+            return used
+
+        def __exit__(self, *exc):
+            pass
+    monkeypatch.setattr(b, "_On", On)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "the stream")
+    monkeypatch.setattr(b._lib, "dat_clip_gradients", lambda *args: 0)
+    b.clip_gradients(table, 1.0, norm=torch.zeros(1))
+    assert all(p.streams == ([] if made == used else ["the stream"]) for p in places)
+
+
 def test_plain_clip():
     norm, out, c = pt.clip([np.array([3.0]), np.array([0.0, 4.0])], 2.5)
     assert norm == 5.0 and c == 0.5 and out[1][1] == 2.0 and pt.clip([np.array([3.0])], 3.0)[2] == 1.0
