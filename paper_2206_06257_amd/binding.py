@@ -504,7 +504,7 @@ def adamw_slots(d, num_tensors):
 def adamw_state(d, num_tensors, bits=32, device="cuda"):
     """Zero moments of `d` parameters in `num_tensors` tensors: (m, v, scales), scales None with 32 bits."""
     if bits == 32:
-        return torch.zeros(d, device=device), torch.zeros(d, device=device), None
+        return torch.zeros(d, dtype=torch.float32, device=device), torch.zeros(d, dtype=torch.float32, device=device), None
     if bits != 8:
         raise ValueError("moments have 8 or 32 bits, not %r" % (bits,))
     return (torch.zeros(d, dtype=torch.uint8, device=device), torch.zeros(d, dtype=torch.uint8, device=device),
@@ -549,7 +549,7 @@ def adamw_moments(m, v, scales, offsets_dev, stream=None):
     d = m.numel()
     ptr, T = _adamw_table(offsets_dev, d, m, v, scales)
     with _On(stream, m, v, scales, None if isinstance(offsets_dev, tuple) else offsets_dev) as st:
-        m_out, v_out = torch.empty(d, device=m.device), torch.empty(d, device=m.device)
+        m_out, v_out = torch.empty(d, dtype=torch.float32, device=m.device), torch.empty(d, dtype=torch.float32, device=m.device)
         _check(_lib.dat_adamw_moments(_at(m), _at(v), _at(scales), ptr, T, d, _at(m_out), _at(v_out), st), "dat_adamw_moments")
     return m_out, v_out
 
@@ -573,9 +573,9 @@ def log_probs(logits, labels=None, top=0, stream=None):
     _want("labels", labels, (torch.int32,), (N,), optional=True)
     with _On(stream, logits, labels) as st:
         device = logits.device
-        lse = torch.empty(N, device=device)
+        lse = torch.empty(N, dtype=torch.float32, device=device)
         entropy, logp = torch.empty_like(lse), None if labels is None else torch.empty_like(lse)
-        top_logp = torch.empty(N, top, device=device) if top > 0 else None
+        top_logp = torch.empty(N, top, dtype=torch.float32, device=device) if top > 0 else None
         top_index = torch.empty(N, top, dtype=torch.int32, device=device) if top > 0 else None
         size = int(_lib.dat_log_probs_workspace(N, V, top))
         ws = torch.empty(size, dtype=torch.uint8, device=device) if size else None
@@ -627,7 +627,7 @@ def group_norm_forward(x, gamma, beta, groups, act=ACT_NONE, eps=1e-5, y=None, s
     with _On(stream, x, gamma, beta, y) as st:
         if y is None:
             y = torch.empty_like(x)
-        mean = torch.empty(B, max(groups, 0), device=x.device)
+        mean = torch.empty(B, max(groups, 0), dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
         ws, size = _gn_workspace(0, x, groups)
         _check(_lib.dat_group_norm_forward(_at(x), _at(gamma), _at(beta), _code(x), B, H, W, Cc, groups, eps, act, _at(y), _at(mean),
@@ -650,8 +650,8 @@ def group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, act=ACT_NONE, dx
         _want(name, t, f32, (B, groups))
     with _On(stream, x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta) as st:
         dx = torch.empty_like(x) if dx is None else dx
-        dgamma = torch.empty(Cc, device=x.device) if dgamma is None else dgamma
-        dbeta = torch.empty(Cc, device=x.device) if dbeta is None else dbeta
+        dgamma = torch.empty(Cc, dtype=torch.float32, device=x.device) if dgamma is None else dgamma
+        dbeta = torch.empty(Cc, dtype=torch.float32, device=x.device) if dbeta is None else dbeta
         ws, size = _gn_workspace(1, x, groups)
         _check(_lib.dat_group_norm_backward(_at(x), _at(dy), _at(gamma), _at(beta), _at(mean), _at(rstd), _code(x), B, H, W, Cc, groups,
                                             act, _at(dx), _at(dgamma), _at(dbeta), _at(ws), size, st), "dat_group_norm_backward")
@@ -761,7 +761,7 @@ def attention_backward(q, k, v, o, lse, do, scale=None, window=(-1, -1), offsets
 
 def rotary_frequencies(sections, base=10000.0, device="cuda"):
     """fp32 [pairs]: base^(-i / n) for the i-th of an axis's n pairs, axis after axis."""
-    return torch.cat([base ** (-torch.arange(n, dtype=torch.float64) / n) for n in sections]).float().to(device) if sections else torch.empty(0, device=device)
+    return torch.cat([base ** (-torch.arange(n, dtype=torch.float64) / n) for n in sections]).float().to(device) if sections else torch.empty(0, dtype=torch.float32, device=device)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -829,7 +829,7 @@ def norm_rotary_backward(q, k, gamma_q, gamma_k, positions, frequencies, section
         _want(name, t, (torch.float32,), (D,), optional=True)
     with _On(stream, first, dyk, q, k, gamma_q, gamma_k, positions, frequencies, dq, dk, dgamma_q, dgamma_k) as st:
         dq, dk = (None if like is None else _like(like) if t is None else t for t, like in ((dq, dyq), (dk, dyk)))
-        dgamma_q, dgamma_k = (torch.empty(D, device=first.device) if t is None and norm and gamma is not None and like is not None else t
+        dgamma_q, dgamma_k = (torch.empty(D, dtype=torch.float32, device=first.device) if t is None and norm and gamma is not None and like is not None else t
                               for t, gamma, like in ((dgamma_q, gamma_q, dyq), (dgamma_k, gamma_k, dyk)))
         out = [None if t is None else _heads("dx", t, dtype, t.shape) for t in (dq, dk)]
         ws = torch.empty(size, dtype=torch.uint8, device=first.device) if size else None
@@ -877,7 +877,7 @@ def clip_gradients(table, largest, norm=None, stream=None):
             for t in (table.pointers, table.types, table.offsets):
                 t.record_stream(torch.cuda.current_stream(t.device))
         if norm is None:
-            norm = torch.empty(1, device=table.pointers.device)
+            norm = torch.empty(1, dtype=torch.float32, device=table.pointers.device)
         size = int(_lib.dat_clip_gradients_workspace(len(table.tensors), table.total))
         ws = torch.empty(size, dtype=torch.uint8, device=table.pointers.device)
         _check(_lib.dat_clip_gradients(_at(table.pointers), _at(table.types), _at(table.offsets), len(table.tensors), table.total, largest, _at(norm), _at(ws),
