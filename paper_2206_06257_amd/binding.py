@@ -3,6 +3,7 @@ methods of Model).  Raises if the library has not been built: there is no fallba
 import ctypes as C
 import functools
 import math
+import operator
 import os
 
 import numpy as np
@@ -611,7 +612,7 @@ def _gn_workspace_bytes(pass_, dtype, B, H, W, channels, groups):
 
 
 def _gn_workspace(pass_, x, groups):
-    size = _gn_workspace_bytes(pass_, _code(x), *x.shape, groups)
+    size = _gn_workspace_bytes(pass_, _code(x), *x.shape, operator.index(groups))       # (a tensor would be kept by its identity)
     return (torch.empty(size, dtype=torch.uint8, device=x.device) if size else None), size
 
 
@@ -710,8 +711,8 @@ def _attention(q, k, scale, window, offsets_q, offsets_k):
     if len(ks) != len(qs) or ks[-1] != qs[-1] or (batched and ks[0] != qs[0]):
         raise ValueError("k: %s does not go with q %s" % (tuple(ks), tuple(qs)))
     left, right = window
-    D = qs[-1]
-    sizes = (_code(q), qs[0] if batched else offsets_q.numel() - 1, qs[-3], ks[-3], qs[-2], ks[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else scale, left, right)
+    left, right, D = operator.index(left), operator.index(right), qs[-1]       # (numbers, not tensors: what is kept of a call goes by their values)
+    sizes = (_code(q), qs[0] if batched else offsets_q.numel() - 1, qs[-3], ks[-3], qs[-2], ks[-2], D, 1.0 / math.sqrt(max(D, 1)) if scale is None else float(scale), left, right)
     if batched:
         return _attention_shape(*sizes) + (True,)
     _want("offsets_q", offsets_q, (torch.int32,), contiguous=True)
@@ -787,14 +788,15 @@ def _rotary(first, second, gamma_q, gamma_k, positions, frequencies, sections, l
         raise ValueError("k: %s does not go with q %s" % (tuple(second.shape), tuple(size)))
     for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
         _want(name, t, (torch.float32,), (D,), optional=True)
-    sections = tuple(sections)
+    sections = tuple(map(operator.index, sections))
     if len(sections) > 4:
         raise ValueError("sections: at most 4 axes, got %r" % (sections,))
     pairs = sum(sections)
     _want("positions", positions, (torch.int32,), lead + (len(sections),), optional=pairs == 0)
     _want("frequencies", frequencies, (torch.float32,), (pairs,), optional=pairs == 0)
     B, S = lead if len(lead) == 2 else (1, lead[0])
-    return _rotary_shape(_code(one), B, S, 0 if first is None else first.shape[-2], 0 if second is None else second.shape[-2], D, sections, layout, int(bool(norm)), eps) + (one,)
+    return _rotary_shape(_code(one), B, S, 0 if first is None else first.shape[-2], 0 if second is None else second.shape[-2], D, sections, operator.index(layout),
+                         int(bool(norm)), float(eps)) + (one,)
 
 
 def norm_rotary_forward(q, k, gamma_q, gamma_k, positions, frequencies, sections, layout=ROTARY_HALVES, eps=1e-6, norm=True, yq=None, yk=None, stream=None):

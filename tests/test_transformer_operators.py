@@ -120,6 +120,37 @@ def test_attention_binding_refuses_sizes_beyond_its_types():
         b.norm_rotary_forward(q[:1].expand((1 << 32) + 1, *q.shape[1:]), None, None, None, None, None, [])
 
 
+def test_numbers_are_taken_by_value():
+    """A scale, a window or sections held in tensors that change: each call goes by what they hold then."""
+    q, k = torch.zeros(2, 5, 4, 16), torch.zeros(2, 7, 2, 16)
+    scale, side, layout = torch.tensor(0.5), torch.tensor(3), torch.tensor(0)
+    pos, f = torch.zeros(2, 5, 2, dtype=torch.int32), torch.zeros(8)
+    sections, eps = [torch.tensor(4), torch.tensor(4)], torch.tensor(0.5)
+    for s, n, e in ((0.5, 4, 0.5), (0.25, 2, 0.125), (2.0, 0, 1.0)):
+        scale.fill_(s), side.fill_(n), sections[0].fill_(n), eps.fill_(e), layout.fill_(n // 4)
+        shape = b._attention(q, k, scale, (side, side), None, None)[0]
+        assert (shape.scale, shape.left, shape.right) == (s, n, n)
+        for given in (sections, torch.stack(sections)):
+            shape = b._rotary(q, k[:, :5], None, None, pos, f[:n + 4], given, layout, eps, True)[0]
+            assert list(shape.sections) == [n, 4, 0, 0] and shape.eps == e and shape.layout == n // 4
+        with pytest.raises(ValueError, match="frequencies"):
+            b._rotary(q, k[:, :5], None, None, pos, f[:n + 3], sections, layout, eps, True)
+    for window in ((1.5, 0), (0, 1.0), ("1", 0)):
+        with pytest.raises((TypeError, ValueError)):
+            b._attention(q, k, None, window, None, None)
+    with pytest.raises((TypeError, ValueError)):
+        b._rotary(q, k[:, :5], None, None, pos, f[:8], [4.0, 4.0], 0, 1e-6, True)
+
+
+def test_group_norm_workspace_is_taken_by_value():
+    x, groups, size = torch.zeros(1, 7, 7, 64), torch.tensor(8), {}
+    for n in (8, 2, 64, 1):
+        groups.fill_(n)
+        size[n] = b._gn_workspace(1, x, groups)[1]
+        assert size[n] == int(b._lib.dat_group_norm_workspace(1, b.F32, *x.shape, n))
+    assert len(set(size.values())) > 1
+
+
 @pytest.mark.parametrize("window", [(-1, -1), (-1, 0), (2, 1)])
 @pytest.mark.parametrize("Lq,Lk", [(5, 7), (7, 4), (1, 1)])
 def test_plain_attention_gradient_against_differences(Lq, Lk, window):
