@@ -166,14 +166,16 @@ __device__ __forceinline__ u32x4 descriptor(const char* p) {      // (buffer_at'
 __device__ __forceinline__ uint32_t lds_at(const unsigned char* p) { return (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)p); }
 
 // Loads straight into LDS, lane l's bytes at `to` + l * BYTES.  Written as one asm statement because the compiler otherwise waits for all such
-// loads in flight before the next LDS read, the next tile's too; wait_tile() waits for them.  No register is written.  The wait states are
-// those that a descriptor just written by a vector instruction, and M0 (which nothing else here uses), need before they are used.
+// loads in flight before the next LDS read, the next tile's too; wait_tile() waits for them.  M0 (which the compiler reserves: no list of
+// overwritten registers holds it) is left as it was.  The instructions before the load give a descriptor just written by a vector instruction
+// the five wait states that it needs, and M0 the one.
 template <int BYTES> __device__ __forceinline__ void load_to_lds(const u32x4& d, uint32_t off, uint32_t to) {
   static_assert(BYTES == 4 || BYTES == 16, "one or four dwords a lane");
+  uint32_t m0;
   if constexpr (BYTES == 16)
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(d), "s"(to) : "memory");
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 2\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0" : "=&s"(m0) : "v"(off), "s"(d), "s"(to) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(d), "s"(to) : "memory");
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 2\n\tbuffer_load_dword %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0" : "=&s"(m0) : "v"(off), "s"(d), "s"(to) : "memory");
 }
 
 // ---- LDS tiles ---------------------------------------------------------------------------------------------------------------

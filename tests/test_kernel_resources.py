@@ -69,3 +69,19 @@ def test_convolution_kernels_load_from_global_memory(tmp_path):
                 assert "global_load" in body or "buffer_load" in body, name
                 assert "flat_load" not in body, name
     assert seen >= 40
+
+
+def test_inline_assembly_names_what_it_overwrites():
+    """Statements of the kernels' sources that load into LDS say so to the compiler; M0, which it reserves for itself, they leave as it was."""
+    csrc = os.path.join(os.path.dirname(LIB), "csrc")
+    seen = 0
+    for name in sorted(os.listdir(csrc)):
+        for text, tail in re.findall(r"asm\s+volatile\s*\(\s*((?:\"[^\"]*\"\s*)+)(.*?)\)\s*;", open(os.path.join(csrc, name)).read(), re.S):
+            clobbers = tail.rsplit(":", 1)[-1]
+            lines = [x for x in re.split(r"\\n|\\t", text.replace('"', "").strip()) if x]
+            if any("m0" in x for x in lines):
+                seen += 1
+                assert lines[0] == "s_mov_b32 %0, m0" and lines[-1] == "s_mov_b32 m0, %0" and '"=&s"' in tail, (name, text)
+            if re.search(r"\blds\b|s_waitcnt|s_barrier", text):
+                assert '"memory"' in clobbers, (name, text)
+    assert seen >= 2
