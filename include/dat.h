@@ -351,7 +351,7 @@ dat_status dat_group_norm_backward(const void* x, const void* dy, const float* g
  * does not see does not enter it, whatever it holds; where it sees a value that is not finite, elements of its result may be NaN where
  * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row
  * NaN), and so do v times 256 keys (o is divided by its probabilities' sum at the end).
- * Outputs overlap neither inputs nor each other (parts of one tensor between each other are fine).  workspace: device, 16-byte aligned,
+ * Outputs, lse among them, overlap neither inputs nor each other (parts of one tensor, with the same strides, are fine between each other).  workspace: device, 16-byte aligned,
  * dat_attention_workspace(pass, shape) bytes (pass 0 forward, 1 backward; may be 0, then NULL is allowed); nothing in it outlives the
  * call.  Asynchronous on `stream`, no allocation.
  * DAT_ERR_ARG: null or misaligned pointers, negative sizes, H no multiple of Hkv, outputs that overlap (above) or whose strides lay
@@ -385,8 +385,8 @@ dat_status dat_attention_backward(const dat_attention* shape, const dat_heads* q
  *   backward: dn = dy turned back, h = dn gamma, xhat = x r; dx = r (h - xhat mean(h xhat)) (norm = 0: dx = dn, q and k are not read and may be NULL);
  *   dgamma_q, dgamma_k (device fp32 [D], either may be NULL; written, not added to): sums of dn xhat over tokens and heads, in a fixed
  *   order; norm = 0 leaves them as they were.
- * yq may be q and yk may be k (same strides); dq may be q or dyq, dk k or dyk; buffers that share elements otherwise are refused.  A
- * head of zeros with eps = 0 becomes NaN; a NaN or an infinity spoils its head (and the scales' gradients).
+ * yq may be q and yk may be k (same strides); dq may be q or dyq, dk k or dyk, and dgamma_q and dgamma_k may be the scales; outputs that share
+ * elements with anything otherwise are refused.  A head of zeros with eps = 0 becomes NaN; a NaN or an infinity spoils its head (and the scales' gradients).
  * workspace: device, 16-byte aligned, dat_norm_rotary_workspace(pass, shape) bytes (pass 0 forward, 1 backward; may be 0, then NULL is
  * allowed); nothing in it outlives the call.  Asynchronous on `stream`, no allocation.  B or S = 0: no output but dgamma = 0.
  * DAT_ERR_ARG: null or misaligned pointers, negative sizes, no head at all, more than 4 axes, more pairs than D / 2, unknown dtype or layout, norm

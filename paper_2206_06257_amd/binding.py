@@ -1,5 +1,6 @@
 """ctypes binding of libdat.so with the same names as include/dat.h (without the dat_ prefix on
 methods of Model).  Raises if the library has not been built: there is no fallback path."""
+import bisect
 import ctypes as C
 import functools
 import math
@@ -857,12 +858,18 @@ class GradientTable:
         for (_, end, a), (start, _, c) in zip(places, places[1:]):
             if start < end:
                 raise ValueError("tensors %d and %d share elements" % (a, c))
+        self.places = [(start, end) for start, end, _ in places]
         device, sizes = tensors[0].device, [t.numel() for t in tensors]
         self.total = sum(sizes)
         self.pointers = torch.tensor([t.data_ptr() for t in tensors], dtype=torch.int64, device=device)
         self.types = torch.tensor([_code(t) for t in tensors], dtype=torch.uint8, device=device)
         self.offsets = torch.tensor(np.concatenate([[0], np.cumsum(sizes)]), dtype=torch.int64, device=device)
         self.stream = torch.cuda.current_stream(device).cuda_stream        # (what the three belong to)
+
+    def holds(self, address, size):
+        """Whether some of these bytes are in one of the tensors."""
+        at = bisect.bisect_left(self.places, (address + size,)) - 1        # the last one that starts before their end
+        return at >= 0 and self.places[at][1] > address
 
 
 def gradient_table(tensors):
@@ -874,6 +881,8 @@ def clip_gradients(table, largest, norm=None, stream=None):
     """norm = sqrt(sum of all squares) of the table's tensors (fp32 [1]); where it is above `largest` they are scaled down to it, in place.
     largest = inf: the norm alone.  See dat_clip_gradients."""
     _want("norm", norm, (torch.float32,), (1,), optional=True)
+    if norm is not None and table.holds(norm.data_ptr(), 4):
+        raise ValueError("norm: it lies among the table's gradients")
     with _On(stream, table.pointers, norm) as st:
         if st != table.stream:                     # (the addresses decide where the call writes: not to be handed out again before)
             for t in (table.pointers, table.types, table.offsets):

@@ -70,6 +70,18 @@ inline bool heads_overlap(const dat_heads& x, const HeadsShape& sx, const dat_he
   return alike ? nested_overlap(gap / (int64_t)width, dims, 3, sx.D) : true;
 }
 
+// A block of memory beside tensors of heads (rows' statistics, scales, positions).
+struct Block { const void* data; uint64_t bytes; };
+inline bool blocks_overlap(const Block& x, const Block& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.data), b = reinterpret_cast<uintptr_t>(y.data);
+  return x.data && y.data && x.bytes && y.bytes && a < b + y.bytes && b < a + x.bytes;
+}
+// What a tensor reaches over, from its first element to behind its last.
+inline Block heads_block(const dat_heads* t, const HeadsShape& s, size_t width) {
+  if (!t || s.batch * s.tokens * s.heads == 0) return Block{nullptr, 0};
+  return Block{t->data, (uint64_t)heads_extent(*t, s) * width};
+}
+
 // Alignment of 16-byte vectors; strides at least 0 (that of a dimension of one is not looked at).
 inline bool heads_vectors(const dat_heads& t, const HeadsShape& s, size_t width) {
   const int64_t v = 16 / (int64_t)width;

@@ -497,6 +497,21 @@ dat_status take_all(std::initializer_list<Tensor> in, std::initializer_list<Tens
   }
   return DAT_OK;
 }
+// The blocks that a call reads lie in no output; those that it writes (the scales' gradients, when all else has been read and written) lie in no
+// tensor and not on each other.
+bool blocks_apart(std::initializer_list<Tensor> in, std::initializer_list<Tensor> out, std::initializer_list<Block> read, std::initializer_list<Block> written, size_t width) {
+  for (const Tensor& x : out)
+    for (const Block& y : read) if (blocks_overlap(heads_block(x.t, x.s, width), y)) return false;
+  for (auto* list : {&in, &out})
+    for (const Tensor& x : *list)
+      for (const Block& y : written) if (blocks_overlap(heads_block(x.t, x.s, width), y)) return false;
+  for (const Block& x : written)
+    for (const Block& y : written) if (&x < &y && blocks_overlap(x, y)) return false;
+  return true;
+}
+Block scale_block(const RotArgs& a, const float* gamma) { return Block{gamma, a.norm ? (uint64_t)a.D * 4 : 0}; }
+Block positions_block(const RotArgs& a, const int32_t* positions) { return Block{positions, a.pairs ? (uint64_t)a.T * a.axes * 4 : 0}; }
+Block frequencies_block(const RotArgs& a, const float* frequencies) { return Block{frequencies, (uint64_t)a.pairs * 4}; }
 
 }  // namespace
 }  // namespace dat
@@ -509,9 +524,12 @@ extern "C" dat_status dat_norm_rotary_forward(const dat_rotary* shape, const dat
   dat_status st;
   if (!fill(shape, a, st)) return st;
   const HeadsShape sq{shape->B, shape->S, shape->H, shape->D}, sk{shape->B, shape->S, shape->Hkv, shape->D};
-  st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}}, {{yq, sq, &a.yq, true}, {yk, sk, &a.yk, true}}, shape->dtype == DAT_BF16 ? 2 : 4);
+  const size_t width = shape->dtype == DAT_BF16 ? 2 : 4;
+  st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}}, {{yq, sq, &a.yq, true}, {yk, sk, &a.yk, true}}, width);
   if (st != DAT_OK) return st;
   if (a.T == 0) return DAT_OK;
+  if (!blocks_apart({}, {{yq, sq, &a.yq, true}, {yk, sk, &a.yk, true}},
+                    {scale_block(a, gamma_q), scale_block(a, gamma_k), positions_block(a, positions), frequencies_block(a, frequencies)}, {}, width)) return DAT_ERR_ARG;
   if (!aligned(gamma_q, 4) || !aligned(gamma_k, 4) || !aligned(positions, 4) || !aligned(frequencies, 4) || (a.pairs > 0 && (!positions || !frequencies))) return DAT_ERR_ARG;
   a.gamma_q = gamma_q; a.gamma_k = gamma_k; a.positions = positions; a.frequencies = frequencies;
   arrange(*shape, a);
@@ -541,6 +559,10 @@ extern "C" dat_status dat_norm_rotary_backward(const dat_rotary* shape, const da
   if (st != DAT_OK) return st;
   if (!aligned(gamma_q, 4) || !aligned(gamma_k, 4) || !aligned(positions, 4) || !aligned(frequencies, 4) || !aligned(dgamma_q, 4) || !aligned(dgamma_k, 4)) return DAT_ERR_ARG;
   if (a.T > 0 && a.pairs > 0 && (!positions || !frequencies)) return DAT_ERR_ARG;
+  if (!blocks_apart({{q, a.norm ? sq : HeadsShape{}, &a.q, false}, {k, a.norm ? sk : HeadsShape{}, &a.k, false}, {dyq, sq, &a.yq, false}, {dyk, sk, &a.yk, false}},
+                    {{dq, sq, &a.dq, true}, {dk, sk, &a.dk, true}},
+                    {scale_block(a, gamma_q), scale_block(a, gamma_k), positions_block(a, positions), frequencies_block(a, frequencies)},
+                    {scale_block(a, dgamma_q), scale_block(a, dgamma_k)}, width)) return DAT_ERR_ARG;
   const bool sums = a.norm && (dgamma_q || dgamma_k);
   if (a.norm && a.T > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < dat_norm_rotary_workspace(1, shape))) return DAT_ERR_ARG;
   a.gamma_q = gamma_q; a.gamma_k = gamma_k; a.positions = positions; a.frequencies = frequencies;

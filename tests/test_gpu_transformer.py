@@ -278,6 +278,17 @@ def test_gradient_table_dropped_while_another_stream_uses_it(dat):
     assert_near(host(g), host(before) / want, 4 * U * np.abs(host(before)) / want, "g")
 
 
+def test_clip_refuses_a_norm_among_the_gradients(dat):
+    g = randn(1, 100)
+    before, table = g.clone(), dat.gradient_table([g[:50], g[:0], g[60:]])
+    for at in (0, 49, 60, 99):
+        with pytest.raises(ValueError, match="norm"):
+            dat.clip_gradients(table, 1.0, norm=g[at:at + 1])
+    assert torch.equal(g, before)
+    dat.clip_gradients(table, math.inf, norm=g[55:56])
+    assert abs(float(g[55]) - math.sqrt(float(torch.cat([before[:50], before[60:]]).double().square().sum()))) < 1e-5
+
+
 def test_gradient_table_refuses(dat):
     g = randn(1, 100)
     for bad in ([], [g.cpu()], [g.half()], [g[::2]], [g, g], [g[:50], g[40:]], [g, None]):

@@ -279,7 +279,7 @@ class Place:
 def test_gradient_table_is_recorded_for_the_stream_it_is_used_on(monkeypatch, made, used):
     """The table's memory goes back to the stream that it was made on, so every other one that reads it has to be known."""
     table = b.GradientTable.__new__(b.GradientTable)
-    table.tensors, table.total, table.stream = [None], 100, made
+    table.tensors, table.total, table.stream, table.places = [None], 100, made, []
     table.pointers, table.types, table.offsets = places = Place(), Place(), Place()
 
     class On:
@@ -310,6 +310,7 @@ def places_in(layout, S, W, D):
     return kw, 4 * kw["head"]
 
 
+A = 1 << 46       # an address that nothing else has
 PARTS = [(S, B, H, Hkv, layout) for B, H, Hkv in ((1 << 22, 1 << 10, 1), (1 << 22, 1 << 10, 2), (1 << 24, 1, 1), (1 << 23, 2, 1), (1, 1 << 24, 1), (1, 1 << 24, 1 << 23))
          for S in (1, 2) for layout in ("tokens", "heads") if not (layout == "tokens" and S > 1 and B == 1)]       # (token strides stay below 2^23 bytes)
 
@@ -322,13 +323,13 @@ def test_attention_tells_parts_of_one_tensor_apart(S, B, H, Hkv, layout):
     h, hk = [b._Heads(data=P + (n + 1) * FAR, **kw) for n in range(3)], [b._Heads(data=P + (n + 20) * FAR, **kw) for n in range(2)]
 
     def call(dq, dk, dv):
-        return lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], hk[0], hk[1], h[1], P, h[2], dq, dk, dv, P, 1 << 62, None)
+        return lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], hk[0], hk[1], h[1], A, h[2], dq, dk, dv, P, 1 << 62, None)
     assert call(part(0), part(H), part(H + Hkv)) == 2 and call(part(2 * Hkv), part(0), part(Hkv)) == 2 and call(part(Hkv), part(0), part(H + Hkv)) == 2
     for dq, dk, dv in ((0, H - 1, H + Hkv), (0, H, H + Hkv - 1), (1, H, H + Hkv), (0, 0, H), (0, H, H)):
         assert call(part(dq), part(dk), part(dv)) == 1, (dq, dk, dv)
     # parts of it as inputs beside outputs in the others
-    assert lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], part(H), part(H + Hkv), part(0), P, P, 1 << 62, None) == 2
-    assert lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], part(H - 1), part(H + Hkv), part(0), P, P, 1 << 62, None) == 1
+    assert lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], part(H), part(H + Hkv), part(0), A, P, 1 << 62, None) == 2
+    assert lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), h[0], part(H - 1), part(H + Hkv), part(0), A, P, 1 << 62, None) == 1
 
 
 def test_attention_tells_parts_along_tokens_and_batches_apart():
@@ -340,7 +341,7 @@ def test_attention_tells_parts_along_tokens_and_batches_apart():
     part = lambda first, **other: b._Heads(data=P + first * D * 4, **dict(kw, **other))  # noqa: E731
 
     def call(dq, dk, dv):
-        return lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=Sk, H=H, Hkv=Hkv)), h[0], hk[0], hk[1], h[1], P, h[2], dq, dk, dv, P, 1 << 62, None)
+        return lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=Sk, H=H, Hkv=Hkv)), h[0], hk[0], hk[1], h[1], A, h[2], dq, dk, dv, P, 1 << 62, None)
     assert call(part(0), part(S), part(S + Sk)) == 2
     assert call(part(0), part(S - 1), part(S + Sk)) == 1 and call(part(0), part(S), part(S + Sk - 1)) == 1
     assert call(part(0), part(S), part(S + Sk, token=2 * D)) == 1          # (a stride unlike dq's, within its extent)
@@ -356,8 +357,79 @@ def test_norm_rotary_tells_parts_of_one_tensor_apart(B, S, H, Hkv, layout):
     d = dict(ROT, B=B, S=S, H=H, Hkv=Hkv, D=D, sections=(2, 2, 0, 0))
     shape = b._Rotary(d["dtype"], B, S, H, Hkv, D, d["axes"], (b.C.c_int32 * 4)(*d["sections"]), 0, 1, 1e-6)
     q, k, far = part(0), part(H), [b._Heads(data=P + (n + 1) * 16 * FAR, **kw) for n in range(4)]
-    forward = lambda yq, yk: lib.dat_norm_rotary_forward(shape, q, k, P, P, P, P, yq, yk, None)  # noqa: E731
+    forward = lambda yq, yk: lib.dat_norm_rotary_forward(shape, q, k, A, A, A, A, yq, yk, None)  # noqa: E731
     assert forward(q, k) == 2 and forward(q, far[0]) == 2 and forward(far[0], k) == 2 and forward(far[0], far[1]) == 2
     assert forward(k, far[0]) == 1 and forward(far[0], q) == 1 and forward(far[0], far[0]) == 1
-    assert lib.dat_norm_rotary_backward(shape, far[0], far[1], P, P, P, P, far[2], far[3], q, k, P, P + 4096, P, 1 << 62, None) == 2
-    assert lib.dat_norm_rotary_backward(shape, far[0], far[1], P, P, P, P, far[2], far[3], k, k, P, P + 4096, P, 1 << 62, None) == 1
+    assert lib.dat_norm_rotary_backward(shape, far[0], far[1], A, A, A, A, far[2], far[3], q, k, A, A + 4096, P, 1 << 62, None) == 2
+    assert lib.dat_norm_rotary_backward(shape, far[0], far[1], A, A, A, A, far[2], far[3], k, k, A, A + 4096, P, 1 << 62, None) == 1
+
+
+# ---- buffers beside the tensors of heads ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "o"])
+def test_attention_forward_refuses_lse_over_a_tensor(name):
+    B, H, Hkv, S, D = 1 << 22, 1 << 10, 2, 2, 16
+    sizes = dict(q=H, k=Hkv, v=Hkv, o=H)
+    t = {n: b._Heads(data=P + i * 4 * FAR, batch=S * h * D, token=h * D, head=D) for i, (n, h) in enumerate(sizes.items())}
+    call = lambda lse: lib.dat_attention_forward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), *t.values(), lse, P, 1 << 62, None)  # noqa: E731
+    first, bytes_, lse = t[name].data, 4 * B * S * sizes[name] * D, 4 * B * H * S
+    assert call(A) == 2 and call(first + bytes_) == 2 and call(first + bytes_ - 4) == 1 and call(first) == 1
+    assert call(first - lse + 4) == 1 if first > lse else True
+
+
+@pytest.mark.parametrize("name", ["dq", "dk", "dv"])
+def test_attention_backward_refuses_gradients_over_lse(name):
+    B, H, Hkv, S, D = 1 << 22, 1 << 10, 2, 2, 16
+    sizes = dict(q=H, k=Hkv, v=Hkv, o=H, do=H, dq=H, dk=Hkv, dv=Hkv)
+    t = {n: b._Heads(data=P + i * 4 * FAR, batch=S * h * D, token=h * D, head=D) for i, (n, h) in enumerate(sizes.items())}
+    x = list(t.values())
+    call = lambda lse: lib.dat_attention_backward(b._Attention(**dict(BASE, B=B, Sq=S, Sk=S, H=H, Hkv=Hkv)), *x[:4], lse, *x[4:], P, 1 << 62, None)  # noqa: E731
+    first, bytes_, lse = t[name].data, 4 * B * S * sizes[name] * D, 4 * B * H * S
+    assert call(A) == 2 and call(first + bytes_) == 2 and call(first - lse) == 2
+    assert call(first + bytes_ - 4) == 1 and call(first) == 1 and call(first - lse + 4) == 1
+    assert call(t["q"].data) == 2 and call(t["o"].data) == 2                 # (both are read)
+
+
+def test_norm_rotary_refuses_outputs_over_what_it_reads_or_writes_beside_them():
+    """Scales' gradients that share elements with each other or with a tensor; outputs over scales, positions or frequencies."""
+    B, S, H, Hkv, D, axes, pairs = 2, 1 << 27, 4, 2, 256, 2, 4
+    d = dict(ROT, B=B, S=S, H=H, Hkv=Hkv, D=D, sections=(2, 2, 0, 0))
+    shape = b._Rotary(d["dtype"], B, S, H, Hkv, D, axes, (b.C.c_int32 * 4)(*d["sections"]), 0, 1, 1e-6)
+    sizes = dict(q=H, k=Hkv, yq=H, yk=Hkv, dq=H, dk=Hkv)
+    t = {n: b._Heads(data=P + i * 4 * FAR, batch=S * h * D, token=h * D, head=D) for i, (n, h) in enumerate(sizes.items())}
+    end = {n: t[n].data + 4 * B * S * h * D for n, h in sizes.items()}
+    small = dict(gq=A, gk=A + 4096, positions=A + 8192, freq=A + 4096 + 16 * B * S)
+    more = dict(dgq=A + (1 << 40), dgk=A + (1 << 40) + 4 * D)
+
+    def forward(**kw):
+        s = dict(small, **kw)
+        return lib.dat_norm_rotary_forward(shape, t["q"], t["k"], s["gq"], s["gk"], s["positions"], s["freq"], t["yq"], t["yk"], None)
+
+    def backward(norm=1, **kw):
+        s = dict(small, **more, **{})
+        s.update(kw)
+        sh = b._Rotary(d["dtype"], B, S, H, Hkv, D, axes, (b.C.c_int32 * 4)(*d["sections"]), 0, norm, 1e-6)
+        return lib.dat_norm_rotary_backward(sh, t["q"], t["k"], s["gq"], s["gk"], s["positions"], s["freq"], t["yq"], t["yk"], t["dq"], t["dk"], s["dgq"], s["dgk"],
+                                            P, 1 << 62, None)
+    assert forward() == 2 and forward(gq=t["q"].data) == 2 and forward(gq=A, gk=A) == 2 and forward(gq=None, gk=None) == 2
+    assert backward() == 2 and backward(dgq=None) == 2 and backward(dgk=None) == 2 and backward(dgq=A, dgk=A + 4 * D) == 2     # (a scale's gradient over the scale)
+    for name, bytes_ in (("gq", 4 * D), ("gk", 4 * D), ("positions", 4 * B * S * axes), ("freq", 4 * pairs)):
+        for out in ("yq", "yk"):
+            assert forward(**{name: end[out] - 4}) == 1 and forward(**{name: end[out]}) == 2
+            assert forward(**{name: t[out].data - bytes_ + 4}) == 1 or t[out].data < bytes_
+        for out in ("dq", "dk"):
+            assert backward(**{name: end[out] - 4}) == 1 and backward(**{name: end[out]}) == 2
+    for name in ("dgq", "dgk"):
+        for over in t:
+            assert backward(**{name: t[over].data}) == 1 and backward(**{name: end[over] - 4}) == 1 and backward(**{name: end[over]}) == 2, (name, over)
+    assert backward(dgq=more["dgk"]) == 1 and backward(dgq=more["dgk"] + 4 * D - 4) == 1 and backward(dgq=more["dgk"] - 4 * D + 4) == 1
+    assert backward(norm=0, dgq=more["dgk"]) == 2                             # (not written)
+
+
+def test_gradient_table_knows_what_it_holds():
+    table = b.GradientTable.__new__(b.GradientTable)
+    table.places = [(100, 140), (200, 204), (204, 300)]
+    for at, held in ((90, False), (96, False), (98, True), (100, True), (136, True), (140, False), (196, False), (200, True), (296, True), (300, False), (1 << 40, False)):
+        assert table.holds(at, 4) is held, at
+    table.places = []
+    assert table.holds(5, 4) is False
