@@ -1062,8 +1062,8 @@ dat_status take(const dat_heads* t, const HeadsShape& s, size_t width, bool outp
 struct Tensor { const dat_heads* t; HeadsShape s; HeadsArg* to; bool output; };
 enum { kStatsRead, kStatsWritten };
 
-// The tensors, and the rows' statistics that a call reads or writes (fp32, none where there are no rows).
-dat_status take_all(std::initializer_list<Tensor> list, size_t width, const float* lse, int64_t rows, int stats) {
+// The tensors, and beside them the rows' statistics that a call reads or writes (fp32, none where there are no rows) and the offsets.
+dat_status take_all(std::initializer_list<Tensor> list, size_t width, const AttnArgs& a, const float* lse, int stats) {
   for (const Tensor& x : list) {
     const dat_status st = take(x.t, x.s, width, x.output, *x.to);
     if (st != DAT_OK) return st;
@@ -1071,8 +1071,13 @@ dat_status take_all(std::initializer_list<Tensor> list, size_t width, const floa
   for (const Tensor& x : list)
     if (x.output)
       for (const Tensor& y : list) if (&x != &y && heads_overlap(*x.t, x.s, *y.t, y.s, width)) return DAT_ERR_ARG;
-  for (const Tensor& x : list)
-    if ((x.output || stats == kStatsWritten) && blocks_overlap(heads_block(x.t, x.s, width), Block{lse, (uint64_t)rows * 4})) return DAT_ERR_ARG;
+  const Block rows{lse, a.B > 0 ? (uint64_t)a.rows * 4 : 0}, offsets_q{a.off_q, (uint64_t)a.B * 4 + 4}, offsets_k{a.off_k, (uint64_t)a.B * 4 + 4};
+  for (const Tensor& x : list) {
+    const Block block = heads_block(x.t, x.s, width);
+    if ((x.output || stats == kStatsWritten) && blocks_overlap(block, rows)) return DAT_ERR_ARG;
+    if (x.output && (blocks_overlap(block, offsets_q) || blocks_overlap(block, offsets_k))) return DAT_ERR_ARG;
+  }
+  if (stats == kStatsWritten && (blocks_overlap(rows, offsets_q) || blocks_overlap(rows, offsets_k))) return DAT_ERR_ARG;
   return DAT_OK;
 }
 
@@ -1099,7 +1104,7 @@ extern "C" dat_status dat_attention_forward(const dat_attention* shape, const da
   const int64_t B = a.off_q ? (a.B > 0) : a.B;
   const HeadsShape sq{B, a.Sq, a.H, a.D}, sk{B, a.Sk, a.Hkv, a.D};
   const size_t width = shape->dtype == DAT_BF16 ? 2 : 4;
-  st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, true}}, width, lse, a.rows, kStatsWritten);
+  st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, true}}, width, a, lse, kStatsWritten);
   if (st != DAT_OK) return st;
   if (B == 0 || a.Sq == 0) return DAT_OK;
   if (!lse || !aligned(lse, 4)) return DAT_ERR_ARG;
@@ -1121,7 +1126,7 @@ extern "C" dat_status dat_attention_backward(const dat_attention* shape, const d
   const HeadsShape sq{B, a.Sq, a.H, a.D}, sk{B, a.Sk, a.Hkv, a.D};
   const size_t width = shape->dtype == DAT_BF16 ? 2 : 4;
   st = take_all({{q, sq, &a.q, false}, {k, sk, &a.k, false}, {v, sk, &a.v, false}, {o, sq, &a.o, false}, {d_o, sq, &a.d_o, false},
-                 {dq, sq, &a.dq, true}, {dk, sk, &a.dk, true}, {dv, sk, &a.dv, true}}, width, lse, a.rows, kStatsRead);
+                 {dq, sq, &a.dq, true}, {dk, sk, &a.dk, true}, {dv, sk, &a.dv, true}}, width, a, lse, kStatsRead);
   if (st != DAT_OK) return st;
   if (B == 0) return DAT_OK;
   if (a.Sq > 0 && (!lse || !aligned(lse, 4))) return DAT_ERR_ARG;

@@ -433,3 +433,26 @@ def test_gradient_table_knows_what_it_holds():
         assert table.holds(at, 4) is held, at
     table.places = []
     assert table.holds(5, 4) is False
+
+
+def test_attention_refuses_outputs_over_offsets():
+    """Packed sequences: more heads than a launch takes, so that what is allowed is refused for that."""
+    T, H, Hkv, D, B = 64, 1 << 24, 2, 8, 5
+    sizes = dict(q=H, k=Hkv, v=Hkv, o=H, do=H, dq=H, dk=Hkv, dv=Hkv)
+    t = {n: b._Heads(data=P + i * FAR, batch=0, token=D, head=T * D) for i, n in enumerate(sizes)}
+    x, end = list(t.values()), {n: t[n].data + 4 * T * D * h for n, h in sizes.items()}
+
+    def call(backward, lse=A, **offsets):
+        shape = b._Attention(**dict(BASE, B=B, Sq=T, Sk=T, H=H, Hkv=Hkv, D=D, **dict(dict(offsets_q=A + FAR, offsets_k=A + FAR + 64), **offsets)))
+        if backward:
+            return lib.dat_attention_backward(shape, *x[:4], lse, *x[4:], P, 1 << 62, None)
+        return lib.dat_attention_forward(shape, *x[:4], lse, P, 1 << 62, None)
+    for name in ("offsets_q", "offsets_k"):
+        for backward, outs, ins in ((False, ("o",), ("q", "k", "v")), (True, ("dq", "dk", "dv"), ("q", "k", "v", "o", "do"))):
+            assert call(backward) == 2
+            for n in outs:
+                assert call(backward, **{name: end[n] - 4}) == 1 and call(backward, **{name: end[n]}) == 2
+                assert call(backward, **{name: t[n].data - 4 * B}) == 1 and call(backward, **{name: t[n].data - 4 * B - 4}) == 2
+            for n in ins:
+                assert call(backward, **{name: t[n].data}) == 2
+        assert call(False, lse=A + FAR - 4 * T * H) == 2 and call(False, lse=A + FAR - 4 * T * H + 4) == 1 and call(True, lse=A + FAR) == 2
