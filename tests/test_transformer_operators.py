@@ -456,3 +456,101 @@ def test_attention_refuses_outputs_over_offsets():
             for n in ins:
                 assert call(backward, **{name: t[n].data}) == 2
         assert call(False, lse=A + FAR - 4 * T * H) == 2 and call(False, lse=A + FAR - 4 * T * H + 4) == 1 and call(True, lse=A + FAR) == 2
+
+
+# ---- what the binding refuses, by the text it says; the first of each list has nothing to refuse but that its tensors are on the CPU ----------
+def refused(call, text):
+    with pytest.raises(ValueError, match=text):
+        call()
+
+
+Q, K, OFF, LSE = torch.zeros(2, 5, 4, 16), torch.zeros(2, 7, 2, 16), torch.zeros(3, dtype=torch.int32), torch.zeros(2, 4, 5)
+PQ, PK, PLSE = Q.flatten(0, 1), K.flatten(0, 1), torch.zeros(4, 10)            # packed
+APART = torch.zeros(2, 5, 4, 32)[..., ::2]                                       # elements of a head apart
+ON_CPU = "belong on a GPU"
+
+
+@pytest.mark.parametrize("text,args,kw", [
+    (ON_CPU, (Q, K, K), {}), (ON_CPU, (Q, K, K), dict(o=Q)), (ON_CPU, (Q, K[:, :0], K[:, :0]), {}), (ON_CPU, (PQ, PK, PK), dict(offsets_q=OFF, offsets_k=OFF)),
+    ("^q: torch.float16", (Q.half(), K, K), {}), ("^q: torch.float64", (Q.double(), K.double(), K.double()), {}), ("^k: torch.bfloat16", (Q, K.bfloat16(), K), {}),
+    ("^v: torch.bfloat16", (Q, K, K.bfloat16()), {}), ("^v: .*expected", (Q, K, K[:, :6]), {}), ("^v: .*expected", (Q, K, K[:, :, :1]), {}), ("^v: .*expected", (Q, K, K[..., :8]), {}),
+    ("^v: .*expected", (Q, K, K[:1]), {}), ("^q: expected .B, S, H, D.", (PQ, K, K), {}), ("^q: expected .T, H, D.", (Q, K, K), dict(offsets_q=OFF, offsets_k=OFF)),
+    ("^k: .*does not go with", (Q, PK, PK), {}), ("^k: .*does not go with", (Q, K[:1], K[:1]), {}), ("^k: .*does not go with", (Q, K[..., :8], K[..., :8]), {}),
+    ("^q: the elements", (APART, K, K), {}), ("^k: the elements", (Q, APART, APART), {}), ("^v: the elements", (Q, Q, APART), {}), ("^o: the elements", (Q, K, K), dict(o=APART)),
+    ("^o: .*expected", (Q, K, K), dict(o=Q[:, :4])), ("^o: torch.bfloat16", (Q, K, K), dict(o=Q.bfloat16())), ("^v: needed", (Q, K, None), {}),
+    ("^offsets_q and offsets_k", (Q, K, K), dict(offsets_q=OFF)), ("^offsets_q and offsets_k", (Q, K, K), dict(offsets_k=OFF)),
+    ("^offsets_q: torch.int64", (PQ, PK, PK), dict(offsets_q=OFF.long(), offsets_k=OFF)), ("^offsets_k: torch.int64", (PQ, PK, PK), dict(offsets_q=OFF, offsets_k=OFF.long())),
+    ("^offsets_k: .*expected", (PQ, PK, PK), dict(offsets_q=OFF, offsets_k=OFF[:2])), ("^offsets_q: .*not contiguous", (PQ, PK, PK), dict(offsets_q=torch.zeros(6, dtype=torch.int32)[::2], offsets_k=OFF)),
+    ("^offsets_k: .*not contiguous", (PQ, PK, PK), dict(offsets_q=OFF, offsets_k=torch.zeros(6, dtype=torch.int32)[::2])),
+    ("^offsets_q: expected .B . 1.", (PQ, PK, PK), dict(offsets_q=OFF[:0], offsets_k=OFF[:0])), ("^offsets_q: expected .B . 1.", (PQ, PK, PK), dict(offsets_q=OFF.view(1, 3), offsets_k=OFF.view(1, 3))),
+    ("^window: ", (Q, K, K), dict(window=(-2, 0))), ("^window: ", (Q, K, K), dict(window=(-1, -2)))])
+def test_attention_forward_binding_says_what_it_refuses(text, args, kw):
+    refused(lambda: b.attention_forward(*args, **kw), text)
+
+
+@pytest.mark.parametrize("text,args,kw", [
+    (ON_CPU, (Q, K, K, Q, LSE, Q), {}), (ON_CPU, (Q, K, K, Q, LSE, Q), dict(dq=Q, dk=K, dv=K)), (ON_CPU, (PQ, PK, PK, PQ, PLSE, PQ), dict(offsets_q=OFF, offsets_k=OFF)),
+    ("^k: .*does not go with", (Q, K[:1], K, Q, LSE, Q), {}), ("^v: .*expected", (Q, K, K[:, :6], Q, LSE, Q), {}), ("^v: torch.bfloat16", (Q, K, K.bfloat16(), Q, LSE, Q), {}),
+    ("^o: .*expected", (Q, K, K, Q[:, :4], LSE, Q), {}), ("^o: torch.bfloat16", (Q, K, K, Q.bfloat16(), LSE, Q), {}), ("^o: the elements", (Q, K, K, APART, LSE, Q), {}),
+    ("^o: needed", (Q, K, K, None, LSE, Q), {}), ("^lse: .*expected", (Q, K, K, Q, LSE[:1], Q), {}), ("^lse: .*expected", (Q, K, K, Q, LSE[:, :, :4], Q), {}),
+    ("^lse: .*expected", (PQ, PK, PK, PQ, PLSE.t().contiguous(), PQ), dict(offsets_q=OFF, offsets_k=OFF)), ("^lse: torch.bfloat16", (Q, K, K, Q, LSE.bfloat16(), Q), {}),
+    ("^lse: .*not contiguous", (Q, K, K, Q, torch.zeros(2, 5, 4).transpose(1, 2), Q), {}), ("^lse: needed", (Q, K, K, Q, None, Q), {}),
+    ("^do: .*expected", (Q, K, K, Q, LSE, K), {}), ("^do: torch.bfloat16", (Q, K, K, Q, LSE, Q.bfloat16()), {}), ("^do: the elements", (Q, K, K, Q, LSE, APART), {}), ("^do: needed", (Q, K, K, Q, LSE, None), {}),
+    ("^dq: .*expected", (Q, K, K, Q, LSE, Q), dict(dq=K)), ("^dk: .*expected", (Q, K, K, Q, LSE, Q), dict(dk=Q)), ("^dv: .*expected", (Q, K, K, Q, LSE, Q), dict(dv=K[:, :6])),
+    ("^dq: torch.bfloat16", (Q, K, K, Q, LSE, Q), dict(dq=Q.bfloat16())), ("^dq: the elements", (Q, K, K, Q, LSE, Q), dict(dq=APART)),
+    ("^offsets_q and offsets_k", (Q, K, K, Q, LSE, Q), dict(offsets_q=OFF))])
+def test_attention_backward_binding_says_what_it_refuses(text, args, kw):
+    refused(lambda: b.attention_backward(*args, **kw), text)
+
+
+RQ, RK, G, POS, FREQ = torch.zeros(5, 4, 32), torch.zeros(5, 2, 32), torch.ones(32), torch.zeros(5, 2, dtype=torch.int32), torch.zeros(16)
+ROT_SHARED = [      # (text, what is given in place of the usual)
+    ("^gamma_q: .*expected", dict(gq=G[:8])), ("^gamma_k: .*expected", dict(gk=G[:8])), ("^gamma_q: torch.bfloat16", dict(gq=G.bfloat16())), ("^gamma_k: torch.float64", dict(gk=G.double())),
+    ("^gamma_q: .*not contiguous", dict(gq=torch.ones(64)[::2])), ("^gamma_k: .*not contiguous", dict(gk=torch.ones(64)[::2])),
+    ("^positions: torch.int64", dict(pos=POS.long())), ("^positions: .*expected", dict(pos=POS[:4])), ("^positions: .*expected", dict(pos=POS[:, :1])), ("^positions: needed", dict(pos=None)),
+    ("^positions: .*expected", dict(sections=[16])), ("^positions: .*not contiguous", dict(pos=torch.zeros(2, 5, dtype=torch.int32).t())), ("^frequencies: .*expected", dict(freq=FREQ[:8])),
+    ("^frequencies: torch.float64", dict(freq=FREQ.double())), ("^frequencies: needed", dict(freq=None)), ("^frequencies: .*not contiguous", dict(freq=torch.zeros(32)[::2])),
+    ("^sections: at most 4", dict(sections=[2, 2, 4, 4, 4])), ("^q or k: one of them", dict(q=None, k=None)), ("^q: expected", dict(q=RQ[0], k=None)),
+    ("^k: .*does not go with", dict(k=RK[:4])), ("^k: .*does not go with", dict(k=RK[..., :16])), ("^k: .*does not go with", dict(k=RK[None])), ("^q: torch.float16", dict(q=RQ.half())),
+    ("^k: torch.float16", dict(q=None, k=RK.half()))]
+
+
+def rot_args(kw):
+    d = dict(q=RQ, k=RK, gq=G, gk=G, pos=POS, freq=FREQ, sections=[8, 8])
+    d.update(kw)
+    return d
+
+
+@pytest.mark.parametrize("text,kw", [(ON_CPU, {}), (ON_CPU, dict(q=None)), (ON_CPU, dict(k=None, gq=None)), (ON_CPU, dict(sections=[], pos=None, freq=None)), (ON_CPU, dict(yq=RQ, yk=RK))] + ROT_SHARED + [
+    ("^k: torch.bfloat16", dict(k=RK.bfloat16())), ("^q: the elements", dict(q=torch.zeros(5, 4, 64)[..., ::2])), ("^k: the elements", dict(k=torch.zeros(5, 2, 64)[..., ::2])),
+    ("^yq: .*expected", dict(yq=RK)), ("^yk: .*expected", dict(yk=RQ)), ("^yq: torch.bfloat16", dict(yq=RQ.bfloat16())), ("^yk: the elements", dict(yk=torch.zeros(5, 2, 64)[..., ::2]))])
+def test_norm_rotary_forward_binding_says_what_it_refuses(text, kw):
+    d = rot_args(kw)
+    refused(lambda: b.norm_rotary_forward(d["q"], d["k"], d["gq"], d["gk"], d["pos"], d["freq"], d["sections"], yq=d.get("yq"), yk=d.get("yk")), text)
+
+
+@pytest.mark.parametrize("text,kw", [(ON_CPU, {}), (ON_CPU, dict(q=None)), (ON_CPU, dict(k=None)), (ON_CPU, dict(xq=None, xk=None, norm=False)), (ON_CPU, dict(dq=RQ, dk=RK, dgq=G, dgk=G + 0))] + [
+    (text, kw) for text, kw in ROT_SHARED] + [
+    ("^dyk: torch.bfloat16", dict(k=RK.bfloat16())), ("^dyq: the elements", dict(q=torch.zeros(5, 4, 64)[..., ::2])), ("^q: needed", dict(xq=None)), ("^k: needed", dict(xk=None)),
+    ("^q: .*expected", dict(xq=RK)), ("^k: .*expected", dict(xk=RQ)), ("^q: torch.bfloat16", dict(xq=RQ.bfloat16())), ("^k: the elements", dict(xk=torch.zeros(5, 2, 64)[..., ::2])),
+    ("^dq: .*expected", dict(dq=RK)), ("^dk: .*expected", dict(dk=RQ)), ("^dq: torch.bfloat16", dict(dq=RQ.bfloat16())), ("^dgamma_q: .*expected", dict(dgq=G[:3])), ("^dgamma_k: torch.bfloat16", dict(dgk=G.bfloat16())),
+    ("^dgamma_q: .*not contiguous", dict(dgq=torch.ones(64)[::2]))])
+def test_norm_rotary_backward_binding_says_what_it_refuses(text, kw):
+    """(q and k of rot_args stand for the incoming gradients here, as which the sizes are taken; xq and xk for what was normed.)"""
+    d = rot_args(kw)
+    refused(lambda: b.norm_rotary_backward(d.get("xq", RQ), d.get("xk", RK), d["gq"], d["gk"], d["pos"], d["freq"], d["sections"], d["q"], d["k"], norm=d.get("norm", True),
+                                           dq=d.get("dq"), dk=d.get("dk"), dgamma_q=d.get("dgq"), dgamma_k=d.get("dgk")), text)
+
+
+@pytest.mark.parametrize("text,tensors", [
+    ("needs a tensor", []), ("tensor 0: all tensors belong on one GPU", [torch.zeros(3)]), ("^tensor 0: torch.float16", [torch.zeros(3, dtype=torch.float16)]),
+    ("^tensor 0: .*not contiguous", [torch.zeros(6)[::2]]), ("^tensor 0: needed", [None])])
+def test_gradient_table_says_what_it_refuses(text, tensors):
+    refused(lambda: b.gradient_table(tensors), text)
+
+
+@pytest.mark.parametrize("norm", [torch.zeros(2), torch.zeros(1, dtype=torch.float64), torch.zeros(1, dtype=torch.bfloat16), torch.zeros(())])
+def test_clip_gradients_says_what_it_refuses(norm):
+    table = b.GradientTable.__new__(b.GradientTable)
+    table.places, table.pointers = [], Place()
+    refused(lambda: b.clip_gradients(table, 1.0, norm=norm), "^norm: .*expected")
