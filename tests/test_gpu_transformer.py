@@ -83,6 +83,25 @@ def test_norm_rotary(dat, shape, dtype, layout):
     check_rotary(dat, x, dy, pos, None, None, sections, layout, norm=False)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", ROT + [(20011, 6, 3, 80, [20, 20]), (70001, 2, 1, 64, [32])])
+def test_gradients_of_scales_by_the_sums_they_are(dat, shape, dtype):
+    """At most 512 workgroups of four waves: a lane adds up the heads of every 2048th token, a workgroup the lanes of an element (1024 / D of a wave
+    at most hold the same one), then eight workgroups a thread and 64 threads."""
+    T, H, Hkv, D, sections = shape
+    x, dy, pos, gq, gk = rot_inputs(70, *shape, dtype)
+    freq = dat.rotary_frequencies(sections)
+    w = pt.angles(pos.cpu().numpy(), freq.cpu().numpy(), sections)
+    for layout in (dat.ROTARY_HALVES, dat.ROTARY_PAIRS):
+        g = dat.norm_rotary_backward(*x, gq, gk, pos, freq, sections, *dy, layout)
+        for n, gamma in enumerate((gq, gk)):
+            if x[n] is None:
+                continue
+            _, dg, _, gsize = pt.norm_rotary_backward(host(x[n]), host(dy[n]), host(gamma), w, layout == dat.ROTARY_HALVES, 1e-6)
+            chain = math.ceil(T / 2048) * x[n].shape[1] + 4096 / D + 8 + 64
+            assert_near(host(g[2 + n]), dg, (chain + D / 8 + 40) * U * gsize, "dgamma")
+
+
 @pytest.mark.parametrize("far", [10**6, 2**31 - 1001, -(2**31) + 50])
 def test_far_positions(dat, far):
     x, dy, pos, gq, gk = rot_inputs(20, 40, 2, 2, 64, [20, 12], F32, far)
@@ -407,6 +426,50 @@ def test_training_step_of_a_layer(dat, capture):
         step()                                    # eager, into the same buffers: the same bits
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(again, (grad, dx, norm)))
+
+
+def test_attack_on_a_layer(dat):
+    """An attack's steps through the operators: the gradient by the input of a layer (projection, norm and rotation, attention, log probabilities)
+    moves the start point by dat.pgd_update; each step's gradient against autograd in 64 bits at the GPU's own point."""
+    B, S, C, H, Hkv, D, V, eps, alpha = 3, 20, 24, 4, 2, 32, 10, 8 / 255, 3 / 255
+    g = torch.Generator().manual_seed(1)
+    T, sizes = B * S, [C * (H + 2 * Hkv) * D, H * D * C, C * V]
+    w, out, head = (t.view(a, -1) for t, a in zip([torch.randn(n, generator=g).cuda() * s for n, s in zip(sizes, (0.3, 0.2, 0.4))], (C, H * D, C)))
+    gq, gk = 1 + 0.1 * randn(2, D), 1 + 0.1 * randn(3, D)
+    x, labels = torch.rand(B, S, C, generator=g).cuda(), torch.randint(0, V, (T,), generator=g, dtype=torch.int32).cuda()
+    pos = torch.stack([torch.arange(S) // 5, torch.arange(S) % 5], 1).int().cuda().expand(B, S, 2).contiguous()
+    freq = dat.rotary_frequencies([8, 8])
+    angle = torch.from_numpy(pt.angles(pos[0].cpu().numpy(), freq.cpu().numpy(), [8, 8]))
+    delta = dat.pgd_init(x, eps, dat.INIT_UNIFORM, seed=5)
+
+    def gradient(z):
+        qkv = (z.view(T, C) @ w).view(B, S, H + 2 * Hkv, D)
+        q, k, v = torch.split(qkv, [H, Hkv, Hkv], dim=2)
+        yq, yk = dat.norm_rotary_forward(q, k, gq, gk, pos, freq, [8, 8])
+        o, lse = dat.attention_forward(yq, yk, v)
+        logits = (o.view(T, H * D) @ out) @ head
+        lp = dat.log_probs(logits, labels)
+        dz = dat.log_probs_backward(logits, labels, lp[2], dlogp=torch.full((T,), -1.0 / T, device="cuda"))
+        do = ((dz @ head.t()) @ out.t()).view(B, S, H, D)
+        dqkv = torch.empty_like(qkv)
+        dq, dk, dv = torch.split(dqkv, [H, Hkv, Hkv], dim=2)
+        dat.attention_backward(yq, yk, v, o, lse, do, dq=dq, dk=dk, dv=dv)
+        dat.norm_rotary_backward(q, k, gq, gk, pos, freq, [8, 8], dq, dk, dq=dq, dk=dk)
+        return (dqkv.view(T, -1) @ w.t()).view_as(z)
+
+    p64 = [t.double().cpu() for t in (w, out, head, gq, gk)]
+    for _ in range(3):
+        z = dat.make_xadv(x, delta)
+        got = gradient(z)
+        z64 = z.double().cpu().requires_grad_(True)
+        sum(plain_step(z64[n], *p64, labels.long().cpu().view(B, S)[n], angle, H, Hkv, D, (-1, -1)) / B for n in range(B)).backward()
+        # every stage's relative error of about a hundred roundings, through six stages: 600 U = 4e-5 of the gradient's size
+        assert float((got.double().cpu() - z64.grad).norm()) < 4e-5 * float(z64.grad.norm())
+        want = torch.clamp(delta.double() + alpha * torch.sign(got.double()), -eps, eps)
+        want = torch.clamp(x.double() + want, 0, 1) - x.double()
+        before = delta.clone()
+        dat.pgd_update(x, got, delta, eps, alpha)
+        assert float((delta.double() - want).abs().max()) < 4 * U and not torch.equal(before, delta)
 
 
 def test_two_graphs_do_not_share_workspaces(dat):
