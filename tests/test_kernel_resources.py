@@ -85,3 +85,24 @@ def test_inline_assembly_names_what_it_overwrites():
             if re.search(r"\blds\b|s_waitcnt|s_barrier", text):
                 assert '"memory"' in clobbers, (name, text)
     assert seen >= 2
+
+
+def test_transformer_operators_spill_where_their_comments_say():
+    """Forward passes spill nothing; backward ones at most what they keep outside their loops over tiles or heads (heads of 112 and more; rotations with 16-byte vectors in bf16)."""
+    seen = 0
+    for k in _kernels():
+        m = re.search(r"(attn_fwd|attn_dq|attn_dkv|attn_join|rotary_forward|rotary_backward|rotary_dgamma|clip)_kernelI?([tf]?)(?:Li(\d+)E)?", k[".name"])
+        if not m or "_GLOBAL__N_1" not in k[".name"]:
+            continue
+        seen += 1
+        name, kind, blocks = m.group(1), m.group(2), int(m.group(3) or 0)
+        most = 0
+        if blocks == 4 and name == "attn_dkv":
+            most = 17 if kind == "t" else 67
+        if blocks == 4 and name == "attn_dq" and kind == "t":
+            most = 17
+        if blocks == 8 and name == "rotary_backward":
+            most = 48
+        assert k[".vgpr_spill_count"] <= most, (k[".name"], k[".vgpr_spill_count"])
+        assert most or k[".private_segment_fixed_size"] == 0, k[".name"]
+    assert seen >= 60
