@@ -5,7 +5,7 @@
     python -m paper_2206_06257_amd.profile_summary mfma    <dir> <prefix> <workload>
 
 The rocprofv3 commands that produce the inputs are written at the head of every summary.  `traffic` also writes
-profiles/traffic_igemm_<workload>.json, which carries a hash of the kernel sources so that bench.py reports the
+profiles/traffic_igemm_<workload>.json, which carries a hash of the step's kernel sources so that bench.py reports the
 figure only while the sources are the ones it was measured on."""
 import collections
 import csv
@@ -19,12 +19,22 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 PROFILES = os.path.join(ROOT, "profiles")
 
 
+STEP_SOURCES = ("conv_direct.hip", "conv_mfma.hip", "layers.hip", "model.hip", "optim.hip", "pgd.hip", "quantize.hip")
+
+
 def source_hash():
-    h = hashlib.sha256()
+    """Of the sources that the step's kernels come from (the operators on their own are no part of it) and the headers that they include."""
     csrc = os.path.join(ROOT, "paper_2206_06257_amd", "csrc")
-    for name in sorted(os.listdir(csrc)):
+    texts, names = {}, list(STEP_SOURCES)
+    while names:
+        name = names.pop()
+        if name not in texts:
+            texts[name] = open(os.path.join(csrc, name), "rb").read()
+            names += [m.decode() for m in re.findall(rb'^#include "([^"/]+)"', texts[name], re.M)]
+    h = hashlib.sha256()
+    for name in sorted(texts):
         h.update(name.encode())
-        h.update(open(os.path.join(csrc, name), "rb").read())
+        h.update(texts[name])
     return h.hexdigest()[:16]
 
 
