@@ -343,14 +343,14 @@ dat_status dat_group_norm_backward(const void* x, const void* dy, const float* g
  * limit on that side; left = -1, right = 0 is causal.
  *   forward:   S = scale q k^T over what a row sees, lse = log sum_j exp S_j, P = exp(S - lse), o = P v; a row that sees nothing has o = 0,
  *              lse = -inf.  lse: device fp32 [B][H][Sq] ([H][Sq] packed).
- *   backward (o and lse: the forward call's for the same shape):  D = sum_d d_o o, dP = d_o v^T, dS = P (dP - D); dq = scale dS k,
+ *   backward (o and lse: the forward call's for the same shape, not merged with those of other keys):  D = sum_d d_o o, dP = d_o v^T, dS = P (dP - D); dq = scale dS k,
  *              dk = scale dS^T q and dv = P^T d_o, over all heads that share the key head.  P is made again from q, k and lse; sums in a
  *              fixed order (the same bits on every call).  A query that sees one key has dq = 0 and adds
  *              nothing to dk.
  * Sums, statistics and S, P, dP, dS in fp32; bf16 rounds P and dS to bf16 where they enter a product, and the outputs once.  What a row
  * does not see does not enter it, whatever it holds; where it sees a value that is not finite, elements of its result may be NaN where
- * the sum is infinite.  Scores have to stay within fp32 (an infinite one that is not -inf makes its row
- * NaN), and so do v times 256 keys (o is divided by its probabilities' sum at the end).
+ * the sum is infinite.  Scores, before and after the scale, and times 1 / ln 2, have to stay within fp32 (an infinite one that is not
+ * -inf makes its row NaN), and so do v times 256 keys (o is divided by its probabilities' sum at the end).
  * Outputs, lse among them, overlap neither inputs nor each other (parts of one tensor, with the same strides, are fine between each other).  workspace: device, 16-byte aligned,
  * dat_attention_workspace(pass, shape) bytes (pass 0 forward, 1 backward; may be 0, then NULL is allowed); nothing in it outlives the
  * call.  Asynchronous on `stream`, no allocation.

@@ -730,7 +730,8 @@ def _lse_shape(q, batched):
 def attention_forward(q, k, v, scale=None, window=(-1, -1), offsets_q=None, offsets_k=None, o=None, stream=None):
     """q [B, Sq, H, D], k and v [B, Sk, Hkv, D], or packed sequences [T, H, D] with int32 offsets [B + 1]; fp32 or bf16, any strides
     between tokens and heads -> (o like q, lse fp32 [B, H, Sq] or [H, T]).  window = (left, right): keys that a query sees beside its own
-    place, -1 for all of them, (-1, 0) is causal; scale: 1 / sqrt(D) for None.  See dat_attention_forward."""
+    place, -1 for all of them, (-1, 0) is causal; scale: 1 / sqrt(D) for None.  Packed tokens in no sequence: their rows of o and lse are not
+    written (uninitialised, where this call makes o).  See dat_attention_forward."""
     shape, need, batched = _attention(q, k, scale, window, offsets_q, offsets_k)
     dtype, qs, ks = q.dtype, q.shape, k.shape
     hq, hk, hv, ho = _heads("q", q, dtype, qs), _heads("k", k, dtype, ks), _heads("v", v, dtype, ks), _heads("o", o, dtype, qs, optional=True)
@@ -745,7 +746,8 @@ def attention_forward(q, k, v, scale=None, window=(-1, -1), offsets_q=None, offs
 
 
 def attention_backward(q, k, v, o, lse, do, scale=None, window=(-1, -1), offsets_q=None, offsets_k=None, dq=None, dk=None, dv=None, stream=None):
-    """Gradients of attention_forward's o from its o and lse and the incoming gradient do -> (dq, dk, dv)."""
+    """Gradients of attention_forward's o from its o and lse and the incoming gradient do -> (dq, dk, dv).  Packed tokens in no sequence: their rows are
+    not written (uninitialised, where this call makes the gradients)."""
     shape, need, batched = _attention(q, k, scale, window, offsets_q, offsets_k)
     dtype, qs, ks = q.dtype, q.shape, k.shape
     given = [_heads(name, t, dtype, like) for name, t, like in (("q", q, qs), ("k", k, ks), ("v", v, ks), ("o", o, qs))]

@@ -15,8 +15,10 @@
 // and about 150 vector instructions, a third of them exponentials and their arguments (at D = 64 16 products, and the vector work is the
 // longer).  The waves of different workgroups on a SIMD fill each other's gaps; inside a wave fragments are read ahead of their
 // products.  Memory: a tile of 64 rows comes in once for 128 rows of the result, 4 to 5 TB/s out of the L2s, and nothing of S x S size is
-// written.  Measured, operations that the mask leaves: forward 1 x 8192 tokens, 32 heads of 128 on 8, causal 497 us (1107 TFLOP/s; a plain
-// product of 8192^3 reaches 1216 here); 32 x 1024 tokens, 16 heads of 64 188 us (730); 2 x 4096 tokens 165 us (833).
+// written.  Measured over several cards, operations that the mask leaves: forward 1 x 8192 tokens, 32 heads of 128 on 8, causal 497 to 525 us (1107 to
+// 1047 TFLOP/s; a plain product of 8192^3 reaches 1216 here); 32 x 1024 tokens, 16 heads of 64 188 us (730); 2 x 4096 tokens 165 us (833).
+// bf16 calls round P and dS to bf16 where they enter a product (fp32 ones run at an eighth of the rate): outputs are then 2.1e-3 to 2.5e-3 of their norm
+// off, where the one rounding at the end leaves 1.7e-3.  Nothing else is rounded to less than fp32.
 // Why 32 rows a wave and 128 a workgroup: 64 rows a wave halve the reads of LDS, but need 512 registers, one wave a SIMD (causal
 // 302 -> 392 us at 32 x 1024 x 16 x 128); 256 rows a workgroup (8 waves) 504 -> 493 us on the 8192 tokens, slower on all shorter ones.
 #include "kernels.h"
@@ -584,7 +586,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_fwd_kernel(AttnArgs a) {
 // ---- gradient by the queries; -D and lse / ln 2 for the pass over the keys --------------------------------------------------
 // The rows of o and d_o are here anyway, so D is made here and no launch of its own reads them.  Three products a pair of tiles; keys by halves of a
 // tile, which needs 32 registers less than both at once and leaves room for two or three workgroups a compute unit.  2 x 6001 tokens, 16
-// heads of 128 on 4, causal: 409 us, 1080 TFLOP/s; 32 x 577 tokens, 16 heads of 64: 93 us, 700 TFLOP/s (640 keys in tiles for 577).
+// heads of 128 on 4, causal: 397 to 419 us, 1110 to 1050 TFLOP/s, matrix cores busy 54 to 57 % of the time; 32 x 577 tokens, 16 heads of 64: 93 to 100 us, 700 to
+// 650 TFLOP/s (640 keys in tiles for 577).
 // (A half tile that no row sees left out: 1112 -> 1147 us for the whole gradient, the test breaks the order of the loads.)
 template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
@@ -708,8 +711,8 @@ __global__ __launch_bounds__(NW * 64, OCC) void attn_dq_kernel(AttnArgs a) {
 // A wave owns 32 keys, its lanes a key each, and walks over the queries of every head of its group: no sum leaves the workgroup (or the
 // parts, which are added in their order), and the order is always the same.
 // Four products a pair of tiles; two accumulators and two own operands of 128 elements take 192 of the 512 registers that one wave a SIMD
-// has at D > 64, so little runs beside its vector work, waits and barriers: 2 x 6001 tokens as above 650 to 710 us by clock, 830 to 900 TFLOP/s, matrix
-// cores busy 43 % of the time (dq 56 %); 32 x 577 tokens, 16 heads of 64, two waves a SIMD: 122 us, 715 TFLOP/s.  Forming one block's probabilities
+// has at D > 64, so little runs beside its vector work, waits and barriers: 2 x 6001 tokens as above 650 to 737 us by card and clock, 900 to 800 TFLOP/s,
+// matrix cores busy 37 % of the time; 32 x 577 tokens, 16 heads of 64, two waves a SIMD: 122 to 141 us, 715 to 620 TFLOP/s.  Forming one block's probabilities
 // under the other's products gave 2 % there and lost 20 % at D = 64 (registers); more fragments ahead gave nothing.
 template <typename T, int NB, int KK, int NW, int OCC>
 __global__ __launch_bounds__(NW * 64, OCC) void attn_dkv_kernel(AttnArgs a) {
@@ -922,7 +925,8 @@ enum { kForward, kGradQ, kGradKV };
 constexpr int kWavesOf = 4, kRows = 32 * kWavesOf, kUnits = 256, kMostParts = 32;
 
 // Workgroups of a pass that a compute unit holds at least (one wave of each on every SIMD): what their registers leave room for without spilling
-// in the loops.  Three where 168 a lane are enough (bf16 heads of up to 64, forward and dq), two with 256, one with 512.
+// in the loops over tiles.  Three where 168 a lane are enough (bf16 heads of up to 64, forward and dq), two with 256, one with 512.  Outside these loops heads of
+// 112 and more spill: 17 registers in dq (bf16, 128) and in dk and dv (bf16, 128), 49 and 67 there in fp32.
 constexpr int occupancy(bool half_width, int nb, int pass) {
   return pass == kGradKV ? (half_width && nb <= 2 ? 2 : 1) : half_width && nb <= 2 ? 3 : half_width || nb <= 2 ? 2 : 1;
 }
