@@ -445,3 +445,18 @@ def test_a_query_of_one_key_adds_nothing_to_dk(dat, Sq, Sk, window, dtype):
     _, dk, dv = dat.attention_backward(q, k, v, o, lse, do, window=window)
     key = see[alone].any(0)
     assert bool(torch.isnan(dk[0, key, 0]).all()) and bool((dk[0, ~key] == 0).all()) and bool((dk[1] == 0).all()) and bool((dk[:, :, 1] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [(-1, 0), (0, -1), (16, 5), (0, 3)])
+def test_packed_queries_of_one_key_add_nothing_to_dk(dat, window, dtype):
+    """The same in packed sequences, each with its own first and last keys."""
+    lq, lk = [1, 70, 0, 129, 64, 3, 33], [40, 70, 5, 50, 97, 1, 33]
+    oq, ok = (torch.tensor(np.cumsum([0] + n), dtype=torch.int32, device="cuda") for n in (lq, lk))
+    q, k, v, do = randn(1, sum(lq), 4, 40).to(dtype), randn(2, sum(lk), 2, 40).to(dtype), randn(3, sum(lk), 2, 40).to(dtype), randn(4, sum(lq), 4, 40).to(dtype)
+    check(dat, q, k, v, do, window=window, offsets_q=oq, offsets_k=ok)
+    alone = torch.cat([torch.from_numpy(pt.seen(a, c, window)).sum(1) == 1 for a, c in zip(lq, lk)]).cuda()
+    assert 1 < int(alone.sum()) < len(alone)
+    do[~alone] = 0
+    _, _, (dq, dk, dv) = check(dat, q, k, v, do, window=window, offsets_q=oq, offsets_k=ok)
+    assert bool((dk == 0).all()) and bool((dq == 0).all()) and bool((dv != 0).any())
